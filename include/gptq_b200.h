@@ -282,6 +282,70 @@ int gptq_dequant_f32_w8(const void *qweight, const void *qzeros, const void *sca
 int gptq_gemm_w8(const void *x, const void *qweight, const void *qzeros, const void *scales, const int32_t *perm,
                  void *y, int M, int N, int K, int group_size, void *stream);
 
+/* ---- rows that choose their weights (no counterpart in the paper, whose models are dense - Section 4.1) ---------------- */
+
+/* The choice of experts in a mixture-of-experts layer: for each of M tokens the top_k largest of its E logits, in descending
+ * order, equal logits by ascending expert: expert_ids int32[M, top_k], and their weights fp32[M, top_k] = softmax over all E
+ * logits (renormalize = 0), or over the chosen ones (renormalize != 0: they sum to one).  logits: [M, E] of logits_type.
+ * A logit of -inf or NaN is an expert that cannot be chosen and has no share in the softmax; +inf counts as the largest finite
+ * number.  Where fewer than top_k can be chosen, the rest of the row is expert -1 with weight 0.
+ * E <= 1024, top_k <= 32 (GPTQ_ERR_UNSUPPORTED), top_k <= E (GPTQ_ERR_SHAPE); pointers 16-byte aligned; an unknown
+ * logits_type: GPTQ_ERR_LAYOUT. */
+#define GPTQ_LOGITS_F32 0
+#define GPTQ_LOGITS_F16 1
+#define GPTQ_LOGITS_BF16 2
+int gptq_moe_route(const void *logits, int32_t *expert_ids, float *expert_weights, int M, int E, int top_k, int logits_type,
+                   int renormalize, void *stream);
+
+/* A whole mixture-of-experts MLP for a few tokens:
+ *     y[m] = residual[m] + sum_j expert_weights[m][j] * ( (silu(x[m] Wg[e]) * (x[m] Wu[e])) Wd[e] ),  e = expert_ids[m][j]
+ * x, residual (or NULL), y fp16 [M, K]; expert_ids int32 [M, top_k]; expert_weights fp32 [M, top_k] (gptq_moe_route's outputs, or
+ * any numbers).  An id outside 0 .. E-1 is a slot that is not used (a padding row: all -1; its y is the residual, or 0); an expert
+ * named twice by a token gets the sum of the two weights.
+ * Experts: layer e of each kind is an ordinary tiled layer, written by gptq_repack_format to
+ * buffer + e * gptq_repack_bytes(which, ...): gate_up [K, 2 F] with GPTQ_FORMAT_GATE_UP (all of them or none with
+ * GPTQ_FORMAT_ZEROS_MINUS_ONE), down [F, K] without it; K and F multiples of 128.  group_size is that of both (a multiple of 128
+ * counts as 128, the way such layers are tiled; layers with one group per column: pass 128).
+ * act_order = 1: gate_up_perm int32 [E, K] = the gate_up layers' perm_out, down_index int32 [E, F] = gptq_invert_perm of the down
+ * layers' perm_out.  0: both ignored, may be NULL.  (GPTQ_ACT_ORDER_PRESORTED is refused: each expert has an order of its own.)
+ * Arithmetic: exact integers q - z times x, fp32 sums, scales in fp32; the activation in fp32, rounded once to fp16 (a value
+ * beyond 65504 becomes an infinity); weights, sums over experts and residual in fp32, one rounding of y.  The order of the sums
+ * is fixed: the same inputs give the same bits.
+ * residual may be y; y may be x.  Scratch: gptq_moe_workspace_bytes of the registered workspace (GPTQ_ERR_WORKSPACE without it),
+ * under the rules of gptq_set_workspace: calls, and graphs captured from calls, that may run at the same time must not share one.
+ * Each expert in use is read once for up to 8 of its tokens (M <= 8), 16 (M <= 16) or 32; M > 64 runs as passes of 64 tokens.  Two kernels per
+ * pass, three with act_order.  Layers of another tiling: nothing is stored, and gptq_check_status returns GPTQ_ERR_LAYOUT.
+ * E <= 1024, top_k <= 32 (GPTQ_ERR_UNSUPPORTED).  Stream semantics and other errors as for gptq_gemm. */
+size_t gptq_moe_workspace_bytes(int M, int K, int F, int top_k, int act_order);
+int gptq_moe_mlp(const void *x, const int32_t *expert_ids, const float *expert_weights, const void *gate_up_qweight,
+                 const void *gate_up_qzeros, const void *gate_up_scales, const int32_t *gate_up_perm, const void *down_qweight,
+                 const void *down_qzeros, const void *down_scales, const int32_t *down_index, const void *residual, void *y, int M, int K,
+                 int F, int E, int top_k, int group_size, int act_order, void *stream);
+/* The same for layers repacked with GPTQ_FORMAT_BF16: x, residual, y and the activation are bfloat16. */
+int gptq_moe_mlp_bf16(const void *x, const int32_t *expert_ids, const float *expert_weights, const void *gate_up_qweight,
+                      const void *gate_up_qzeros, const void *gate_up_scales, const int32_t *gate_up_perm, const void *down_qweight,
+                      const void *down_qzeros, const void *down_scales, const int32_t *down_index, const void *residual, void *y, int M,
+                      int K, int F, int E, int top_k, int group_size, int act_order, void *stream);
+
+/* gptq_gemm with a low-rank adapter per row, the adapters of many requests at once:
+ *     y[m] = x[m] . dequant(W) + adapter_scales[a] * (x[m] A[a]^T) B[a]^T,   a = adapter_ids[m]
+ * lora_a fp16 [adapters, rank, K], lora_b fp16 [adapters, N, rank] (each as the two linear layers of an adapter store their
+ * weights; an adapter of lower rank is padded with zero rows of A or zero columns of B), adapter_ids int32 [M],
+ * adapter_scales fp32 [adapters] or NULL (1).  An id outside 0 .. adapters-1: the row has no adapter.  rank: a multiple of 8 up
+ * to 256 (GPTQ_ERR_UNSUPPORTED).  W, x, y, g_idx, act_order, errors and accuracy of the product with W as for gptq_gemm; with
+ * act_order = 1 x and lora_a are in the checkpoint's row order, with GPTQ_ACT_ORDER_PRESORTED both are in the sorted one.
+ * x A^T, scaled, is summed and kept in fp32.  Up to 16 rows the expansion joins the fp32 sums before the one rounding of y; above,
+ * it is rounded to 16 bits on its way to them.  y must not be x.  Scratch: gptq_lora_workspace_bytes of the registered workspace,
+ * always needed.  A layer tiled with GPTQ_FORMAT_GATE_UP or GPTQ_FORMAT_BF16 is refused as by gptq_gemm. */
+size_t gptq_lora_workspace_bytes(int M, int N, int K, int group_size, int act_order, int rank);
+int gptq_gemm_lora(const void *x, const void *qweight, const void *qzeros, const void *scales, const int32_t *g_idx,
+                   const void *lora_a, const void *lora_b, const int32_t *adapter_ids, const float *adapter_scales, void *y,
+                   int M, int N, int K, int group_size, int act_order, int rank, int adapters, void *stream);
+/* The same for layers repacked with GPTQ_FORMAT_BF16: x, lora_a, lora_b and y are bfloat16. */
+int gptq_gemm_lora_bf16(const void *x, const void *qweight, const void *qzeros, const void *scales, const int32_t *g_idx,
+                        const void *lora_a, const void *lora_b, const int32_t *adapter_ids, const float *adapter_scales, void *y,
+                        int M, int N, int K, int group_size, int act_order, int rank, int adapters, void *stream);
+
 /* Process-wide switch: with enable != 0, gptq_gemm runs problems with M >= 256 and an even number
  * of 128-column panels on CTA pairs (tcgen05.mma.cta_group::2: two SMs share one 256 x 256 x 16 MMA and
  * each loads half of the x tile).  Same arithmetic and tolerance as the default kernel; it halves the

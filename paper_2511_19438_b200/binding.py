@@ -26,6 +26,7 @@ GPTQ_FORMAT_ZEROS_MINUS_ONE = 1
 GPTQ_FORMAT_GATE_UP = 2
 GPTQ_FORMAT_BF16 = 4
 GPTQ_ACT_ORDER_PRESORTED = 2
+GPTQ_LOGITS_F32, GPTQ_LOGITS_F16, GPTQ_LOGITS_BF16 = 0, 1, 2
 GPTQ_OK = 0
 GPTQ_ERR_NULL = -1
 GPTQ_ERR_SHAPE = -2
@@ -85,6 +86,13 @@ _SIGNATURES = {
     "gptq_gemm_bias_residual": (_i, [_vp] * 8 + [_i, _i, _i, _i, _i, _vp]),
     "gptq_gemm_silu_mul_scatter": (_i, [_vp] * 7 + [_i, _i, _i, _i, _i, _vp]),
     "gptq_invert_perm": (_i, [_vp, _vp, _i, _vp]),
+    "gptq_moe_route": (_i, [_vp] * 3 + [_i] * 5 + [_vp]),
+    "gptq_moe_workspace_bytes": (_sz, [_i] * 5),
+    "gptq_moe_mlp": (_i, [_vp] * 13 + [_i] * 7 + [_vp]),
+    "gptq_moe_mlp_bf16": (_i, [_vp] * 13 + [_i] * 7 + [_vp]),
+    "gptq_lora_workspace_bytes": (_sz, [_i] * 6),
+    "gptq_gemm_lora": (_i, [_vp] * 10 + [_i] * 7 + [_vp]),
+    "gptq_gemm_lora_bf16": (_i, [_vp] * 10 + [_i] * 7 + [_vp]),
     "gptq_set_cta_pairs": (_i, [_i]),
     "gptq_gemm_host": (_i, [_vp] * 8 + [_i, _i, _i, _i, _i, _vp]),
     "gptq_gemm_noalloc": (_i, [_vp] * 6 + [_i, _i, _i, _i, _i, _vp]),
@@ -258,6 +266,53 @@ def gptq_dequant_f32_w8(qweight, qzeros, scales, g_idx, w_out, N, K, group_size,
 def gptq_gemm_w8(x, qweight, qzeros, scales, perm, y, M, N, K, group_size, stream=None) -> int:
     return _lib.gptq_gemm_w8(_ptr(x), _ptr(qweight), _ptr(qzeros), _ptr(scales), _ptr(perm), _ptr(y), M, N, K, group_size,
                              _stream(stream))
+
+
+def gptq_moe_route(logits, expert_ids, expert_weights, M, E, top_k, logits_type, renormalize, stream=None) -> int:
+    return _lib.gptq_moe_route(_ptr(logits), _ptr(expert_ids), _ptr(expert_weights), M, E, top_k, int(logits_type),
+                               int(bool(renormalize)), _stream(stream))
+
+
+def gptq_moe_workspace_bytes(M, K, F, top_k, act_order) -> int:
+    return _lib.gptq_moe_workspace_bytes(M, K, F, top_k, int(act_order))
+
+
+def _moe_mlp(fn, x, ids, weights, gu_qw, gu_qz, gu_sc, gu_perm, dn_qw, dn_qz, dn_sc, dn_index, residual, y, M, K, F, E, top_k,
+             group_size, act_order, stream):
+    return fn(_ptr(x), _ptr(ids), _ptr(weights), _ptr(gu_qw), _ptr(gu_qz), _ptr(gu_sc), _ptr(gu_perm), _ptr(dn_qw), _ptr(dn_qz),
+              _ptr(dn_sc), _ptr(dn_index), _ptr(residual), _ptr(y), M, K, F, E, top_k, group_size, int(act_order), _stream(stream))
+
+
+def gptq_moe_mlp(x, expert_ids, expert_weights, gate_up_qweight, gate_up_qzeros, gate_up_scales, gate_up_perm, down_qweight,
+                 down_qzeros, down_scales, down_index, residual, y, M, K, F, E, top_k, group_size, act_order, stream=None) -> int:
+    return _moe_mlp(_lib.gptq_moe_mlp, x, expert_ids, expert_weights, gate_up_qweight, gate_up_qzeros, gate_up_scales, gate_up_perm,
+                    down_qweight, down_qzeros, down_scales, down_index, residual, y, M, K, F, E, top_k, group_size, act_order, stream)
+
+
+def gptq_moe_mlp_bf16(x, expert_ids, expert_weights, gate_up_qweight, gate_up_qzeros, gate_up_scales, gate_up_perm, down_qweight,
+                      down_qzeros, down_scales, down_index, residual, y, M, K, F, E, top_k, group_size, act_order,
+                      stream=None) -> int:
+    return _moe_mlp(_lib.gptq_moe_mlp_bf16, x, expert_ids, expert_weights, gate_up_qweight, gate_up_qzeros, gate_up_scales,
+                    gate_up_perm, down_qweight, down_qzeros, down_scales, down_index, residual, y, M, K, F, E, top_k, group_size,
+                    act_order, stream)
+
+
+def gptq_lora_workspace_bytes(M, N, K, group_size, act_order, rank) -> int:
+    return _lib.gptq_lora_workspace_bytes(M, N, K, group_size, int(act_order), rank)
+
+
+def gptq_gemm_lora(x, qweight, qzeros, scales, g_idx, lora_a, lora_b, adapter_ids, adapter_scales, y, M, N, K, group_size,
+                   act_order, rank, adapters, stream=None) -> int:
+    return _lib.gptq_gemm_lora(_ptr(x), _ptr(qweight), _ptr(qzeros), _ptr(scales), _ptr(g_idx), _ptr(lora_a), _ptr(lora_b),
+                               _ptr(adapter_ids), _ptr(adapter_scales), _ptr(y), M, N, K, group_size, int(act_order), rank, adapters,
+                               _stream(stream))
+
+
+def gptq_gemm_lora_bf16(x, qweight, qzeros, scales, g_idx, lora_a, lora_b, adapter_ids, adapter_scales, y, M, N, K, group_size,
+                        act_order, rank, adapters, stream=None) -> int:
+    return _lib.gptq_gemm_lora_bf16(_ptr(x), _ptr(qweight), _ptr(qzeros), _ptr(scales), _ptr(g_idx), _ptr(lora_a), _ptr(lora_b),
+                                    _ptr(adapter_ids), _ptr(adapter_scales), _ptr(y), M, N, K, group_size, int(act_order), rank,
+                                    adapters, _stream(stream))
 
 
 def gptq_set_cta_pairs(enable) -> int:

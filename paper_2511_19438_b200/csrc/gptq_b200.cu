@@ -10,6 +10,9 @@
 #include "gptq_umma2.cuh"
 #include "gptq_w8.cuh"
 #include "gptq_wn.cuh"
+#include "gptq_direct.cuh"
+#include "gptq_moe.cuh"
+#include "gptq_lora.cuh"
 
 #include <atomic>
 #include <cstdio>
@@ -458,7 +461,8 @@ static int gemm_dispatch(const void *x, const void *qweight, const void *qzeros,
     cudaStream_t s = (cudaStream_t)stream;
     const __half *xin = (const __half *)x;
     const bool extras = bias != nullptr || residual != nullptr;
-    if (bf16 && (fuse || extras)) return GPTQ_ERR_UNSUPPORTED;     // the fused epilogues exist for fp16 only
+    // the fused epilogues exist for fp16 only, but for the additions of the tcgen05 kernels (gptq_gemm_lora_bf16)
+    if (bf16 && (fuse || (extras && M < kUmmaMinTokens))) return GPTQ_ERR_UNSUPPORTED;
     if (act_order == 1) {
         Workspace ws;
         {
@@ -1137,6 +1141,186 @@ int gptq_check_status(void *stream)
     if (e == cudaSuccess) e = cudaStreamSynchronize(s);
     if (e != cudaSuccess) return record_cuda_error(e);
     return status == kStatusLayoutMismatch ? GPTQ_ERR_LAYOUT : GPTQ_ERR_TIMEOUT;
+}
+
+// ---- rows that choose their weights: routed experts (gptq_moe.cuh), low-rank adapters (gptq_lora.cuh) ----------------------
+
+int gptq_moe_route(const void *logits, int32_t *expert_ids, float *expert_weights, int M, int E, int top_k, int logits_type,
+                   int renormalize, void *stream)
+{
+    if (!logits || !expert_ids || !expert_weights) return GPTQ_ERR_NULL;
+    if (logits_type < GPTQ_LOGITS_F32 || logits_type > GPTQ_LOGITS_BF16) return GPTQ_ERR_LAYOUT;
+    if (M < 1 || E < 1 || top_k < 1 || top_k > E) return GPTQ_ERR_SHAPE;
+    if (E > kMoeMaxExperts || top_k > kMoeMaxTopK) return GPTQ_ERR_UNSUPPORTED;
+    if (!aligned16(logits) || !aligned16(expert_ids) || !aligned16(expert_weights)) return GPTQ_ERR_ALIGN;
+    return launch_route(logits, logits_type, expert_ids, expert_weights, M, E, top_k, renormalize != 0, (cudaStream_t)stream);
+}
+
+size_t gptq_moe_workspace_bytes(int M, int K, int F, int top_k, int act_order)
+{
+    if (M < 1 || K < kGroup || F < kGroup || K % kGroup || F % kGroup || top_k < 1 || top_k > kMoeMaxTopK) return 0;
+    return moe_workspace_need(M, K, F, top_k, act_order);
+}
+
+}  // extern "C"
+
+static int registered_workspace(int dev, size_t need, uint8_t **out)
+{
+    std::lock_guard<std::mutex> lock(g_mutex);
+    if (g_workspace[dev].ptr == nullptr || g_workspace[dev].bytes < need) return GPTQ_ERR_WORKSPACE;
+    *out = (uint8_t *)g_workspace[dev].ptr;
+    return GPTQ_OK;
+}
+
+static int moe_dispatch(const void *x, const int32_t *ids, const float *weights, const void *gu_qweight, const void *gu_qzeros,
+                        const void *gu_scales, const int32_t *gu_perm, const void *dn_qweight, const void *dn_qzeros,
+                        const void *dn_scales, const int32_t *down_index, const void *residual, void *y, int M, int K, int F, int E,
+                        int top_k, int group_size, int act_order, void *stream, int bf16)
+{
+    if (act_order != 0 && act_order != 1) return GPTQ_ERR_LAYOUT;
+    if (!x || !ids || !weights || !gu_qweight || !gu_qzeros || !gu_scales || !dn_qweight || !dn_qzeros || !dn_scales || !y)
+        return GPTQ_ERR_NULL;
+    if (act_order && (!gu_perm || !down_index)) return GPTQ_ERR_NULL;
+    if (E < 1 || top_k < 1 || top_k > E || F < 1 || F > (1 << 29)) return GPTQ_ERR_SHAPE;
+    int st = check_shape(M, 2 * F, K, group_size);
+    if (!st) st = check_shape(M, K, F, group_size);
+    if (st) return st;
+    const void *ptrs[] = {x, ids, weights, gu_qweight, gu_qzeros, gu_scales, dn_qweight, dn_qzeros, dn_scales, y, residual,
+                          act_order ? gu_perm : nullptr, act_order ? down_index : nullptr};
+    for (const void *p : ptrs)
+        if (!aligned16(p)) return GPTQ_ERR_ALIGN;
+    if (E > kMoeMaxExperts || top_k > kMoeMaxTopK) return GPTQ_ERR_UNSUPPORTED;
+    int tiled = group_size;
+    st = check_fast_path(K, F, tiled);
+    tiled = group_size;
+    if (!st) st = check_fast_path(2 * F, K, tiled);
+    if (st) return st;
+    int dev, sms;
+    st = current_device_sms(&dev, &sms);
+    if (st) return st;
+    uint8_t *ws;
+    st = registered_workspace(dev, moe_workspace_need(M, K, F, top_k, act_order), &ws);
+    if (st) return st;
+
+    MoeArgs a{};
+    a.gu_w = (const uint8_t *)gu_qweight, a.gu_z = (const uint8_t *)gu_qzeros, a.gu_s = (const uint8_t *)gu_scales;
+    a.dn_w = (const uint8_t *)dn_qweight, a.dn_z = (const uint8_t *)dn_qzeros, a.dn_s = (const uint8_t *)dn_scales;
+    a.gu_w_bytes = gptq_repack_bytes(0, 2 * F, K, tiled, 0);
+    a.gu_z_bytes = gptq_repack_bytes(1, 2 * F, K, tiled, 0);
+    a.gu_s_bytes = gptq_repack_bytes(2, 2 * F, K, tiled, 0);
+    a.dn_w_bytes = gptq_repack_bytes(0, K, F, tiled, 0);
+    a.dn_z_bytes = gptq_repack_bytes(1, K, F, tiled, 0);
+    a.dn_s_bytes = gptq_repack_bytes(2, K, F, tiled, 0);
+    a.down_index = act_order ? down_index : nullptr;
+    a.h = (__half *)ws;
+    a.k = top_k, a.E = E, a.K = K, a.F = F;
+    a.x_by_slot = act_order;
+    for (int m0 = 0; m0 < M; m0 += kMoeMaxRows) {
+        a.M = (M - m0) < kMoeMaxRows ? (M - m0) : kMoeMaxRows;
+        a.x = (const __half *)x + (size_t)m0 * K;
+        a.ids = ids + (size_t)m0 * top_k;
+        a.weights = weights + (size_t)m0 * top_k;
+        a.residual = residual ? (const __half *)residual + (size_t)m0 * K : nullptr;
+        a.y = (__half *)y + (size_t)m0 * K;
+        if (act_order) {
+            __half *sorted = (__half *)(ws + moe_h_bytes((M < kMoeMaxRows ? M : kMoeMaxRows) * top_k, F));
+            st = launch_moe_gather(a.x, a.ids, gu_perm, sorted, a.M * top_k, top_k, E, K, (cudaStream_t)stream);
+            if (st) return st;
+            a.x = sorted;
+        }
+        st = launch_moe(a, tiled, bf16, (cudaStream_t)stream);
+        if (st) return st;
+    }
+    return GPTQ_OK;
+}
+
+static int lora_dispatch(const void *x, const void *qweight, const void *qzeros, const void *scales, const int32_t *g_idx,
+                         const void *lora_a, const void *lora_b, const int32_t *adapter_ids, const float *adapter_scales, void *y, int M,
+                         int N, int K, int group_size, int act_order, int rank, int adapters, void *stream, int bf16)
+{
+    if (act_order < 0 || act_order > GPTQ_ACT_ORDER_PRESORTED) return GPTQ_ERR_LAYOUT;
+    if (!x || !qweight || !qzeros || !scales || !lora_a || !lora_b || !adapter_ids || !y || (act_order == 1 && !g_idx)) return GPTQ_ERR_NULL;
+    int st = check_shape(M, N, K, group_size);
+    if (st) return st;
+    if (rank < 1 || adapters < 1) return GPTQ_ERR_SHAPE;
+    const void *ptrs[] = {x, qweight, qzeros, scales, lora_a, lora_b, adapter_ids, adapter_scales, y, act_order == 1 ? g_idx : nullptr};
+    for (const void *p : ptrs)
+        if (!aligned16(p)) return GPTQ_ERR_ALIGN;
+    int tiled = group_size;
+    st = check_fast_path(N, K, tiled);
+    if (st) return st;
+    if (rank % 8 || rank > kLoraMaxRank) return GPTQ_ERR_UNSUPPORTED;
+    int dev, sms;
+    st = current_device_sms(&dev, &sms);
+    if (st) return st;
+    uint8_t *ws;
+    const LoraScratch lay = lora_scratch(M, N, K, rank, act_order);
+    st = registered_workspace(dev, lay.total, &ws);
+    if (st) return st;
+    cudaStream_t s = (cudaStream_t)stream;
+    LoraArgs a{};
+    a.x = (const __half *)x, a.a = (const __half *)lora_a, a.b = (const __half *)lora_b;
+    a.ids = adapter_ids, a.scales = adapter_scales, a.v = (float *)(ws + lay.v);
+    a.M = M, a.N = N, a.K = K, a.rank = rank, a.adapters = adapters;
+    if (M <= kLoraDirectRows) {
+        const __half *xin = a.x;
+        if (act_order == 1) {
+            st = launch_gather_x(a.x, g_idx, (__half *)ws, M, K, s);
+            if (st) return st;
+            xin = (const __half *)ws;
+        }
+        st = launch_lora_shrink(a, bf16, s);
+        if (st) return st;
+        return launch_lora_gemm(a, xin, qweight, scales, qzeros, (__half *)y, tiled, bf16, s);
+    }
+    __half *delta = (__half *)(ws + lay.delta);
+    st = launch_lora_shrink(a, bf16, s);
+    if (!st) st = launch_lora_delta(a, delta, bf16, s);
+    if (st) return st;
+    return gemm_dispatch(x, qweight, qzeros, scales, g_idx, y, M, N, K, group_size, act_order, 0, nullptr, delta, nullptr, stream, bf16);
+}
+
+extern "C" {
+
+int gptq_moe_mlp(const void *x, const int32_t *expert_ids, const float *expert_weights, const void *gate_up_qweight,
+                 const void *gate_up_qzeros, const void *gate_up_scales, const int32_t *gate_up_perm, const void *down_qweight,
+                 const void *down_qzeros, const void *down_scales, const int32_t *down_index, const void *residual, void *y, int M, int K,
+                 int F, int E, int top_k, int group_size, int act_order, void *stream)
+{
+    return moe_dispatch(x, expert_ids, expert_weights, gate_up_qweight, gate_up_qzeros, gate_up_scales, gate_up_perm, down_qweight,
+                        down_qzeros, down_scales, down_index, residual, y, M, K, F, E, top_k, group_size, act_order, stream, 0);
+}
+
+int gptq_moe_mlp_bf16(const void *x, const int32_t *expert_ids, const float *expert_weights, const void *gate_up_qweight,
+                      const void *gate_up_qzeros, const void *gate_up_scales, const int32_t *gate_up_perm, const void *down_qweight,
+                      const void *down_qzeros, const void *down_scales, const int32_t *down_index, const void *residual, void *y, int M,
+                      int K, int F, int E, int top_k, int group_size, int act_order, void *stream)
+{
+    return moe_dispatch(x, expert_ids, expert_weights, gate_up_qweight, gate_up_qzeros, gate_up_scales, gate_up_perm, down_qweight,
+                        down_qzeros, down_scales, down_index, residual, y, M, K, F, E, top_k, group_size, act_order, stream, 1);
+}
+
+size_t gptq_lora_workspace_bytes(int M, int N, int K, int group_size, int act_order, int rank)
+{
+    if (check_shape(M, N, K, group_size) != GPTQ_OK || check_fast_path(N, K, group_size) != GPTQ_OK) return 0;
+    if (rank < 8 || rank % 8 || rank > kLoraMaxRank) return 0;
+    return lora_scratch(M, N, K, rank, act_order).total;
+}
+
+int gptq_gemm_lora(const void *x, const void *qweight, const void *qzeros, const void *scales, const int32_t *g_idx, const void *lora_a,
+                   const void *lora_b, const int32_t *adapter_ids, const float *adapter_scales, void *y, int M, int N, int K,
+                   int group_size, int act_order, int rank, int adapters, void *stream)
+{
+    return lora_dispatch(x, qweight, qzeros, scales, g_idx, lora_a, lora_b, adapter_ids, adapter_scales, y, M, N, K, group_size,
+                         act_order, rank, adapters, stream, 0);
+}
+
+int gptq_gemm_lora_bf16(const void *x, const void *qweight, const void *qzeros, const void *scales, const int32_t *g_idx,
+                        const void *lora_a, const void *lora_b, const int32_t *adapter_ids, const float *adapter_scales, void *y, int M,
+                        int N, int K, int group_size, int act_order, int rank, int adapters, void *stream)
+{
+    return lora_dispatch(x, qweight, qzeros, scales, g_idx, lora_a, lora_b, adapter_ids, adapter_scales, y, M, N, K, group_size,
+                         act_order, rank, adapters, stream, 1);
 }
 
 }  // extern "C"

@@ -362,6 +362,13 @@ __device__ __forceinline__ float2 pair_to_float2(uint32_t v)
     if constexpr (BF) return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
     else return __half22float2(*reinterpret_cast<const __half2 *>(&v));
 }
+// one element stored as 16 bits of the matmul's format -> float
+template <bool BF>
+__device__ __forceinline__ float out16_to_float(__half v)
+{
+    if constexpr (BF) return __uint_as_float((uint32_t)__half_as_ushort(v) << 16);
+    else return __half2float(v);
+}
 // one float -> the 16 bits of the matmul's output format, round to nearest even
 template <bool BF>
 __device__ __forceinline__ unsigned short float_to_out16(float v)

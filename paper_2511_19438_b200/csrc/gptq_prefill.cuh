@@ -467,12 +467,12 @@ prefill_kernel(const PrefillArgs a, const __grid_constant__ CUtensorMap w_map, c
                             v[2] += __uint_as_float(u.z);
                             v[3] += __uint_as_float(u.w);
                         }
-                        const float bias = a.bias ? __half2float(a.bias[col]) : 0.f;
+                        const float bias = a.bias ? out16_to_float<BF>(a.bias[col]) : 0.f;
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             if (m + e >= rows) break;
                             float f = v[e] + bias;
-                            if (a.residual) f += __half2float(a.residual[at + (size_t)e * a.N]);
+                            if (a.residual) f += out16_to_float<BF>(a.residual[at + (size_t)e * a.N]);
                             store_out16<BF>(a.y + at + (size_t)e * a.N, f);
                         }
                     }
@@ -532,8 +532,7 @@ prefill_kernel(const PrefillArgs a, const __grid_constant__ CUtensorMap w_map, c
                         }
                         auto add4 = [&](const __half *from) {
                             const uint2 b = *reinterpret_cast<const uint2 *>(from);
-                            const float2 b0 = __half22float2(*reinterpret_cast<const __half2 *>(&b.x));
-                            const float2 b1 = __half22float2(*reinterpret_cast<const __half2 *>(&b.y));
+                            const float2 b0 = pair_to_float2<BF>(b.x), b1 = pair_to_float2<BF>(b.y);
                             v.x += b0.x, v.y += b0.y, v.z += b1.x, v.w += b1.y;
                         };
                         if (a.bias) add4(a.bias + col);
@@ -576,7 +575,7 @@ prefill_kernel(const PrefillArgs a, const __grid_constant__ CUtensorMap w_map, c
             float bv[4] = {};                        // columns lane / 4 + 8 j of the warp's 32
             if (has_bias) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) bv[j] = __half2float(a.bias[(size_t)p * kPanel + 32 * q + 8 * j + (lane >> 2)]);
+                for (int j = 0; j < 4; ++j) bv[j] = out16_to_float<BF>(a.bias[(size_t)p * kPanel + 32 * q + 8 * j + (lane >> 2)]);
             }
             decode_wait(bar_dfull + 8 * d, ph, flag);        // (unambiguous for the dequant warps too: kPrefillMinItems)
             __syncwarp();
@@ -634,7 +633,7 @@ prefill_kernel(const PrefillArgs a, const __grid_constant__ CUtensorMap w_map, c
                             ldmatrix_x4_trans(frag + 512 * i, rr);
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
-                                const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&rr[j]));
+                                const float2 f = pair_to_float2<BF>(rr[j]);
                                 v[j].x += f.x, v[j].y += f.y;
                             }
                             __syncwarp();

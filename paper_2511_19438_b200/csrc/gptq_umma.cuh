@@ -559,12 +559,12 @@ umma_kernel(const UmmaArgs a, const __grid_constant__ CUtensorMap w_map, const _
                         // bias[column] + residual[token][column] join the fp32 sum before the one rounding; the 32 lanes
                         // of a warp read 32 neighbouring columns of one token row per load
                         const size_t ncol = (size_t)p * kPanel + n;
-                        const float bv = a.bias ? __half2float(a.bias[ncol]) : 0.f;
+                        const float bv = a.bias ? out16_to_float<BF>(a.bias[ncol]) : 0.f;
 #pragma unroll
                         for (int i = 0; i < 32; ++i) {
                             const int m = m0 + c0 + i;
                             float v = __uint_as_float(r[i]) + bv;
-                            if (a.residual && m < a.M) v += __half2float(a.residual[(size_t)m * a.N + ncol]);
+                            if (a.residual && m < a.M) v += out16_to_float<BF>(a.residual[(size_t)m * a.N + ncol]);
                             r[i] = __float_as_uint(v);
                         }
                     }
@@ -719,14 +719,12 @@ umma_kernel(const UmmaArgs a, const __grid_constant__ CUtensorMap w_map, const _
                     float4 v = sum4(m, cc);
                     if (a.bias) {
                         const uint2 b = *reinterpret_cast<const uint2 *>(a.bias + (size_t)p * kPanel + cc);
-                        const float2 b0 = __half22float2(*reinterpret_cast<const __half2 *>(&b.x));
-                        const float2 b1 = __half22float2(*reinterpret_cast<const __half2 *>(&b.y));
+                        const float2 b0 = pair_to_float2<BF>(b.x), b1 = pair_to_float2<BF>(b.y);
                         v.x += b0.x, v.y += b0.y, v.z += b1.x, v.w += b1.y;
                     }
                     if (a.residual) {
                         const uint2 q = *reinterpret_cast<const uint2 *>(a.residual + at);
-                        const float2 q0 = __half22float2(*reinterpret_cast<const __half2 *>(&q.x));
-                        const float2 q1 = __half22float2(*reinterpret_cast<const __half2 *>(&q.y));
+                        const float2 q0 = pair_to_float2<BF>(q.x), q1 = pair_to_float2<BF>(q.y);
                         v.x += q0.x, v.y += q0.y, v.z += q1.x, v.w += q1.y;
                     }
                     store4(a.y + at, v);
@@ -801,14 +799,12 @@ umma_kernel(const UmmaArgs a, const __grid_constant__ CUtensorMap w_map, const _
                     float4 v = sum4(m, cc);
                     if (a.bias) {
                         const uint2 b = *reinterpret_cast<const uint2 *>(a.bias + (size_t)p * kPanel + cc);
-                        const float2 b0 = __half22float2(*reinterpret_cast<const __half2 *>(&b.x));
-                        const float2 b1 = __half22float2(*reinterpret_cast<const __half2 *>(&b.y));
+                        const float2 b0 = pair_to_float2<BF>(b.x), b1 = pair_to_float2<BF>(b.y);
                         v.x += b0.x, v.y += b0.y, v.z += b1.x, v.w += b1.y;
                     }
                     if (a.residual) {
                         const uint2 q = *reinterpret_cast<const uint2 *>(a.residual + at);
-                        const float2 q0 = __half22float2(*reinterpret_cast<const __half2 *>(&q.x));
-                        const float2 q1 = __half22float2(*reinterpret_cast<const __half2 *>(&q.y));
+                        const float2 q0 = pair_to_float2<BF>(q.x), q1 = pair_to_float2<BF>(q.y);
                         v.x += q0.x, v.y += q0.y, v.z += q1.x, v.w += q1.y;
                     }
                     store4(a.y + at, v);

@@ -208,3 +208,78 @@ def upload_and_repack_bits(L: QuantLinear, bits: int, keep_canonical: bool = Fal
     torch.cuda.current_stream().synchronize()
     canonical = (qw, qz, sc, gi) if keep_canonical else None
     return DeviceLinear(L.K, L.N, L.group_size, L.act_order, outs[0], outs[1], outs[2], perm, canonical)
+
+
+# ---- rows that choose their weights: routed experts, low-rank adapters -------------------------------------------------
+
+@dataclass
+class DeviceExperts:
+    """The experts' layers of one kind (all gate_up or all down) behind one another, tiled."""
+    K: int
+    N: int
+    group_size: int
+    act_order: bool
+    count: int
+    qweight_t: torch.Tensor      # uint8 [count, bytes]
+    qzeros_t: torch.Tensor
+    scales_t: torch.Tensor
+    perm: torch.Tensor | None    # int32 [count, K]
+    index: torch.Tensor | None   # its inverse: where row k of the checkpoint sits
+
+
+def upload_experts(layers: list[QuantLinear], gate_up: bool = False, scales_bf16_bits: list[np.ndarray] | None = None,
+                   device="cuda") -> DeviceExperts:
+    """Repacks every layer and puts the tiled buffers behind one another, as gptq_moe_mlp takes them."""
+    D = [upload_and_repack(L, device=device, gate_up=gate_up, scales_bf16_bits=None if scales_bf16_bits is None else scales_bf16_bits[e])
+         for e, L in enumerate(layers)]
+    act = D[0].act_order
+    return DeviceExperts(D[0].K, D[0].N, D[0].group_size, act, len(D), torch.stack([d.qweight_t for d in D]),
+                         torch.stack([d.qzeros_t for d in D]), torch.stack([d.scales_t for d in D]),
+                         torch.stack([d.perm for d in D]) if act else None,
+                         torch.stack([invert_perm(d.perm) for d in D]) if act else None)
+
+
+_LOGITS_TYPE = {torch.float32: B.GPTQ_LOGITS_F32, torch.float16: B.GPTQ_LOGITS_F16, torch.bfloat16: B.GPTQ_LOGITS_BF16}
+
+
+def moe_route(logits: torch.Tensor, top_k: int, renormalize: bool = True, stream=None) -> tuple[torch.Tensor, torch.Tensor]:
+    """(expert ids int32 [M, top_k], weights fp32 [M, top_k]) of router logits [M, E] through gptq_moe_route."""
+    M, E = logits.shape
+    ids = torch.empty((M, top_k), dtype=torch.int32, device=logits.device)
+    weights = torch.empty((M, top_k), dtype=torch.float32, device=logits.device)
+    B.check(B.gptq_moe_route(logits, ids, weights, M, E, top_k, _LOGITS_TYPE[logits.dtype], renormalize, stream), "gptq_moe_route")
+    return ids, weights
+
+
+def moe_mlp(x: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor, gate_up: DeviceExperts, down: DeviceExperts,
+            residual: torch.Tensor | None = None, y: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """A mixture-of-experts MLP through gptq_moe_mlp or, for bfloat16 x, gptq_moe_mlp_bf16 (workspace: ensure_for_moe)."""
+    M, K = x.shape
+    if y is None:
+        y = torch.empty_like(x)
+    fn = B.gptq_moe_mlp_bf16 if x.dtype == torch.bfloat16 else B.gptq_moe_mlp
+    B.check(fn(x, ids, weights, gate_up.qweight_t, gate_up.qzeros_t, gate_up.scales_t, gate_up.perm, down.qweight_t, down.qzeros_t,
+               down.scales_t, down.index, residual, y, M, K, down.K, gate_up.count, ids.shape[1], min(gate_up.group_size, 128),
+               gate_up.act_order, stream), fn.__name__)
+    return y
+
+
+def ensure_for_moe(ws: "WorkspaceHolder", M: int, gate_up: DeviceExperts, top_k: int) -> None:
+    ws.ensure(B.gptq_moe_workspace_bytes(M, gate_up.K, gate_up.N // 2, top_k, gate_up.act_order))
+
+
+def gemm_lora(x: torch.Tensor, D: DeviceLinear, lora_a: torch.Tensor, lora_b: torch.Tensor, adapter_ids: torch.Tensor,
+              adapter_scales: torch.Tensor | None = None, y: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """y = x . dequant(W) + scale (x A^T) B^T with each row's adapter, through gptq_gemm_lora or, for bfloat16 x,
+    gptq_gemm_lora_bf16 (workspace: ensure_for_lora)."""
+    M = x.shape[0]
+    if y is None:
+        y = torch.empty((M, D.N), dtype=x.dtype, device=x.device)
+    fn = B.gptq_gemm_lora_bf16 if x.dtype == torch.bfloat16 else B.gptq_gemm_lora
+    B.check(fn(x, D.qweight_t, D.qzeros_t, D.scales_t, D.perm, lora_a, lora_b, adapter_ids, adapter_scales, y, M, D.N, D.K,
+               D.group_size, D.act_order, lora_a.shape[1], lora_a.shape[0], stream), fn.__name__)
+    return y
+
+
+def ensure_for_lora(ws: "WorkspaceHolder", M: int, D: DeviceLinear, rank: int) -> None:
+    ws.ensure(B.gptq_lora_workspace_bytes(M, D.N, D.K, D.group_size, D.act_order, rank))

@@ -1,0 +1,472 @@
+"""GPU tests of the operators whose rows choose their weights: routing, routed experts, low-rank adapters.
+
+Plain implementations in 64 bits on the oracle's dequantised weights.  Tolerances, with u = half a step of the 16-bit type
+(2^-11 fp16, 2^-8 bfloat16):
+
+* a sum of n products in fp32, in any order and with truncation, is off by at most n 2^-23 of the sum of their absolute values;
+* experts: each activation h is rounded once, which moves y by at most u sum |w h d|, and y is rounded once, u |y|; the fp32
+  errors of gate and up reach h through silu (slope below 1.1) and the product, 2^-18 covers the fast exponential and division.
+  All roundings are independent, so the rms error stays below u sqrt(y^2 + sum (w h d)^2) (three times its variance);
+* adapters: one rounding of y up to 16 rows; above, every scaled weight is rounded, u sum |x w|, rms u sqrt(sum (x w)^2), and so is
+  the adapters' part.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from paper_2511_19438_b200 import workloads as wl
+
+pytestmark = pytest.mark.gpu
+
+if torch.cuda.is_available():
+    from paper_2511_19438_b200 import build as libbuild
+    libbuild.build()
+    from paper_2511_19438_b200 import binding as B
+    from paper_2511_19438_b200 import harness as H
+
+U = {torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+F32 = 2.0 ** -23
+
+
+@pytest.fixture(scope="module")
+def ws():
+    return H.WorkspaceHolder()
+
+
+def gen(*parts):
+    return torch.Generator(device="cuda").manual_seed(wl.seed_for(*parts))
+
+
+def layer(K, N, seed, group=128, act=False, minus_one=False, bf16=False):
+    """(QuantLinear, bf16 scale bits or None, float64 [K, N] on the GPU)"""
+    L = wl.make_linear(K, N, seed=seed, group_size=group, act_order=act)
+    L.zeros_minus_one = minus_one
+    if bf16:
+        bits = wl.make_scales_bf16(K // group, N, seed + 1)
+        w = oracle.dequant_f32_bf16(L.qweight, L.qzeros, bits, L.g_idx, group, minus_one)
+    else:
+        bits, w = None, oracle.dequant_f32(L.qweight, L.qzeros, L.scales, L.g_idx, group, minus_one)
+    return L, bits, H.to_device(w).double()
+
+
+# ---------------------------------------------------------------------------------------------------------------- routing
+
+def plain_route(logits, k, renormalize):
+    ids, weights = [], []
+    for row in logits.double().cpu().tolist():
+        big = float(np.finfo(np.float32).max)
+        open_ = sorted((-min(v, big), e) for e, v in enumerate(row) if v == v and v != -math.inf)
+        top = -open_[0][0] if open_ else 0.0
+        p = [math.exp(-v - top) for v, _ in open_]
+        total = math.fsum(p[:k]) if renormalize else math.fsum(p)
+        ids.append([e for _, e in open_[:k]] + [-1] * (k - len(open_[:k])))
+        weights.append([q / total for q in p[:k]] + [0.0] * (k - len(open_[:k])))
+    return np.array(ids), np.array(weights)
+
+
+def check_route(logits, k, renormalize):
+    ids, w = H.moe_route(logits, k, renormalize)
+    want_ids, want_w = plain_route(logits, k, renormalize)
+    assert np.array_equal(ids.cpu().numpy(), want_ids)
+    # exp and the division are good to a few steps of 2^-24 times the exponent; a sum of E terms
+    err = np.abs(w.cpu().double().numpy() - want_w)
+    assert np.all(err <= 2.0 ** -18 * want_w + 1e-37), err.max()
+
+
+@pytest.mark.parametrize("M,E,k", [(1, 1, 1), (1, 64, 8), (3, 7, 7), (5, 32, 4), (130, 33, 2), (2, 100, 32), (9, 128, 6), (4, 256, 8),
+                                   (3, 500, 10), (2, 1024, 32), (1025, 60, 4)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+def test_route(M, E, k, dtype):
+    logits = (3 * torch.randn((M, E), generator=gen("route", M, E), device="cuda")).to(dtype)
+    check_route(logits, k, True)
+    check_route(logits, k, False)
+
+
+def test_route_ties_and_closed_experts():
+    g = gen("route-ties")
+    logits = torch.randint(-2, 3, (40, 50), generator=g, device="cuda").float()        # many ties, -0 among them
+    logits[::2] *= -1.0
+    check_route(logits, 8, True)
+    check_route(logits.half(), 8, False)
+    logits[:, 10:] = -math.inf
+    logits[3] = -math.inf                                                              # nothing to choose
+    logits[4] = math.nan
+    logits[5, :7] = math.nan
+    logits[6, 4] = math.inf
+    logits[7, 4:6] = math.inf
+    for k in (1, 8, 12, 32):
+        check_route(logits, k, True)
+        check_route(logits, k, False)
+    tiny = torch.tensor([[1e-42, 2e-42, 0.0, -0.0, -1e-42, 1e-45]], device="cuda").repeat(2, 1)
+    check_route(tiny, 6, True)
+
+
+# ---------------------------------------------------------------------------------------------------------------- experts
+
+class Moe:
+    def __init__(self, K, F, E, group=128, act=False, minus_one=False, dtype=torch.float16):
+        bf16 = dtype == torch.bfloat16
+        up = [layer(K, 2 * F, wl.seed_for("moe-up", K, F, e, group), group, act, minus_one, bf16) for e in range(E)]
+        down = [layer(F, K, wl.seed_for("moe-down", K, F, e, group), group, act, minus_one, bf16) for e in range(E)]
+        self.K, self.F, self.E, self.dtype = K, F, E, dtype
+        self.up64, self.down64 = [l[2] for l in up], [l[2] for l in down]
+        self.up = H.upload_experts([l[0] for l in up], gate_up=True, scales_bf16_bits=[l[1] for l in up] if bf16 else None)
+        self.down = H.upload_experts([l[0] for l in down], scales_bf16_bits=[l[1] for l in down] if bf16 else None)
+
+    def plain(self, x, ids, weights, residual):
+        """(y, bound of the largest errors, bound of the mean square error), float64"""
+        u, x = U[self.dtype], x.double()
+        M = x.shape[0]
+        y = torch.zeros((M, self.K), dtype=torch.float64, device="cuda")
+        if residual is not None:
+            y += residual.double()
+        most, square = y.abs() * 4 * F32, torch.zeros_like(y)
+        for m in range(M):
+            named = {}
+            for e, w in zip(ids[m].tolist(), weights[m].tolist()):
+                if 0 <= e < self.E:
+                    named[e] = named.get(e, 0.0) + w
+            for e, w in named.items():
+                gu, size = x[m] @ self.up64[e], x[m].abs() @ self.up64[e].abs()
+                gate, up, dg, du = gu[:self.F], gu[self.F:], self.K * F32 * size[:self.F], self.K * F32 * size[self.F:]
+                silu = gate * torch.sigmoid(gate)
+                h = silu * up
+                dh = 1.1 * dg * (up.abs() + du) + silu.abs() * du + 2.0 ** -18 * h.abs()
+                d = self.down64[e].abs()
+                y[m] += w * (h @ self.down64[e])
+                most[m] += abs(w) * (((u + self.F * F32) * h.abs() + 1.01 * dh + 2.0 ** -24) @ d)
+                square[m] += (w * u) ** 2 * ((h * h) @ (d * d))
+        return y, most + u * y.abs(), square + (u * y) ** 2
+
+    def inputs(self, M, k, *seed):
+        g = gen("moe-in", M, k, *seed)
+        x = torch.randn((M, self.K), generator=g, device="cuda").to(self.dtype)
+        p, ids = torch.randn((M, self.E), generator=g, device="cuda").softmax(-1).topk(k)
+        residual = (4 * torch.randn((M, self.K), generator=g, device="cuda")).to(self.dtype)
+        return x, ids.to(torch.int32), p.contiguous(), residual
+
+    def check(self, ws, x, ids, weights, residual, y=None):
+        want, most, square = self.plain(x, ids, weights, residual)
+        H.ensure_for_moe(ws, x.shape[0], self.up, ids.shape[1])
+        ws.buf.fill_(0xff)                             # NaNs: nothing of an earlier call may be read
+        y = H.moe_mlp(x, ids, weights, self.up, self.down, residual, y)
+        assert B.gptq_check_status() == B.GPTQ_OK
+        err = (y.double() - want).abs()
+        assert torch.isfinite(y).all()
+        assert (err <= most).all(), f"{int((err > most).sum())} of {err.numel()} beyond the bound, worst {float((err / most).max()):.2f} of it"
+        assert float((err * err).mean()) <= float(square.mean()), (float((err * err).mean()), float(square.mean()))
+        return y
+
+
+@pytest.mark.parametrize("M,K,F,E,k", [(1, 128, 128, 2, 1), (1, 512, 256, 8, 2), (2, 256, 384, 4, 4), (5, 384, 128, 16, 3),
+                                       (8, 1152, 256, 3, 2), (9, 256, 128, 5, 2), (16, 128, 640, 4, 1), (17, 256, 256, 3, 2),
+                                       (33, 128, 256, 2, 1), (64, 256, 128, 4, 3), (65, 128, 128, 3, 2), (130, 256, 128, 6, 2)])
+def test_moe(ws, M, K, F, E, k):
+    moe = Moe(K, F, E)
+    x, ids, w, r = moe.inputs(M, k)
+    moe.check(ws, x, ids, w, r)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("group,act,minus_one", [(128, True, False), (64, False, True), (64, True, False), (32, False, False),
+                                                 (32, True, True), (256, False, False)])
+@pytest.mark.parametrize("M", [1, 11, 40])
+def test_moe_formats(ws, M, group, act, minus_one, dtype):
+    moe = Moe(256, 512, 4, group, act, minus_one, dtype)
+    x, ids, w, r = moe.inputs(M, 2, group, act)
+    moe.check(ws, x, ids, w, r)
+
+
+def test_moe_larger_shapes(ws):
+    moe = Moe(2048, 1408, 4)
+    for M, k in ((1, 2), (3, 4), (12, 2)):
+        x, ids, w, r = moe.inputs(M, k, "large")
+        moe.check(ws, x, ids, w, r)
+
+
+def test_moe_every_token_to_one_expert(ws):
+    moe = Moe(256, 256, 5)
+    for M in (8, 16, 31, 64):
+        x, ids, w, r = moe.inputs(M, 1, "one")
+        ids.fill_(3)
+        moe.check(ws, x, ids, w, r)
+
+
+def test_moe_unused_slots_and_padding(ws):
+    moe = Moe(256, 256, 6)
+    for M in (4, 20):
+        x, ids, w, r = moe.inputs(M, 3, "pad")
+        ids[0, 1] = -1
+        ids[1] = -1
+        ids[2, 0] = moe.E
+        ids[2, 2] = -2147483648
+        ids[M - 1] = 2147483647
+        x[1] = math.nan                    # padding rows hold anything
+        x[M - 1] = math.inf
+        w[1] = math.nan
+        w[0, 1] = math.inf
+        clean_x, clean_w = x.clone(), w.clone()
+        clean_x[1], clean_x[M - 1], clean_w[1], clean_w[0, 1] = 0, 0, 0, 0
+        want, most, _ = moe.plain(clean_x, ids, clean_w, r)
+        H.ensure_for_moe(ws, M, moe.up, 3)
+        y = H.moe_mlp(x, ids, w, moe.up, moe.down, r)
+        assert ((y.double() - want).abs() <= most).all()
+        assert torch.equal(y[1], r[1]) and torch.equal(y[M - 1], r[M - 1])
+        y = H.moe_mlp(x, ids, w, moe.up, moe.down)
+        assert torch.equal(y[1], torch.zeros_like(y[1]))
+    x, ids, w, r = moe.inputs(7, 2, "none")
+    ids.fill_(-1)
+    assert torch.equal(H.moe_mlp(x, ids, w, moe.up, moe.down, r), r)
+    assert not H.moe_mlp(x, ids, w, moe.up, moe.down).any()
+
+
+def test_moe_expert_named_twice(ws):
+    moe = Moe(256, 128, 4)
+    for M in (1, 6, 30):
+        x, ids, w, r = moe.inputs(M, 3, "twice")
+        ids[:, 2] = ids[:, 0]
+        ids[0] = 2
+        moe.check(ws, x, ids, w, r)
+
+
+def test_moe_top_32_of_many_experts(ws):
+    moe = Moe(128, 128, 40)
+    for M in (1, 64):
+        x, ids, w, r = moe.inputs(M, 32, "many")
+        moe.check(ws, x, ids, w, r)
+
+
+def test_moe_buffers_may_be_shared(ws):
+    moe = Moe(256, 256, 4)
+    for M in (3, 70):
+        x, ids, w, r = moe.inputs(M, 2, "alias")
+        y = moe.check(ws, x, ids, w, r)
+        shared = r.clone()
+        assert torch.equal(H.moe_mlp(x, ids, w, moe.up, moe.down, shared, shared), y)
+        shared = x.clone()
+        assert torch.equal(H.moe_mlp(shared, ids, w, moe.up, moe.down, r, shared), y)
+
+
+def test_moe_infinite_activations(ws):
+    """An infinity in x reaches its own row only, and there as the formula has it."""
+    moe = Moe(256, 128, 4)
+    x, ids, w, r = moe.inputs(6, 2, "inf")
+    want = moe.check(ws, x, ids, w, r)
+    x[2, 17] = math.inf
+    y = H.moe_mlp(x, ids, w, moe.up, moe.down, r)
+    keep = torch.tensor([0, 1, 3, 4, 5], device="cuda")
+    assert torch.equal(y[keep], want[keep])
+    assert not torch.isfinite(y[2]).any()
+
+
+def test_moe_refuses_other_layouts(ws):
+    moe = Moe(256, 128, 4)
+    bf = Moe(256, 128, 4, dtype=torch.bfloat16)
+    plain_up = H.upload_experts([wl.make_linear(256, 256, seed=e) for e in range(4)])
+    flagged_down = H.upload_experts([wl.make_linear(128, 256, seed=e) for e in range(4)], gate_up=True)
+    x, ids, w, r = moe.inputs(5, 2, "layout")
+    H.ensure_for_moe(ws, 5, moe.up, 2)
+    for up, down in ((plain_up, moe.down), (moe.up, flagged_down), (bf.up, bf.down), (moe.up, bf.down)):
+        y = torch.full_like(x, 7.0)
+        H.moe_mlp(x, ids, w, up, down, r, y)
+        assert B.gptq_check_status() == B.GPTQ_ERR_LAYOUT
+        assert torch.equal(y, torch.full_like(x, 7.0))
+    assert B.gptq_check_status() == B.GPTQ_OK
+
+
+def test_moe_needs_its_workspace(ws):
+    moe = Moe(128, 128, 2)
+    x, ids, w, r = moe.inputs(2, 1, "ws")
+    H.ensure_for_moe(ws, 2, moe.up, 1)
+    B.check(B.gptq_set_workspace(None, 0), "unregister")
+    with pytest.raises(B.GptqError) as e:
+        H.moe_mlp(x, ids, w, moe.up, moe.down, r)
+    assert e.value.status == B.GPTQ_ERR_WORKSPACE
+    B.check(B.gptq_set_workspace(ws.buf, 255), "small")
+    with pytest.raises(B.GptqError):
+        H.moe_mlp(x, ids, w, moe.up, moe.down, r)
+    ws.ensure(1)
+
+
+# --------------------------------------------------------------------------------------------------------------- adapters
+
+class Lora:
+    def __init__(self, K, N, rank, n, group=128, act=False, minus_one=False, dtype=torch.float16):
+        self.L, bits, self.w64 = layer(K, N, wl.seed_for("lora", K, N, group, act), group, act, minus_one, dtype == torch.bfloat16)
+        self.D = H.upload_and_repack(self.L, scales_bf16_bits=bits)
+        self.K, self.N, self.rank, self.n, self.dtype = K, N, rank, n, dtype
+        g = gen("lora", K, N, rank, n)
+        self.a = (torch.randn((n, rank, K), generator=g, device="cuda") / K ** 0.5).to(dtype)
+        self.b = (0.5 * torch.randn((n, N, rank), generator=g, device="cuda")).to(dtype)
+        self.scales = 0.25 + torch.rand(n, generator=g, device="cuda")
+
+    def inputs(self, M, *seed):
+        g = gen("lora-in", M, *seed)
+        x = torch.randn((M, self.K), generator=g, device="cuda").to(self.dtype)
+        ids = torch.randint(-1, self.n, (M,), generator=g, device="cuda").to(torch.int32)
+        return x, ids
+
+    def plain(self, x, ids, scales):
+        u, x = U[self.dtype], x.double()
+        y, size, square = x @ self.w64, x.abs() @ self.w64.abs(), (x * x) @ (self.w64 * self.w64)
+        part, part_size = torch.zeros_like(y), torch.zeros_like(y)
+        for a in range(self.n):
+            m = (ids == a).nonzero().squeeze(1)
+            A, Bm = self.a[a].double(), self.b[a].double()
+            s = 1.0 if scales is None else float(scales[a])
+            part[m] = s * ((x[m] @ A.t()) @ Bm.t())
+            part_size[m] = abs(s) * ((x[m].abs() @ A.abs().t()) @ Bm.abs().t())
+        y = y + part
+        few = x.shape[0] <= 16
+        most = u * y.abs() + self.K * F32 * size + (self.K + self.rank) * F32 * part_size
+        mean_square = (u * y) ** 2
+        if not few:
+            most += u * size + u * part.abs()
+            mean_square += u * u * (square + part * part)
+        return y, 1.01 * most + 2.0 ** -24, mean_square
+
+    def check(self, ws, x, ids, scales, D=None, y=None, stream=None):
+        want, most, square = self.plain(x, ids, scales)
+        D = D or self.D
+        H.ensure_for_lora(ws, x.shape[0], D, self.rank)
+        ws.buf.fill_(0xff)
+        y = H.gemm_lora(x, D, self.a, self.b, ids, scales, y)
+        assert B.gptq_check_status() == B.GPTQ_OK
+        assert torch.isfinite(y).all()
+        err = (y.double() - want).abs()
+        assert (err <= most).all(), f"{int((err > most).sum())} of {err.numel()} beyond the bound, worst {float((err / most).max()):.2f} of it"
+        assert float((err * err).mean()) <= float(square.mean()), (float((err * err).mean()), float(square.mean()))
+        return y
+
+
+@pytest.mark.parametrize("M,K,N,rank,n", [(1, 128, 128, 8, 1), (1, 1024, 384, 16, 4), (2, 2048, 256, 64, 3), (7, 512, 640, 24, 7),
+                                          (8, 4096, 256, 16, 2), (9, 640, 128, 128, 5), (16, 1152, 384, 40, 16), (17, 512, 256, 16, 3),
+                                          (40, 384, 512, 256, 6), (65, 1024, 256, 8, 64), (130, 640, 384, 64, 2), (513, 512, 384, 16, 9)])
+def test_lora(ws, M, K, N, rank, n):
+    lora = Lora(K, N, rank, n)
+    x, ids = lora.inputs(M)
+    lora.check(ws, x, ids, lora.scales)
+    lora.check(ws, x, ids, None)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("group,act,minus_one", [(128, True, False), (64, False, True), (32, True, False), (256, False, False)])
+@pytest.mark.parametrize("M", [1, 5, 13, 30, 200])
+def test_lora_formats(ws, M, group, act, minus_one, dtype):
+    lora = Lora(512, 384, 16, 4, group, act, minus_one, dtype)
+    x, ids = lora.inputs(M, group)
+    lora.check(ws, x, ids, lora.scales)
+
+
+def test_lora_presorted(ws):
+    lora = Lora(512, 256, 16, 3, act=True)
+    for M in (4, 33):
+        x, ids = lora.inputs(M, "sorted")
+        want = lora.check(ws, x, ids, lora.scales)
+        order = lora.D.perm.long()
+        D = H.DeviceLinear(**{**lora.D.__dict__, "act_order": B.GPTQ_ACT_ORDER_PRESORTED, "perm": None})
+        a = lora.a
+        lora.a = a[:, :, order].contiguous()
+        y = H.gemm_lora(x[:, order].contiguous(), D, lora.a, lora.b, ids, lora.scales)
+        lora.a = a
+        _, most, _ = lora.plain(x, ids, lora.scales)
+        assert ((y.double() - want.double()).abs() <= 2 * most).all()
+
+
+def test_lora_rows_without_adapter(ws):
+    """Rows without an adapter are rows of the plain product; adapters nobody uses are not read."""
+    lora = Lora(512, 256, 16, 4)
+    lora.a[2] = math.nan
+    lora.b[2] = math.inf
+    for M in (1, 6, 16, 50):
+        x, ids = lora.inputs(M, "none")
+        ids[ids == 2] = 1
+        ids[0] = 4
+        ids[M // 2] = -2147483648
+        lora.a[2], lora.b[2] = 0, 0
+        lora.check(ws, x, ids, lora.scales)
+        lora.a[2], lora.b[2] = math.nan, math.inf
+        y = H.gemm_lora(x, lora.D, lora.a, lora.b, ids, lora.scales)
+        assert torch.isfinite(y).all()
+        ids.fill_(-1)
+        lora.a[2], lora.b[2] = 0, 0
+        lora.check(ws, x, ids, None)
+
+
+def test_lora_runs_of_rows(ws):
+    """Packed prompts: runs of rows of odd lengths, a run of one row, rows of one adapter in two places."""
+    lora = Lora(512, 384, 16, 5)
+    ids = torch.cat([torch.full((c,), a, dtype=torch.int32) for a, c in ((2, 37), (0, 1), (-1, 5), (4, 64), (2, 70), (1, 23))]).cuda()
+    x, _ = lora.inputs(ids.numel(), "runs")
+    lora.check(ws, x, ids, lora.scales)
+
+
+def test_lora_refuses_other_layouts(ws):
+    lora, bf = Lora(256, 256, 8, 2), Lora(256, 256, 8, 2, dtype=torch.bfloat16)
+    flagged = H.upload_and_repack(lora.L, gate_up=True)
+    for M in (3, 40):
+        x, ids = lora.inputs(M, "layout")
+        H.ensure_for_lora(ws, M, lora.D, 8)
+        for D in (flagged, bf.D):
+            y = torch.full((M, 256), 7.0, dtype=torch.float16, device="cuda")
+            H.gemm_lora(x, D, lora.a, lora.b, ids, None, y)
+            assert B.gptq_check_status() == B.GPTQ_ERR_LAYOUT
+            assert (y == 7).all()
+
+
+# -------------------------------------------------------------------------------------------------------------- together
+
+def block(x, lora, router, moe, k):
+    """A projection under adapters, its residual by hand, then the routed MLP with its residual."""
+    ids = block.adapter_ids[:x.shape[0]]
+    h = (H.gemm_lora(x, lora.D, lora.a, lora.b, ids, lora.scales).float() + x.float()).to(x.dtype)
+    experts, weights = H.moe_route(h @ router, k)
+    return h, experts, weights, H.moe_mlp(h, experts, weights, moe.up, moe.down, h)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("M", [1, 12, 40])
+def test_together_eager_stream_and_graph(ws, M, dtype):
+    lora, moe, k = Lora(256, 256, 16, 3, dtype=dtype), Moe(256, 384, 8, dtype=dtype), 2
+    H.ensure_for_lora(ws, 64, lora.D, 16)
+    H.ensure_for_moe(ws, 64, moe.up, k)
+    router = (torch.randn((256, 8), generator=gen("router"), device="cuda") / 16).to(dtype)
+    x, block.adapter_ids = lora.inputs(M, "block")
+    h, experts, weights, y = block(x, lora, router, moe, k)
+    want, most, _ = moe.plain(h, experts, weights, h)
+    assert ((y.double() - want).abs() <= most).all()
+    assert torch.equal(block(x, lora, router, moe, k)[3], y)          # the same bits again
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        again = block(x, lora, router, moe, k)[3]
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(again, y)
+    graph = torch.cuda.CUDAGraph()
+    static = x.clone()
+    with torch.cuda.graph(graph):
+        out = block(static, lora, router, moe, k)[3]
+    for seed in ("first", "second"):
+        x2, _ = lora.inputs(M, seed)
+        want2 = block(x2, lora, router, moe, k)[3]
+        static.copy_(x2)
+        for _ in range(3):
+            graph.replay()
+        assert torch.equal(out, want2)
+    assert B.gptq_check_status() == B.GPTQ_OK
+
+
+def test_repeats_bit_for_bit(ws):
+    moe, lora = Moe(1024, 512, 8), Lora(1024, 512, 16, 4)
+    x, ids, w, r = moe.inputs(7, 3, "repeat")
+    xl, il = lora.inputs(9, "repeat")
+    H.ensure_for_moe(ws, 7, moe.up, 3)
+    H.ensure_for_lora(ws, 9, lora.D, 16)
+    y, z = H.moe_mlp(x, ids, w, moe.up, moe.down, r), H.gemm_lora(xl, lora.D, lora.a, lora.b, il, lora.scales)
+    for _ in range(200):
+        ys = [H.moe_mlp(x, ids, w, moe.up, moe.down, r) for _ in range(4)]
+        zs = [H.gemm_lora(xl, lora.D, lora.a, lora.b, il, lora.scales) for _ in range(4)]
+        assert all(torch.equal(v, y) for v in ys) and all(torch.equal(v, z) for v in zs)

@@ -1,0 +1,90 @@
+"""Argument checks of the operators whose rows choose their weights (routing, routed experts, adapters): no GPU needed, nothing
+is launched."""
+import pytest
+
+from paper_2511_19438_b200 import build as libbuild
+
+libbuild.build()
+from paper_2511_19438_b200 import binding as B  # noqa: E402
+
+A16 = 0x1000  # a fake, 16-byte aligned "device address"; validation never dereferences it
+
+
+def route(logits=A16, ids=A16, weights=A16, M=4, E=64, k=8, kind=B.GPTQ_LOGITS_F32, renormalize=1):
+    return B.gptq_moe_route(logits, ids, weights, M, E, k, kind, renormalize, stream=0)
+
+
+def test_route_refusals():
+    for name in ("logits", "ids", "weights"):
+        assert route(**{name: None}) == B.GPTQ_ERR_NULL
+        assert route(**{name: A16 + 4}) == B.GPTQ_ERR_ALIGN
+    for bad in (dict(M=0), dict(E=0), dict(k=0), dict(k=65), dict(M=-1)):
+        assert route(**bad) == B.GPTQ_ERR_SHAPE, bad
+    assert route(E=1025) == B.GPTQ_ERR_UNSUPPORTED
+    assert route(k=33) == B.GPTQ_ERR_UNSUPPORTED
+    for kind in (-1, 3):
+        assert route(kind=kind) == B.GPTQ_ERR_LAYOUT
+
+
+MOE_POINTERS = ["x", "ids", "weights", "gu_qw", "gu_qz", "gu_sc", "gu_perm", "dn_qw", "dn_qz", "dn_sc", "dn_index", "residual", "y"]
+
+
+@pytest.mark.parametrize("fn", [B.gptq_moe_mlp, B.gptq_moe_mlp_bf16])
+def test_moe_refusals(fn):
+    def call(**kw):
+        p = {n: A16 for n in MOE_POINTERS}
+        s = dict(M=2, K=512, F=256, E=8, k=2, group=128, act=1)
+        for n, v in kw.items():
+            (p if n in p else s)[n] = v
+        return fn(*p.values(), *s.values(), stream=0)
+
+    for name in MOE_POINTERS:
+        if name != "residual":
+            assert call(**{name: None}) == B.GPTQ_ERR_NULL, name
+        assert call(**{name: A16 + 8}) == B.GPTQ_ERR_ALIGN, name
+    for bad in (dict(M=0), dict(K=516), dict(F=260), dict(F=0), dict(E=0), dict(k=0), dict(k=9), dict(group=0), dict(K=512 + 64),
+                dict(group=512)):
+        assert call(**bad) == B.GPTQ_ERR_SHAPE, bad
+    assert call(act=2) == B.GPTQ_ERR_LAYOUT
+    assert call(act=-1) == B.GPTQ_ERR_LAYOUT
+    for bad in (dict(group=16), dict(K=192, F=192, group=64), dict(F=192, group=64), dict(E=1025), dict(E=64, k=33)):
+        assert call(**bad) == B.GPTQ_ERR_UNSUPPORTED, bad
+
+
+LORA_POINTERS = ["x", "qw", "qz", "sc", "g_idx", "a", "b", "ids", "scales", "y"]
+
+
+@pytest.mark.parametrize("fn", [B.gptq_gemm_lora, B.gptq_gemm_lora_bf16])
+def test_lora_refusals(fn):
+    def call(**kw):
+        p = {n: A16 for n in LORA_POINTERS}
+        s = dict(M=2, N=256, K=512, group=128, act=1, rank=16, adapters=4)
+        for n, v in kw.items():
+            (p if n in p else s)[n] = v
+        return fn(*p.values(), *s.values(), stream=0)
+
+    for name in LORA_POINTERS:
+        if name != "scales":
+            assert call(**{name: None}) == B.GPTQ_ERR_NULL, name
+        assert call(**{name: A16 + 8}) == B.GPTQ_ERR_ALIGN, name
+    for bad in (dict(M=0), dict(K=516), dict(N=260 + 1), dict(rank=0), dict(adapters=0), dict(group=0)):
+        assert call(**bad) == B.GPTQ_ERR_SHAPE, bad
+    for bad in (dict(act=3), dict(act=-1)):
+        assert call(**bad) == B.GPTQ_ERR_LAYOUT, bad
+    for bad in (dict(group=16), dict(N=192), dict(rank=12), dict(rank=264)):
+        assert call(**bad) == B.GPTQ_ERR_UNSUPPORTED, bad
+
+
+def test_workspace_sizes():
+    # the activation of every slot in 16 bits; with act-order also each slot's row of x; passes of 64 tokens share it
+    assert B.gptq_moe_workspace_bytes(4, 512, 256, 2, 0) == 8 * 256 * 2
+    assert B.gptq_moe_workspace_bytes(4, 512, 256, 2, 1) == 8 * 256 * 2 + 8 * 512 * 2
+    assert B.gptq_moe_workspace_bytes(1000, 512, 256, 2, 0) == 128 * 256 * 2
+    for bad in ((0, 512, 256, 2), (4, 500, 256, 2), (4, 512, 200, 2), (4, 512, 256, 0), (4, 512, 256, 33)):
+        assert B.gptq_moe_workspace_bytes(*bad, 0) == 0
+    few, many = B.gptq_lora_workspace_bytes(16, 256, 512, 128, 0, 16), B.gptq_lora_workspace_bytes(17, 256, 512, 128, 0, 16)
+    assert few >= 16 * 16 * 4 and many >= 17 * 16 * 4 + 17 * 256 * 2
+    assert B.gptq_lora_workspace_bytes(16, 256, 512, 128, 1, 16) == few + 16 * 512 * 2
+    assert B.gptq_lora_workspace_bytes(16, 256, 512, 128, 2, 16) == few
+    for bad in ((0, 256, 512, 128, 0, 16), (4, 200, 512, 128, 0, 16), (4, 256, 512, 128, 0, 12), (4, 256, 512, 16, 0, 16)):
+        assert B.gptq_lora_workspace_bytes(*bad) == 0
