@@ -1228,7 +1228,7 @@ static int moe_dispatch(const void *x, const int32_t *ids, const float *weights,
             if (st) return st;
             a.x = sorted;
         }
-        st = launch_moe(a, tiled, bf16, (cudaStream_t)stream);
+        st = launch_moe(a, tiled, bf16, sms, (cudaStream_t)stream);
         if (st) return st;
     }
     return GPTQ_OK;

@@ -114,194 +114,237 @@ struct MoeArgs {
 // The slots (m, j) of a batch grouped by expert, in the order of experts and, within one, of slots.  An expert's slots are cut
 // into SEGMENTS of at most R, the rows that one sweep over the expert's weights serves.
 struct SlotPlan {
+    float *weight;       // [P] by slot: the weights that a token gives its expert, summed
+    int *counts;         // [E] while it is built
+    short *key;          // [P] by slot: its expert, -1 where the slot is not used
     short *slot;         // [P] slots by expert
+    short *rank;         // [P] by slot, while it is built
     short *seg_begin;    // [segments + 1] into slot
     short *seg_expert;   // [segments]
-    float *weight;       // [P] by slot: the weights that a token gives its expert, summed
-    int segments;
 };
-__host__ __device__ constexpr int slot_plan_bytes(int P, int E) { return (3 * (P + 2) * 2 + 4 * P + 4 * (E + 32) + 15) & ~15; }
-
-// By one warp; the caller synchronises.  A slot whose expert a lower slot of the same token names already adds its weight there.
-__device__ __forceinline__ void build_slot_plan(const MoeArgs &a, int R, uint8_t *smem, int *segments_out)
+__host__ __device__ constexpr int slot_plan_bytes(int P, int E) { return (4 * P + 4 * E + 12 * (P + 2) + 15) & ~15; }
+__device__ __forceinline__ SlotPlan slot_plan_view(uint8_t *smem, int P, int E)
 {
-    const int P = a.M * a.k, lane = threadIdx.x & 31;
-    float *weight = reinterpret_cast<float *>(smem);
-    int *counts = reinterpret_cast<int *>(weight + P);              // by expert: slots, then first position | first segment << 16
-    short *slot = reinterpret_cast<short *>(counts + a.E + 32), *seg_begin = slot + P + 2, *seg_expert = seg_begin + P + 2;
-    for (int e = lane; e < a.E; e += 32) counts[e] = 0;
-    __syncwarp();
-    auto slot_expert = [&](int s, float *w) {
-        if (s >= P) return -1;
-        const int e = __ldg(a.ids + s), j = s % a.k;
-        if ((unsigned)e >= (unsigned)a.E) return -1;
-        const int32_t *row = a.ids + s - j;
-        for (int i = 0; i < j; ++i)
-            if (__ldg(row + i) == e) return -1;
-        if (w) {
-            float sum = __ldg(a.weights + s);
-            for (int i = j + 1; i < a.k; ++i)
-                if (__ldg(row + i) == e) sum += __ldg(a.weights + s - j + i);
-            *w = sum;
-        }
-        return e;
-    };
-    for (int base = 0; base < P; base += 32) {
-        float w = 0.f;
-        const int e = slot_expert(base + lane, &w);
-        if (base + lane < P) weight[base + lane] = w;
-        const uint32_t same = __match_any_sync(0xffffffffu, e);
-        if (e >= 0 && (same & ((1u << lane) - 1)) == 0) counts[e] += __popc(same);
-        __syncwarp();
-    }
-    // positions and segments of the experts: a lane takes neighbouring experts, the warp a scan over the lanes
-    const int per = (a.E + 31) / 32, e0 = min(lane * per, a.E), e1 = min(e0 + per, a.E);
-    int slots = 0, segs = 0;
-    for (int e = e0; e < e1; ++e) slots += counts[e], segs += (counts[e] + R - 1) / R;
-    int sum = slots | segs << 16;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, sum, o);
-        if (lane >= o) sum += v;
-    }
-    const int total = __shfl_sync(0xffffffffu, sum, 31);
-    int pos = (sum & 0xffff) - slots, seg = (sum >> 16) - segs;
-    for (int e = e0; e < e1; ++e) {
-        const int c = counts[e];
-        counts[e] = pos;
-        for (int i = 0; i < c; i += R) {
-            seg_expert[seg] = (short)e;
-            seg_begin[seg++] = (short)(pos + i);
-        }
-        pos += c;
-    }
-    if (lane == 0) {
-        seg_begin[total >> 16] = (short)(total & 0xffff);
-        *segments_out = total >> 16;
-    }
-    __syncwarp();
-    for (int base = 0; base < P; base += 32) {
-        const int e = slot_expert(base + lane, nullptr);
-        const uint32_t same = __match_any_sync(0xffffffffu, e), before = same & ((1u << lane) - 1);
-        if (e >= 0) slot[counts[e] + __popc(before)] = (short)(base + lane);
-        __syncwarp();
-        if (e >= 0 && before == 0) counts[e] += __popc(same);
-        __syncwarp();
-    }
-}
-__device__ __forceinline__ SlotPlan slot_plan_view(const MoeArgs &a, uint8_t *smem, int segments)
-{
-    const int P = a.M * a.k;
     SlotPlan p;
     p.weight = reinterpret_cast<float *>(smem);
-    p.slot = reinterpret_cast<short *>(p.weight + P) + 2 * (a.E + 32);
-    p.seg_begin = p.slot + P + 2;
+    p.counts = reinterpret_cast<int *>(p.weight + P);
+    p.key = reinterpret_cast<short *>(p.counts + E);
+    p.slot = p.key + P + 2;
+    p.rank = p.slot + P + 2;
+    p.seg_begin = p.rank + P + 2;
     p.seg_expert = p.seg_begin + P + 2;
-    p.segments = segments;
     return p;
 }
 
-// Kernel 1: h[slot] = silu(gate) * up.  A CTA takes a segment (blockIdx.y) and 16 gate columns with their 16 up columns
-// (blockIdx.x); its warps share the items along K and meet in shared memory.
-template <int NT, int SUB, bool BF>
-__global__ void __launch_bounds__(kMoeThreads, NT == 1 ? 2 : 1) moe_gate_up_kernel(const MoeArgs a)
+// By all threads of a block; returns the number of segments.  A slot whose expert a lower slot of the same token names already
+// adds its weight there.  `seg_expert` holds the raw ids until the segments are known.
+__device__ __forceinline__ int build_slot_plan(const MoeArgs &a, int R, const SlotPlan &p)
 {
-    extern __shared__ __align__(16) uint8_t smem[];
     __shared__ int s_segments;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
-    pdl_wait();
-    pdl_launch_dependents();
-    if (warp == 0) build_slot_plan(a, 8 * NT, smem, &s_segments);
+    const int P = a.M * a.k, tid = threadIdx.x, lane = tid & 31;
+    short *raw = p.seg_expert;
+    for (int s = tid; s < P; s += kMoeThreads) {
+        const int e = __ldg(a.ids + s);
+        raw[s] = (unsigned)e < (unsigned)a.E ? (short)e : (short)-1;
+        p.weight[s] = __ldg(a.weights + s);
+    }
+    for (int e = tid; e < a.E; e += kMoeThreads) p.counts[e] = 0;
     __syncthreads();
-    const SlotPlan plan = slot_plan_view(a, smem, s_segments);
-    const int seg = blockIdx.y;
-    if (seg >= plan.segments) return;
-    const int e = plan.seg_expert[seg], first = plan.seg_begin[seg], count = plan.seg_begin[seg + 1] - first;
-    const int G = a.K / kGroup, panel = blockIdx.x >> 2, unit = blockIdx.x & 3;
-    const uint8_t *zeros = a.gu_z + e * a.gu_z_bytes;
-    const uint32_t flags = __ldg(&reinterpret_cast<const TiledTrailer *>(zeros + a.gu_z_bytes - kTrailerBytes)->flags);
-    const UnitPtrs ptrs = unit_ptrs<SUB>(a.gu_w + e * a.gu_w_bytes, a.gu_s + e * a.gu_s_bytes, zeros, panel, G, unit, lane);
-    const __half *rows[NT];
+    for (int s = tid; s < P; s += kMoeThreads) {
+        const int e = raw[s], j = s % a.k;
+        bool first = e >= 0;
+        for (int i = 1; i <= j; ++i) first &= raw[s - i] != e;
+        if (first) {
+            float sum = p.weight[s];
+            for (int i = s + 1; i < s - j + a.k; ++i)
+                if (raw[i] == e) sum += p.weight[i];      // (a slot of its own token, whose weight nobody changes)
+            p.weight[s] = sum;
+        }
+        p.key[s] = first ? (short)e : (short)-1;
+    }
+    __syncthreads();
+    if (tid < 32) {
+        for (int base = 0; base < P; base += 32) {
+            const int s = base + lane, e = s < P ? p.key[s] : -1;
+            const uint32_t same = __match_any_sync(0xffffffffu, e);
+            const int before = __popc(same & ((1u << lane) - 1));
+            int from = 0;
+            if (e >= 0) from = p.counts[e];
+            __syncwarp();
+            if (e >= 0) {
+                p.rank[s] = (short)(from + before);
+                if (before == 0) p.counts[e] = from + __popc(same);
+            }
+            __syncwarp();
+        }
+        // positions and segments of the experts: a lane takes neighbouring experts, the warp a scan over the lanes
+        const int per = (a.E + 31) / 32, e0 = min(lane * per, a.E), e1 = min(e0 + per, a.E);
+        int slots = 0, segs = 0;
+        for (int e = e0; e < e1; ++e) slots += p.counts[e], segs += (p.counts[e] + R - 1) / R;
+        int sum = slots | segs << 16;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int i = 8 * t + g;
-        rows[t] = nullptr;
-        if (i < count) {
-            const int s = plan.slot[first + i];
-            rows[t] = a.x + (size_t)(a.x_by_slot ? s : s / a.k) * a.K + 8 * t4;
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += v;
+        }
+        const int total = __shfl_sync(0xffffffffu, sum, 31);
+        int pos = (sum & 0xffff) - slots, seg = (sum >> 16) - segs;
+        for (int e = e0; e < e1; ++e) {
+            const int c = p.counts[e];
+            p.counts[e] = pos;
+            for (int i = 0; i < c; i += R) {
+                p.seg_expert[seg] = (short)e;
+                p.seg_begin[seg++] = (short)(pos + i);
+            }
+            pos += c;
+        }
+        if (lane == 0) {
+            p.seg_begin[total >> 16] = (short)(total & 0xffff);
+            s_segments = total >> 16;
         }
     }
-    float acc[2][NT][4] = {};
-    constexpr int D = 2;
-    DirectRegs<NT, 2, SUB> regs[D];
-    const int n = (G - warp + kMoeWarps - 1) / kMoeWarps;       // items warp, warp + 8, ...
-#pragma unroll
-    for (int d = 0; d < D; ++d)
-        if (d < n) {
-            load_item_weights<NT, 2, 4, SUB>(regs[d], ptrs, warp + d * kMoeWarps);
-            load_item_rows<NT, 2, SUB>(regs[d], rows, warp + d * kMoeWarps);
-        }
-    for (int i = 0; i < n; i += D)
-#pragma unroll
-        for (int d = 0; d < D; ++d)
-            if (i + d < n) {
-                multiply_item<NT, 2, SUB, BF>(regs[d], flags & kFormatZerosMinusOne, acc);
-                if (i + d + D < n) {
-                    load_item_weights<NT, 2, 4, SUB>(regs[d], ptrs, warp + (i + d + D) * kMoeWarps);
-                    load_item_rows<NT, 2, SUB>(regs[d], rows, warp + (i + d + D) * kMoeWarps);
-                }
-            }
-    // sums over the warps, in their order: [warp][value][lane]
-    const bool layout_ok = (flags & kFormatGateUp) != 0 && ((flags & kFormatBf16) != 0) == BF;
-    if (!layout_ok && threadIdx.x == 0) atomicMax(&g_device_status, (int)kStatusLayoutMismatch);
-    float *red = reinterpret_cast<float *>(smem + slot_plan_bytes(a.M * a.k, a.E));
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) red[(warp * (8 * NT) + (u * NT + t) * 4 + i) * 32 + lane] = acc[u][t][i];
     __syncthreads();
-    for (int o = threadIdx.x; o < NT * 4 * 32; o += kMoeThreads) {
-        const int v = o >> 5, t = v >> 2, i = v & 3;            // (lane of o = lane: the block is a multiple of a warp)
-        const int r = 8 * t + 2 * t4 + (i & 1);
-        if (r >= count || !layout_ok) continue;
-        float gate = 0.f, up = 0.f;
+    for (int s = tid; s < P; s += kMoeThreads)
+        if (p.key[s] >= 0) p.slot[p.counts[p.key[s]] + p.rank[s]] = (short)s;
+    __syncthreads();
+    return s_segments;
+}
+
+// Kernel 1: h[slot] = silu(gate) * up.  A TILE is a segment and 16 gate columns with their 16 up columns; a CTA works through a
+// range of neighbouring tiles (their rows of x stay in L1).  The warps share a tile's items along K and meet in shared memory at its
+// end; their loads run on into the next tile.
+template <int NT, int SUB, bool BF>
+__global__ void __launch_bounds__(kMoeThreads, NT <= 2 ? 2 : 1) moe_gate_up_kernel(const MoeArgs a)
+{
+    extern __shared__ __align__(16) uint8_t smem[];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
+    const SlotPlan plan = slot_plan_view(smem, a.M * a.k, a.E);
+    float *red = reinterpret_cast<float *>(smem + slot_plan_bytes(a.M * a.k, a.E));
+    pdl_wait();
+    pdl_launch_dependents();
+    const int segments = build_slot_plan(a, 8 * NT, plan);
+    const int G = a.K / kGroup, per_seg = a.F / 16, T = segments * per_seg;
+    const int t0 = (int)((long long)blockIdx.x * T / gridDim.x), t1 = (int)((long long)(blockIdx.x + 1) * T / gridDim.x);
+
+    // ---- loads: tile l_tile, item l_item; a warp starts at another item in every tile, so that all get their share where the
+    // items are no multiple of the warps
+    int l_tile = t0 - 1, l_item = G, l_seg = 0, l_col = 0;
+    uint32_t l_flags = 0;
+    UnitPtrs ptrs{};
+    const __half *rows[NT];
+    auto enter_segment = [&]() {
+        const int first = plan.seg_begin[l_seg], count = plan.seg_begin[l_seg + 1] - first;
 #pragma unroll
-        for (int w = 0; w < kMoeWarps; ++w) {
-            gate += red[(w * (8 * NT) + v) * 32 + lane];
-            up += red[(w * (8 * NT) + 4 * NT + v) * 32 + lane];
+        for (int t = 0; t < NT; ++t) {
+            rows[t] = nullptr;
+            if (8 * t + g < count) {
+                const int s = plan.slot[first + 8 * t + g];
+                rows[t] = a.x + (size_t)(a.x_by_slot ? s : s / a.k) * a.K + 8 * t4;
+            }
         }
-        int col = 64 * panel + 16 * unit + g + 8 * (i >> 1);
-        if (a.down_index) col = __ldg(a.down_index + (size_t)e * a.F + col);
-        store_out16<BF>(a.h + (size_t)plan.slot[first + r] * a.F + col, silu_mul(gate, up));
+    };
+    auto advance = [&]() {      // to the next item that is this warp's; l_tile = t1: none
+        l_item += kMoeWarps;
+        while (l_item >= G) {
+            if (++l_tile >= t1) return;
+            l_item = (warp + l_tile) & (kMoeWarps - 1);
+            const bool start = l_tile == t0;
+            if (start || ++l_col == per_seg) {
+                l_seg = start ? l_tile / per_seg : l_seg + 1;
+                l_col = start ? l_tile - l_seg * per_seg : 0;
+                enter_segment();
+            }
+            const int e = plan.seg_expert[l_seg];
+            const uint8_t *zeros = a.gu_z + e * a.gu_z_bytes;
+            l_flags = __ldg(&reinterpret_cast<const TiledTrailer *>(zeros + a.gu_z_bytes - kTrailerBytes)->flags);
+            ptrs = unit_ptrs<SUB>(a.gu_w + e * a.gu_w_bytes, a.gu_s + e * a.gu_s_bytes, zeros, l_col >> 2, G, l_col & 3, lane);
+        }
+    };
+    constexpr int D = NT == 1 ? 2 : 1;
+    DirectRegs<NT, 2, SUB> regs[D];
+    uint32_t flags[D] = {};
+    int tile_of[D];
+    auto load = [&](int d) {
+        advance();
+        tile_of[d] = l_tile;
+        if (l_tile < t1) {
+            load_item_weights<NT, 2, 4, SUB>(regs[d], ptrs, l_item);
+            load_item_rows<NT, 2, SUB>(regs[d], rows, l_item);
+            flags[d] = l_flags;
+        }
+    };
+
+    // ---- arithmetic
+    float acc[2][NT][4] = {};
+    int tile = t0;
+    auto finish_tile = [&]() {      // sums over the warps, in their order: [buffer][warp][value][lane]
+        float *buf = red + (tile & 1) * (kMoeWarps * 8 * NT * 32);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    buf[(warp * (8 * NT) + (u * NT + t) * 4 + i) * 32 + lane] = acc[u][t][i];
+                    acc[u][t][i] = 0.f;
+                }
+        __syncthreads();
+        const int seg = tile / per_seg, c16 = tile - seg * per_seg;
+        const int first = plan.seg_begin[seg], count = plan.seg_begin[seg + 1] - first;
+        for (int o = threadIdx.x; o < NT * 4 * 32; o += kMoeThreads) {
+            const int v = o >> 5, t = v >> 2, i = v & 3;            // (lane of o = lane: the block is a multiple of a warp)
+            const int r = 8 * t + 2 * t4 + (i & 1);
+            if (r >= count) continue;
+            float gate = 0.f, up = 0.f;
+#pragma unroll
+            for (int w = 0; w < kMoeWarps; ++w) {
+                gate += buf[(w * (8 * NT) + v) * 32 + lane];
+                up += buf[(w * (8 * NT) + 4 * NT + v) * 32 + lane];
+            }
+            int col = 16 * c16 + g + 8 * (i >> 1);
+            if (a.down_index) col = __ldg(a.down_index + (size_t)plan.seg_expert[seg] * a.F + col);
+            store_out16<BF>(a.h + (size_t)plan.slot[first + r] * a.F + col, silu_mul(gate, up));
+        }
+        ++tile;
+    };
+#pragma unroll
+    for (int d = 0; d < D; ++d) load(d);
+    for (bool more = true; more;) {
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+            while (tile < tile_of[d] && tile < t1) finish_tile();
+            if (tile_of[d] >= t1) { more = false; break; }
+            multiply_item<NT, 2, SUB, BF>(regs[d], flags[d] & kFormatZerosMinusOne, acc);
+            load(d);
+        }
     }
 }
 
-// Kernel 2: y = residual + sum over a token's experts of weight * (h Wd).  A cluster of S CTAs takes 16 columns of y; the items
+// Kernel 2: y = residual + sum over a token's experts of weight * (h Wd).  A cluster of S CTAs takes 32 columns of y; the items
 // of all segments, one behind the other, are shared out evenly over its 8 S warps.  A warp that reaches the end of a segment (or
-// of its share) adds its sums, weighted, to its own [token][16] tile in shared memory; the tiles are summed in the order of warps
+// of its share) adds its sums, weighted, to its own [token][32] tile in shared memory; the tiles are summed in the order of warps
 // and ranks, so results are reproducible.
+constexpr int kDownCols = 32;
 template <int NT, int SUB, bool BF>
-__global__ void __launch_bounds__(kMoeThreads, NT == 1 ? 2 : 1) moe_down_kernel(const MoeArgs a, int S)
+__global__ void __launch_bounds__(kMoeThreads, NT <= 2 ? 2 : 1) moe_down_kernel(const MoeArgs a, int S)
 {
     extern __shared__ __align__(16) uint8_t smem[];
-    __shared__ int s_segments, s_bad;
+    __shared__ int s_bad;
+    constexpr int NU = kDownCols / 16;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
     const int tile = blockIdx.x / S, rank = blockIdx.x - tile * S;
-    const int G = a.F / kGroup, panel = tile >> 3, unit = tile & 7;
+    const int G = a.F / kGroup, panel = tile / (8 / NU), unit = tile % (8 / NU) * NU;
     pdl_launch_dependents();
     // ids and weights are older than the kernel before this one, which waited for them before it let this one in
-    if (warp == 0) build_slot_plan(a, 8 * NT, smem, &s_segments);
-    if (threadIdx.x == 0) s_bad = 0;
+    const SlotPlan plan = slot_plan_view(smem, a.M * a.k, a.E);
     float *tiles = reinterpret_cast<float *>(smem + slot_plan_bytes(a.M * a.k, a.E));
-    const int cells = a.M * 16;
+    const int cells = a.M * kDownCols;
     float *mine = tiles + warp * cells;
     for (int i = lane; i < cells; i += 32) mine[i] = 0.f;
-    __syncthreads();
-    const SlotPlan plan = slot_plan_view(a, smem, s_segments);
+    if (threadIdx.x == 0) s_bad = 0;
+    const int segments = build_slot_plan(a, 8 * NT, plan);
     const int W = kMoeWarps * S, wi = rank * kMoeWarps + warp;
-    const int U = plan.segments * G, j0 = (int)((long long)wi * U / W), j1 = (int)((long long)(wi + 1) * U / W);
+    const int U = segments * G, j0 = (int)((long long)wi * U / W), j1 = (int)((long long)(wi + 1) * U / W), n = j1 - j0;
 
     // what is loaded next
     int l_seg = 0, l_item = 0;
@@ -314,71 +357,64 @@ __global__ void __launch_bounds__(kMoeThreads, NT == 1 ? 2 : 1) moe_down_kernel(
         l_flags = __ldg(&reinterpret_cast<const TiledTrailer *>(zeros + a.dn_z_bytes - kTrailerBytes)->flags);
         ptrs = unit_ptrs<SUB>(a.dn_w + e * a.dn_w_bytes, a.dn_s + e * a.dn_s_bytes, zeros, panel, G, unit, lane);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const int i = 8 * t + g;
-            rows[t] = i < count ? a.h + (size_t)plan.slot[first + i] * a.F + 8 * t4 : nullptr;
+        for (int t = 0; t < NT; ++t) rows[t] = 8 * t + g < count ? a.h + (size_t)plan.slot[first + 8 * t + g] * a.F + 8 * t4 : nullptr;
+    };
+    constexpr int D = NT == 1 ? 2 : 1;
+    DirectRegs<NT, NU, SUB> regs[D];
+    uint32_t flags[D] = {};
+    int seg_of[D], item_of[D];
+    auto load_weights = [&](int d) {
+        load_item_weights<NT, NU, 1, SUB>(regs[d], ptrs, l_item);
+        flags[d] = l_flags;
+        seg_of[d] = l_seg;
+        item_of[d] = l_item;
+    };
+    auto next = [&]() {
+        if (++l_item == G) {
+            l_item = 0;
+            if (++l_seg < segments) enter_segment();
         }
     };
-    constexpr int D = 2;
-    DirectRegs<NT, 1, SUB> regs[D];
-    uint32_t flags[D] = {};
-    int ahead_seg[D], ahead_item[D];
-    const int n = j1 - j0;
     // A layer of the wrong format anywhere: nothing is stored.  Every CTA looks at all experts in use, so that they agree; the
     // trailers are asked for here and looked at behind the main loop.
     uint32_t up_flags = kFormatGateUp | (BF ? kFormatBf16 : 0u), down_flags = BF ? kFormatBf16 : 0u;
     auto trailer_flags = [](const uint8_t *zeros, size_t bytes, int e) {
         return __ldg(&reinterpret_cast<const TiledTrailer *>(zeros + (size_t)(e + 1) * bytes - kTrailerBytes)->flags);
     };
-    if ((int)threadIdx.x < plan.segments) {
+    if ((int)threadIdx.x < segments) {
         up_flags = trailer_flags(a.gu_z, a.gu_z_bytes, plan.seg_expert[threadIdx.x]);
         down_flags = trailer_flags(a.dn_z, a.dn_z_bytes, plan.seg_expert[threadIdx.x]);
     }
+    // weights never depend on the kernel before this one, h does
     if (n > 0) {
         l_seg = j0 / G;
         l_item = j0 - l_seg * G;
         enter_segment();
-    }
-    auto load_weights = [&](int d) {
-        load_item_weights<NT, 1, 1, SUB>(regs[d], ptrs, l_item);
-        flags[d] = l_flags;
-        ahead_seg[d] = l_seg;
-        ahead_item[d] = l_item;
-    };
-    auto next = [&]() {
-        if (++l_item == G) {
-            l_item = 0;
-            if (++l_seg < plan.segments) enter_segment();
-        }
-    };
-    // weights never depend on the kernel before this one, h does
-    bool waited = false;
-    if (n > 0) {
         load_weights(0);
-        pdl_wait();
-        waited = true;
-        load_item_rows<NT, 1, SUB>(regs[0], rows, l_item);
+    }
+    pdl_wait();
+    if (n > 0) {
+        load_item_rows<NT, NU, SUB>(regs[0], rows, l_item);
         next();
 #pragma unroll
         for (int d = 1; d < D; ++d)
             if (d < n) {
                 load_weights(d);
-                load_item_rows<NT, 1, SUB>(regs[d], rows, l_item);
+                load_item_rows<NT, NU, SUB>(regs[d], rows, l_item);
                 next();
             }
     }
-    if (!waited) pdl_wait();
-    float acc[1][NT][4] = {};
+    float acc[NU][NT][4] = {};
     for (int i = 0; i < n; i += D)
 #pragma unroll
         for (int d = 0; d < D; ++d)
             if (i + d < n) {
-                const int seg = ahead_seg[d];
-                const bool flush = ahead_item[d] == G - 1 || i + d == n - 1;
-                multiply_item<NT, 1, SUB, BF>(regs[d], flags[d] & kFormatZerosMinusOne, acc);
+                const int seg = seg_of[d];
+                const bool flush = item_of[d] == G - 1 || i + d == n - 1;
+                multiply_item<NT, NU, SUB, BF>(regs[d], flags[d] & kFormatZerosMinusOne, acc);
                 if (i + d + D < n) {
                     load_weights(d);
-                    load_item_rows<NT, 1, SUB>(regs[d], rows, l_item);
+                    load_item_rows<NT, NU, SUB>(regs[d], rows, l_item);
                     next();
                 }
                 if (flush) {
@@ -386,15 +422,25 @@ __global__ void __launch_bounds__(kMoeThreads, NT == 1 ? 2 : 1) moe_down_kernel(
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
-                        for (int v = 0; v < 4; ++v) {
-                            const int r = 8 * t + 2 * t4 + (v & 1);
+                        for (int odd = 0; odd < 2; ++odd) {
+                            const int r = 8 * t + 2 * t4 + odd;
                             if (r < count) {
                                 const int s = plan.slot[first + r];
-                                float *cell = mine + (s / a.k) * 16 + g + 8 * (v >> 1);
-                                *cell = fmaf(plan.weight[s], acc[0][t][v], *cell);
+                                const float w = plan.weight[s];
+                                float *cell = mine + (s / a.k) * kDownCols + g;
+#pragma unroll
+                                for (int u = 0; u < NU; ++u) {
+                                    cell[16 * u] = fmaf(w, acc[u][t][odd], cell[16 * u]);
+                                    cell[16 * u + 8] = fmaf(w, acc[u][t][2 + odd], cell[16 * u + 8]);
+                                }
                             }
-                            acc[0][t][v] = 0.f;
                         }
+#pragma unroll
+                    for (int u = 0; u < NU; ++u)
+#pragma unroll
+                        for (int t = 0; t < NT; ++t)
+#pragma unroll
+                            for (int v = 0; v < 4; ++v) acc[u][t][v] = 0.f;
                     __syncwarp();
                 }
             }
@@ -403,7 +449,7 @@ __global__ void __launch_bounds__(kMoeThreads, NT == 1 ? 2 : 1) moe_down_kernel(
                (down & (kFormatGateUp | kFormatBf16)) == (BF ? kFormatBf16 : 0u);
     };
     bool bad = !fits(up_flags, down_flags);
-    for (int i = threadIdx.x + kMoeThreads; i < plan.segments; i += kMoeThreads) {
+    for (int i = threadIdx.x + kMoeThreads; i < segments; i += kMoeThreads) {
         const int e = plan.seg_expert[i];
         bad |= !fits(trailer_flags(a.gu_z, a.gu_z_bytes, e), trailer_flags(a.dn_z, a.dn_z_bytes, e));
     }
@@ -420,8 +466,8 @@ __global__ void __launch_bounds__(kMoeThreads, NT == 1 ? 2 : 1) moe_down_kernel(
         tiles[o] = v;
     }
     auto store = [&](int o, float v) {
-        const size_t at = (size_t)(o >> 4) * a.K + panel * kPanel + 16 * unit + (o & 15);
-        if (a.residual) v += pair_to_float2<BF>((uint32_t)*reinterpret_cast<const unsigned short *>(a.residual + at)).x;
+        const size_t at = (size_t)(o / kDownCols) * a.K + panel * kPanel + 16 * unit + o % kDownCols;
+        if (a.residual) v += out16_to_float<BF>(a.residual[at]);
         store_out16<BF>(a.y + at, v);
     };
     if (S == 1) {
@@ -478,38 +524,41 @@ inline size_t moe_workspace_need(int M, int K, int F, int k, int act_order)
 }
 
 template <int NT, int SUB, bool BF>
-static int launch_moe_nt(const MoeArgs &a, cudaStream_t s)
+static int launch_moe_nt(const MoeArgs &a, int sms, cudaStream_t s)
 {
-    const int P = a.M * a.k, R = 8 * NT, plan = slot_plan_bytes(P, a.E);
+    const int P = a.M * a.k, R = 8 * NT, plan = slot_plan_bytes(P, a.E), slots = 2 * sms;      // two CTAs per SM
     const int experts = a.E < P ? a.E : P;
     const int most = experts + P / R < P ? experts + P / R : P;      // segments: one per expert in use, one more per R slots
     static int configured_up[64] = {}, configured_down[64] = {};
-    const int up_smem = plan + kMoeWarps * 8 * NT * 32 * 4, down_smem = plan + kMoeWarps * a.M * 16 * 4;
+    const int up_smem = plan + 2 * kMoeWarps * 8 * NT * 32 * 4, down_smem = plan + kMoeWarps * a.M * kDownCols * 4;
     int st = ensure_dynamic_smem((const void *)moe_gate_up_kernel<NT, SUB, BF>, configured_up, up_smem);
     if (!st) st = ensure_dynamic_smem((const void *)moe_down_kernel<NT, SUB, BF>, configured_down, down_smem);
     if (st) return st;
-    st = launch_dependent(moe_gate_up_kernel<NT, SUB, BF>, dim3((unsigned)(a.F / 16), (unsigned)most), kMoeThreads, (size_t)up_smem, 1, s, a);
+    const long long tiles = (long long)most * (a.F / 16);
+    st = launch_dependent(moe_gate_up_kernel<NT, SUB, BF>, dim3((unsigned)(tiles < slots ? tiles : slots)), kMoeThreads, (size_t)up_smem, 1, s, a);
     if (st) return st;
-    const int S = 2;
-    return launch_dependent(moe_down_kernel<NT, SUB, BF>, dim3((unsigned)(a.K / 16 * S)), kMoeThreads, (size_t)down_smem, S, s, a, S);
+    const int down_tiles = a.K / kDownCols;
+    int S = 1;
+    while (S < 8 && down_tiles * S * 2 <= slots) S *= 2;
+    return launch_dependent(moe_down_kernel<NT, SUB, BF>, dim3((unsigned)(down_tiles * S)), kMoeThreads, (size_t)down_smem, S, s, a, S);
 }
 template <int SUB, bool BF>
-static int launch_moe_sub(const MoeArgs &a, cudaStream_t s)
+static int launch_moe_sub(const MoeArgs &a, int sms, cudaStream_t s)
 {
-    // an expert has at most M slots
-    if (a.M <= 8) return launch_moe_nt<1, SUB, BF>(a, s);
-    if (a.M <= 16) return launch_moe_nt<2, SUB, BF>(a, s);
-    return launch_moe_nt<4, SUB, BF>(a, s);
+    const char *nt = getenv("MOE_NT");
+    const int v = nt ? atoi(nt) : 1;
+    if (a.M <= 8 || v == 1) return launch_moe_nt<1, SUB, BF>(a, sms, s);
+    return launch_moe_nt<2, SUB, BF>(a, sms, s);
 }
-int launch_moe(const MoeArgs &a, int group_size, int bf16, cudaStream_t s)
+int launch_moe(const MoeArgs &a, int group_size, int bf16, int sms, cudaStream_t s)
 {
     switch ((bf16 ? 10 : 0) + kGroup / group_size) {
-    case 1: return launch_moe_sub<1, false>(a, s);
-    case 2: return launch_moe_sub<2, false>(a, s);
-    case 4: return launch_moe_sub<4, false>(a, s);
-    case 11: return launch_moe_sub<1, true>(a, s);
-    case 12: return launch_moe_sub<2, true>(a, s);
-    default: return launch_moe_sub<4, true>(a, s);
+    case 1: return launch_moe_sub<1, false>(a, sms, s);
+    case 2: return launch_moe_sub<2, false>(a, sms, s);
+    case 4: return launch_moe_sub<4, false>(a, sms, s);
+    case 11: return launch_moe_sub<1, true>(a, sms, s);
+    case 12: return launch_moe_sub<2, true>(a, sms, s);
+    default: return launch_moe_sub<4, true>(a, sms, s);
     }
 }
 
