@@ -308,13 +308,14 @@ int gptq_moe_route(const void *logits, int32_t *expert_ids, float *expert_weight
  * counts as 128, the way such layers are tiled; layers with one group per column: pass 128).
  * act_order = 1: gate_up_perm int32 [E, K] = the gate_up layers' perm_out, down_index int32 [E, F] = gptq_invert_perm of the down
  * layers' perm_out.  0: both ignored, may be NULL.  (GPTQ_ACT_ORDER_PRESORTED is refused: each expert has an order of its own.)
- * Arithmetic: exact integers q - z times x, fp32 sums, scales in fp32; the activation in fp32, rounded once to fp16 (a value
- * beyond 65504 becomes an infinity); weights, sums over experts and residual in fp32, one rounding of y.  The order of the sums
- * is fixed: the same inputs give the same bits.
+ * Arithmetic: sum q x and z sum x apart for each quantisation group, both in fp32 (their error: see gptq_gemm's one and two rows),
+ * scales in fp32; the activation in fp32, rounded once to fp16 (a value beyond 65504 becomes an infinity); weights, sums over
+ * experts and residual in fp32, one rounding of y.  The order of the sums is fixed: the same inputs give the same bits.  Sums that
+ * infinities reach are formed as the formula has them.
  * residual may be y; y may be x.  Scratch: gptq_moe_workspace_bytes of the registered workspace (GPTQ_ERR_WORKSPACE without it),
  * under the rules of gptq_set_workspace: calls, and graphs captured from calls, that may run at the same time must not share one.
- * Each expert in use is read once for up to 8 of its tokens (M <= 8), 16 (M <= 16) or 32; M > 64 runs as passes of 64 tokens.  Two kernels per
- * pass, three with act_order.  Layers of another tiling: nothing is stored, and gptq_check_status returns GPTQ_ERR_LAYOUT.
+ * Each expert in use is read once for every 8 of its tokens; M > 64 runs as passes of 64 tokens.  Two kernels per pass, three with
+ * act_order.  Layers of another tiling: nothing is stored, and gptq_check_status returns GPTQ_ERR_LAYOUT.
  * E <= 1024, top_k <= 32 (GPTQ_ERR_UNSUPPORTED).  Stream semantics and other errors as for gptq_gemm. */
 size_t gptq_moe_workspace_bytes(int M, int K, int F, int top_k, int act_order);
 int gptq_moe_mlp(const void *x, const int32_t *expert_ids, const float *expert_weights, const void *gate_up_qweight,
@@ -334,9 +335,11 @@ int gptq_moe_mlp_bf16(const void *x, const int32_t *expert_ids, const float *exp
  * adapter_scales fp32 [adapters] or NULL (1).  An id outside 0 .. adapters-1: the row has no adapter.  rank: a multiple of 8 up
  * to 256 (GPTQ_ERR_UNSUPPORTED).  W, x, y, g_idx, act_order, errors and accuracy of the product with W as for gptq_gemm; with
  * act_order = 1 x and lora_a are in the checkpoint's row order, with GPTQ_ACT_ORDER_PRESORTED both are in the sorted one.
- * x A^T, scaled, is summed and kept in fp32.  Up to 16 rows the expansion joins the fp32 sums before the one rounding of y; above,
- * it is rounded to 16 bits on its way to them.  y must not be x.  Scratch: gptq_lora_workspace_bytes of the registered workspace,
- * always needed.  A layer tiled with GPTQ_FORMAT_GATE_UP or GPTQ_FORMAT_BF16 is refused as by gptq_gemm. */
+ * x A^T, scaled, is summed and kept in fp32.  Up to 8 rows the expansion joins the fp32 sums before the one rounding of y (two
+ * kernels, three with act_order = 1; the products are those of gptq_gemm's one and two rows: sum q x and z sum x apart); above, it
+ * is rounded to 16 bits on its way to them (two kernels and gptq_gemm's).  A row's result does not depend on the other rows'
+ * adapters, whatever these hold.  y must not be x.  Scratch: gptq_lora_workspace_bytes of the registered workspace, always needed,
+ * under the rules of gptq_set_workspace.  A layer tiled with GPTQ_FORMAT_GATE_UP or GPTQ_FORMAT_BF16 is refused as by gptq_gemm. */
 size_t gptq_lora_workspace_bytes(int M, int N, int K, int group_size, int act_order, int rank);
 int gptq_gemm_lora(const void *x, const void *qweight, const void *qzeros, const void *scales, const int32_t *g_idx,
                    const void *lora_a, const void *lora_b, const int32_t *adapter_ids, const float *adapter_scales, void *y,

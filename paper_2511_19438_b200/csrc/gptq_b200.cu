@@ -461,8 +461,8 @@ static int gemm_dispatch(const void *x, const void *qweight, const void *qzeros,
     cudaStream_t s = (cudaStream_t)stream;
     const __half *xin = (const __half *)x;
     const bool extras = bias != nullptr || residual != nullptr;
-    // the fused epilogues exist for fp16 only, but for the additions of the tcgen05 kernels (gptq_gemm_lora_bf16)
-    if (bf16 && (fuse || (extras && M < kUmmaMinTokens))) return GPTQ_ERR_UNSUPPORTED;
+    // the gate/up epilogue exists for fp16 only (gptq_gemm_lora_bf16 brings a residual)
+    if (bf16 && fuse) return GPTQ_ERR_UNSUPPORTED;
     if (act_order == 1) {
         Workspace ws;
         {
@@ -1214,6 +1214,8 @@ static int moe_dispatch(const void *x, const int32_t *ids, const float *weights,
     a.down_index = act_order ? down_index : nullptr;
     a.h = (__half *)ws;
     a.k = top_k, a.E = E, a.K = K, a.F = F;
+    a.sms = sms;
+    a.one = 1;
     a.x_by_slot = act_order;
     for (int m0 = 0; m0 < M; m0 += kMoeMaxRows) {
         a.M = (M - m0) < kMoeMaxRows ? (M - m0) : kMoeMaxRows;
@@ -1228,7 +1230,7 @@ static int moe_dispatch(const void *x, const int32_t *ids, const float *weights,
             if (st) return st;
             a.x = sorted;
         }
-        st = launch_moe(a, tiled, bf16, sms, (cudaStream_t)stream);
+        st = launch_moe(a, tiled, bf16, (cudaStream_t)stream);
         if (st) return st;
     }
     return GPTQ_OK;
@@ -1262,22 +1264,24 @@ static int lora_dispatch(const void *x, const void *qweight, const void *qzeros,
     a.x = (const __half *)x, a.a = (const __half *)lora_a, a.b = (const __half *)lora_b;
     a.ids = adapter_ids, a.scales = adapter_scales, a.v = (float *)(ws + lay.v);
     a.M = M, a.N = N, a.K = K, a.rank = rank, a.adapters = adapters;
-    if (M <= kLoraDirectRows) {
-        const __half *xin = a.x;
-        if (act_order == 1) {
-            st = launch_gather_x(a.x, g_idx, (__half *)ws, M, K, s);
-            if (st) return st;
-            xin = (const __half *)ws;
-        }
-        st = launch_lora_shrink(a, bf16, s);
+    a.k_parts = lora_k_parts(M, K, rank);
+    a.sms = sms;
+    a.one = 1;
+    const __half *xin = a.x;
+    if (M <= kLoraDirectRows && act_order == 1) {
+        st = launch_gather_x(a.x, g_idx, (__half *)ws, M, K, s);
         if (st) return st;
-        return launch_lora_gemm(a, xin, qweight, scales, qzeros, (__half *)y, tiled, bf16, s);
+        xin = (const __half *)ws;
     }
-    __half *delta = (__half *)(ws + lay.delta);
-    st = launch_lora_shrink(a, bf16, s);
-    if (!st) st = launch_lora_delta(a, delta, bf16, s);
+    const bool sorts = M > kLoraDirectRows && act_order == 1;      // (the matmul of many rows is the one after the next: time enough)
+    st = launch_lora_shrink(a, sorts ? g_idx : nullptr, (__half *)ws, bf16, s);
     if (st) return st;
-    return gemm_dispatch(x, qweight, qzeros, scales, g_idx, y, M, N, K, group_size, act_order, 0, nullptr, delta, nullptr, stream, bf16);
+    if (M <= kLoraDirectRows) return launch_lora_gemm(a, xin, qweight, scales, qzeros, (__half *)y, tiled, bf16, s);
+    __half *delta = (__half *)(ws + lay.delta);
+    st = launch_lora_delta(a, delta, bf16, s);
+    if (st) return st;
+    return gemm_dispatch(sorts ? (const void *)ws : x, qweight, qzeros, scales, g_idx, y, M, N, K, group_size, sorts ? GPTQ_ACT_ORDER_PRESORTED : act_order, 0,
+                         nullptr, delta, nullptr, stream, bf16);
 }
 
 extern "C" {

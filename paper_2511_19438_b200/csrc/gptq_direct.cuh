@@ -1,30 +1,44 @@
-// Products of few rows with parts of tiled layers, weights straight from global memory into the registers of the warp that
-// multiplies them: the common ground of the routed-expert kernels (gptq_moe.cuh) and of the projection with adapters
-// (gptq_lora.cuh).
+// Products of few rows with parts of tiled layers, each warp fetching what it multiplies: the common ground of the routed-expert
+// kernels (gptq_moe.cuh) and of the projection with adapters (gptq_lora.cuh).
 //
 // A warp takes NU UNITS (16 columns each) of a panel and some of the panel's 128-row items.  A lane's share of a unit's item
-// is two 16-byte chunks (see the layout in gptq_common.cuh), exactly the A fragments of eight mma.m16n8k16, so a load of 512
-// neighbouring bytes per warp is all there is between memory and the dequantisation: no ring, no barriers, and a warp's work can
-// begin in any layer, panel and row of K - which is what rows that choose their weights need.  The activations are read the
-// same way: lane (g, t4) reads 16 bytes of token row g, which serve as B fragments for all of the warp's units.  Up to 8 NT
-// rows; rows beyond `count` are zeros that no memory is read for.  Loads run kDepth items ahead of the arithmetic.
+// is two 16-byte chunks (see the layout in gptq_common.cuh), exactly the A fragments of eight mma.m16n8k16; it copies them into a
+// ring of its warp's in shared memory with cp.async and reads back what it copied itself (scales and zero points: what its warp did), so that
+// no barrier of the CTA stands between memory and the tensor cores, and a warp's next item may lie in any layer, panel and row of K - which is what rows that choose their
+// weights need.  The ring holds pairs of units: the rest of the item at hand and the whole next one are on their way.  Activations are
+// loaded into registers an item ahead: lane (g, t4) reads 16 bytes of token row g, the B fragments for all of the warp's units.  Up to 8 NT
+// rows; a lane without a row reads another one's, whose products land in columns that nobody looks at.
 //
-// Arithmetic as in the mma.sync kernels: exact integers q - z times x, fp32 sums per quantisation group, the scale in fp32.
+// Arithmetic, fp16: a nibble alone in a 16-bit word is the subnormal number q 2^-24, so the MMAs take `w & 0x000f000f` and
+// `w & 0x00f000f0` as they are (the second kind, 16 q, into sums of its own).  sum (q - z) x = sum q x - z sum x, and sum x of a
+// quantisation group comes from MMAs with a matrix of ones, which all units share.  bfloat16 (subnormals would vanish): 128 + q
+// by one more OR, and -(128 + z) sum x.  All in fp32: the error is that of sums of (q + z) |x| (bfloat16: (256 + q + z) |x|), far
+// below the rounding of the 16-bit results.  Against subtracting z from each weight this is 5 instead of 9 instructions per eight
+// weights; these kernels are bound by instruction issue as much as by memory.
+// An infinity in x makes such a difference NaN, whatever the product is; sums that end up NaN are formed again the long way, in the epilogues.
 #pragma once
+#include <mutex>
+
 #include "gptq_common.cuh"
-#include "gptq_streamk.cuh"
 
 namespace gptq {
 
-// read once, by one SM: not kept in L1
-__device__ __forceinline__ uint4 ldg_stream128(const void *p)
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src)
 {
-    uint4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-    return v;
+    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
-// activations: written by an earlier kernel of the stream, read after griddepcontrol.wait; neighbouring CTAs of an SM read the
-// same rows, so these stay in L1
+__device__ __forceinline__ void cp_async8_if(bool wanted, uint32_t dst, const void *src)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p cp.async.ca.shared.global [%0], [%1], 8;\n\t}"
+                 ::"r"(dst), "l"(src), "r"((uint32_t)wanted) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait()
+{
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+// activations: written by an earlier kernel of the stream, read after it has finished; in L1 for the next tile and CTA
 __device__ __forceinline__ uint4 ldg_rows128(const void *p)
 {
     uint4 v;
@@ -32,100 +46,304 @@ __device__ __forceinline__ uint4 ldg_rows128(const void *p)
     return v;
 }
 
-template <int NT, int NU, int SUB>
-struct DirectRegs {
-    uint4 w[NU][2];               // [K64 block]
-    uint32_t sc[NU][SUB], z[NU][SUB];
-    uint4 x[NT][4];               // [32-row quarter]
-};
+// A stage of the ring, a pair of units of an item: the weights, then for each quantisation group 32 bytes of scales and behind those of both
+// units 8 bytes of zero points per unit.
+constexpr int kPairW = 4 * kUnitBytes, kPairMeta = 80;
+template <int SUB>
+__host__ __device__ constexpr int direct_stage_bytes() { return kPairW + SUB * kPairMeta; }
+template <int NU, int SUB>
+__host__ __device__ constexpr int direct_ring_bytes(int warps) { return warps * (NU / 2 + 2) * direct_stage_bytes<SUB>(); }
 
-// A warp's units within a panel: addresses of item 0, the lane's share added
+// fp16 products take the words of eight rows (four pairs e = 01, 23, 45, 67 of a lane's 16 bytes of x) in the order 01, 45, 23, 67: an
+// activation that only these kernels read is stored that way.
+template <bool BF>
+__host__ __device__ constexpr int direct_column(int c)
+{
+    return BF ? c : (c & ~6) | (c & 2) << 1 | (c & 4) >> 1;
+}
+
+// The warp's units, counted from the first: neighbours, or with GATE_UP a gate unit and its up unit, half a panel further, and so on
+template <bool GATE_UP>
+__host__ __device__ constexpr int unit_offset(int u)
+{
+    return GATE_UP ? u % 2 * 4 + u / 2 : u;
+}
 struct UnitPtrs {
     const uint8_t *w, *s, *z;
 };
+// a unit in item 0 of a panel
 template <int SUB>
-__device__ __forceinline__ UnitPtrs unit_ptrs(const uint8_t *qweight, const uint8_t *scales, const uint8_t *qzeros, int panel, int G,
-                                              int unit, int lane)
+__device__ __forceinline__ UnitPtrs unit_ptrs(const uint8_t *qweight, const uint8_t *scales, const uint8_t *qzeros, int panel, int G, int unit)
 {
     const size_t item = (size_t)panel * G;
-    const int g = lane >> 2;
-    return {qweight + item * kItemWBytes + unit * kUnitBytes + lane * 16, scales + item * (SUB * kItemSBytes) + (16 * unit + 2 * g) * 2,
-            qzeros + item * (SUB * kItemZBytes) + 8 * unit + g};
+    return {qweight + item * kItemWBytes + unit * kUnitBytes, scales + item * (SUB * kItemSBytes) + unit * 32, qzeros + item * (SUB * kItemZBytes) + unit * 8};
+}
+// The same with a lane's share added: 16 bytes of weights; of the pair's scales 8 bytes for a lane below 8 SUB, of its zero points for a
+// lane below 2 SUB.
+template <bool GATE_UP, int SUB>
+__device__ __forceinline__ UnitPtrs lane_ptrs(UnitPtrs p, int lane)
+{
+    p.w += lane * 16;
+    p.s += (lane >> 3) * kItemSBytes + unit_offset<GATE_UP>(lane >> 2 & 1) * 32 + (lane & 3) * 8;
+    p.z += (lane >> 1) * kItemZBytes + unit_offset<GATE_UP>(lane & 1) * 8;
+    return p;
+}
+// What a warp multiplies next: the item's addresses, the lane's token rows at the item's first column + 8 t4, the layer's
+// format flags as loaded (looked at only when the item is multiplied), a number of the caller's
+// (not negative), and how many of the warp's pairs of units are wanted (the others' sums stay as they are).
+template <int NT>
+struct DirectItem {
+    UnitPtrs p;
+    const __half *x[NT];
+    uint32_t flags;
+    int tag, pairs;
+};
+template <int NT, int SUB>
+__device__ __forceinline__ void set_item(DirectItem<NT> &it, const UnitPtrs &p, const __half *const (&rows)[NT], int item)
+{
+    it.p.w = p.w + (size_t)item * kItemWBytes;
+    it.p.s = p.s + (size_t)item * (SUB * kItemSBytes);
+    it.p.z = p.z + (size_t)item * (SUB * kItemZBytes);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) it.x[t] = rows[t] + (size_t)item * kGroup;
 }
 
-// DU: distance of the warp's units (1 neighbours, 4 a gate unit and its up unit)
-template <int NT, int NU, int DU, int SUB>
-__device__ __forceinline__ void load_item_weights(DirectRegs<NT, NU, SUB> &r, const UnitPtrs &p, int item)
+template <int NT>
+struct DirectRows {
+    uint4 x[NT][4];               // [32-row quarter]
+    uint32_t flags;
+    int tag, pairs;
+};
+template <int NT>
+__device__ __forceinline__ void load_rows(DirectRows<NT> &r, const DirectItem<NT> &it)
 {
-#pragma unroll
-    for (int u = 0; u < NU; ++u) {
-        const uint8_t *w = p.w + (size_t)item * kItemWBytes + u * DU * kUnitBytes;
-        r.w[u][0] = ldg_stream128(w);
-        r.w[u][1] = ldg_stream128(w + kBlockWBytes);
-#pragma unroll
-        for (int sub = 0; sub < SUB; ++sub) {
-            r.sc[u][sub] = __ldg(reinterpret_cast<const uint32_t *>(p.s + (size_t)item * (SUB * kItemSBytes) + sub * kItemSBytes + u * DU * 32));
-            r.z[u][sub] = __ldg(p.z + (size_t)item * (SUB * kItemZBytes) + sub * kItemZBytes + u * DU * 8);
-        }
-    }
-}
-// rows[t]: the lane's token row of tile t at column 8 * t4 (nullptr: none)
-template <int NT, int NU, int SUB>
-__device__ __forceinline__ void load_item_rows(DirectRegs<NT, NU, SUB> &r, const __half *const (&rows)[NT], int item)
-{
+    r.tag = it.tag;
+    r.flags = it.flags;
+    r.pairs = it.pairs;
+    if (it.tag < 0) return;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            r.x[t][q] = rows[t] ? ldg_rows128(rows[t] + (size_t)item * kGroup + 32 * q) : make_uint4(0, 0, 0, 0);
+        for (int q = 0; q < 4; ++q) r.x[t][q] = ldg_rows128(it.x[t] + 32 * q);
 }
 
-// acc[u][t][i]: column g + 8 (i >> 1) of unit u, token 8 t + 2 t4 + (i & 1)
-template <int NT, int NU, int SUB, bool BF>
-__device__ __forceinline__ void multiply_item(const DirectRegs<NT, NU, SUB> &r, uint32_t z_add, float (&acc)[NU][NT][4])
+__device__ __forceinline__ uint64_t register_pair(uint32_t lo, uint32_t hi)
 {
+    uint64_t p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "r"(lo), "r"(hi));
+    return p;
+}
+// D = A B (START) or D += A B
+template <bool BF, bool START>
+__device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint64_t b)
+{
+#define GPTQ_MMA16(TYPE, D, C, ...)                                                                                           \
+    asm("{\n\t.reg .b32 b0, b1;\n\tmov.b64 {b0, b1}, %8;\n\t"                                                                \
+        "mma.sync.aligned.m16n8k16.row.col.f32." TYPE "." TYPE ".f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {b0,b1}, " C ";\n\t}"      \
+        : D(d[0]), D(d[1]), D(d[2]), D(d[3])                                                                                  \
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "l"(b) __VA_ARGS__)
+    if constexpr (START) {
+        if constexpr (BF) GPTQ_MMA16("bf16", "=f", "{%9,%9,%9,%9}", , "f"(0.f));
+        else GPTQ_MMA16("f16", "=f", "{%9,%9,%9,%9}", , "f"(0.f));
+    } else {
+        if constexpr (BF) GPTQ_MMA16("bf16", "+f", "{%0,%1,%2,%3}", );
+        else GPTQ_MMA16("f16", "+f", "{%0,%1,%2,%3}", );
+    }
+#undef GPTQ_MMA16
+}
+template <bool BF>
+__device__ __forceinline__ void mma16_from(bool start, float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint64_t b)
+{
+    if (start) mma16<BF, true>(d, a0, a1, a2, a3, b);
+    else mma16<BF, false>(d, a0, a1, a2, a3, b);
+}
+
+// What the units of an item share: x as B fragments, in the order of the products below, and its sums over the quantisation groups
+// (elements 2 and 3 repeat 0 and 1).
+template <int NT, int SUB>
+struct ItemRows {
+    uint64_t xp[NT][4][2];
+    float xs[SUB][NT][4];
+};
+// IN_ORDER: x lies in memory as direct_column has it.  Else its words change places, by multiplications with `one` = 1 that the
+// compiler cannot see through: as plain moves they are made anew for every unit (84 moves per item of four units instead of 16).
+template <int NT, int SUB, bool BF, bool IN_ORDER>
+__device__ __forceinline__ void prepare_rows(ItemRows<NT, SUB> &rows, const uint4 (&x)[NT][4], uint32_t one)
+{
+    constexpr uint32_t ONES = BF ? 0x3f803f80u : 0x3c003c00u;
 #pragma unroll
-    for (int u = 0; u < NU; ++u) {
-        float gs[NT][4];
-        uint32_t zloA = 0, zhiA = 0, zloB = 0, zhiB = 0;
+    for (int q = 0; q < 4; ++q) {
+        const int sub = q * SUB / 4;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const uint4 v = x[t][q];
+            if constexpr (BF || IN_ORDER) {
+                rows.xp[t][q][0] = register_pair(v.x, v.y);
+                rows.xp[t][q][1] = register_pair(v.z, v.w);
+            } else {
+                rows.xp[t][q][0] = register_pair(v.x * one, v.z * one);
+                rows.xp[t][q][1] = register_pair(v.y * one, v.w * one);
+            }
+            mma16_from<BF>(q * SUB % 4 == 0, rows.xs[sub][t], ONES, ONES, ONES, ONES, rows.xp[t][q][0]);
+            mma16<BF, false>(rows.xs[sub][t], ONES, ONES, ONES, ONES, rows.xp[t][q][1]);
+        }
+    }
+}
+
+// acc[u][t][i], u = U0, U0 + 1: column g + 8 (i >> 1) of unit u, token 8 t + 2 t4 + (i & 1); `stage`: the pair's stage of the ring
+template <int U0, int NT, int NU, int SUB, bool BF>
+__device__ __forceinline__ void multiply_pair(uint32_t stage, int lane, uint32_t flags, const ItemRows<NT, SUB> &rows, float (&acc)[NU][NT][4])
+{
+    const uint32_t slot = stage + lane * 16, meta = stage + kPairW + (lane >> 2) * 4, zeros = stage + kPairW + 64 + (lane >> 2);
+    constexpr uint32_t LO = 0x000f000fu, HI = 0x00f000f0u, MAGIC = 0x43004300u;
+    const float z_add = (flags & kFormatZerosMinusOne) ? 1.f : 0.f;
+    // -z as floats: the nibble in the lowest bits of 2^23, or 16 z there
+    const float c_lo = 8388608.f - (BF ? 128.f : 0.f) - z_add, c_hi = 524288.f - (BF ? 128.f : 0.f) - z_add;
+#pragma unroll
+    for (int u = U0; u < U0 + 2; ++u) {
+        const uint4 wq[2] = {lds128(slot + (u - U0) * 2 * kUnitBytes), lds128(slot + (u - U0) * 2 * kUnitBytes + kUnitBytes)};
+        float lo[NT][4], hi[NT][4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const int sub = q * SUB / 4;
-            if (q * SUB % 4 == 0) {                 // first quarter of a quantisation group
+            const bool start = q * SUB % 4 == 0;    // first quarter of a quantisation group
+            const uint32_t a = (q & 1) ? wq[q >> 1].y : wq[q >> 1].x, b = (q & 1) ? wq[q >> 1].w : wq[q >> 1].z;
+            if constexpr (BF) {
+                const uint32_t a0 = lop3_and_or(a, LO, MAGIC), a1 = lop3_and_or(a >> 4, LO, MAGIC), a2 = lop3_and_or(a >> 8, LO, MAGIC),
+                               a3 = lop3_and_or(a >> 12, LO, MAGIC);
+                const uint32_t b0 = lop3_and_or(b, LO, MAGIC), b1 = lop3_and_or(b >> 4, LO, MAGIC), b2 = lop3_and_or(b >> 8, LO, MAGIC),
+                               b3 = lop3_and_or(b >> 12, LO, MAGIC);
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
+                for (int t = 0; t < NT; ++t) {
+                    mma16_from<true>(start, lo[t], a0, b0, a1, b1, rows.xp[t][q][0]);
+                    mma16<true, false>(lo[t], a2, b2, a3, b3, rows.xp[t][q][1]);
+                }
+            } else {
+                const uint32_t a8 = a >> 8, b8 = b >> 8;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) gs[t][i] = 0.f;
-                zero_constants<BF>((r.z[u][sub] & 15u) + z_add, zloA, zhiA);
-                zero_constants<BF>((r.z[u][sub] >> 4) + z_add, zloB, zhiB);
-            }
-            const uint4 wq = r.w[u][q >> 1];
-            uint32_t pA[4], pB[4];
-            nibble_pairs_minus_zero<BF>((q & 1) ? wq.y : wq.x, zloA, zhiA, pA);
-            nibble_pairs_minus_zero<BF>((q & 1) ? wq.w : wq.z, zloB, zhiB, pB);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const uint4 xb = r.x[t][q];
-                if constexpr (BF) {
-                    mma_m16n8k16_bf16(gs[t], pA[0], pB[0], pA[1], pB[1], xb.x, xb.y);
-                    mma_m16n8k16_bf16(gs[t], pA[2], pB[2], pA[3], pB[3], xb.z, xb.w);
-                } else {
-                    mma_m16n8k16(gs[t], pA[0], pB[0], pA[1], pB[1], xb.x, xb.y);
-                    mma_m16n8k16(gs[t], pA[2], pB[2], pA[3], pB[3], xb.z, xb.w);
+                for (int t = 0; t < NT; ++t) {
+                    mma16_from<false>(start, lo[t], a & LO, b & LO, a8 & LO, b8 & LO, rows.xp[t][q][0]);
+                    mma16_from<false>(start, hi[t], a & HI, b & HI, a8 & HI, b8 & HI, rows.xp[t][q][1]);
                 }
             }
             if ((q + 1) * SUB % 4 == 0) {           // last quarter of the group
-                const float2 sf = pair_to_float2<BF>(r.sc[u][sub]);
+                const float2 sf = pair_to_float2<BF>(lds32(meta + sub * kPairMeta + (u - U0) * 32));
+                const uint32_t zz = lds8(zeros + sub * kPairMeta + (u - U0) * 8);
+                const float za = c_lo - __uint_as_float((zz & 15u) | 0x4b000000u);
+                const float zb = fmaf(__uint_as_float((zz & 0xf0u) | 0x4b000000u), -0.0625f, c_hi);
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    acc[u][t][0] = fmaf(sf.x, gs[t][0], acc[u][t][0]);
-                    acc[u][t][1] = fmaf(sf.x, gs[t][1], acc[u][t][1]);
-                    acc[u][t][2] = fmaf(sf.y, gs[t][2], acc[u][t][2]);
-                    acc[u][t][3] = fmaf(sf.y, gs[t][3], acc[u][t][3]);
-                }
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float v = lo[t][i];
+                        if constexpr (!BF) v = fmaf(hi[t][i], 1048576.f, v * 16777216.f);
+                        v = fmaf(i < 2 ? za : zb, rows.xs[sub][t][i & 1], v);
+                        acc[u][t][i] = fmaf(i < 2 ? sf.x : sf.y, v, acc[u][t][i]);
+                    }
             }
         }
     }
+}
+
+// Works through the items that `next` yields (it fills a DirectItem, tag < 0 at the end); `before(tag)` is called ahead of each
+// item's product.  `ring`: the warp's part of the ring.
+// A stage is filled again a pair after it was read: the reads are over.
+template <int NT, int NU, bool GATE_UP, int SUB, bool BF, bool IN_ORDER, typename Next, typename Before>
+__device__ __forceinline__ void stream_items(uint32_t ring, int lane, uint32_t one, float (&acc)[NU][NT][4], Next next, Before before)
+{
+    static_assert(NU == 2 || NU == 4, "one or two pairs of units");
+    constexpr int NP = NU / 2, kStages = NP + 2;
+    constexpr uint32_t kStage = direct_stage_bytes<SUB>(), kEnd = kStages * kStage;
+    DirectItem<NT> it{};
+    DirectRows<NT> x;
+    uint32_t fill = 0, at = 0;      // offsets into the ring
+    auto advance = [&](uint32_t &offset) { offset = offset == kEnd - kStage ? 0 : offset + kStage; };
+    auto copy_pair = [&](int pair) {
+        if (it.tag >= 0 && pair < it.pairs) {
+            const uint32_t to = ring + fill;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const uint8_t *src = it.p.w + unit_offset<GATE_UP>(2 * pair + u) * kUnitBytes;
+                cp_async16(to + lane * 16 + u * 2 * kUnitBytes, src);
+                cp_async16(to + lane * 16 + u * 2 * kUnitBytes + kUnitBytes, src + kBlockWBytes);
+            }
+            cp_async8_if(lane < 8 * SUB, to + kPairW + (lane >> 3) * kPairMeta + (lane & 7) * 8, it.p.s + unit_offset<GATE_UP>(2 * pair) * 32);
+            cp_async8_if(lane < 2 * SUB, to + kPairW + (lane >> 1) * kPairMeta + 64 + (lane & 1) * 8, it.p.z + unit_offset<GATE_UP>(2 * pair) * 8);
+        }
+        cp_async_commit();
+        advance(fill);
+    };
+    next(it);
+#pragma unroll
+    for (int p = 0; p < NP; ++p) copy_pair(p);
+    load_rows<NT>(x, it);
+    next(it);
+    copy_pair(0);
+    while (x.tag >= 0) {
+        before(x.tag);
+        ItemRows<NT, SUB> rows;
+        prepare_rows<NT, SUB, BF, IN_ORDER>(rows, x.x, one);
+        const uint32_t flags = x.flags;
+        const int pairs = x.pairs;
+        load_rows<NT>(x, it);
+        if constexpr (NP == 2) {
+            copy_pair(1);
+            cp_async_wait<NP + 1>();
+            __syncwarp();      // (the scales and zero points are other lanes' copies)
+            multiply_pair<0, NT, NU, SUB, BF>(ring + at, lane, flags, rows, acc);
+            advance(at);
+        }
+        next(it);
+        copy_pair(0);
+        cp_async_wait<NP + 1>();
+        __syncwarp();
+        if (NP == 1 || pairs == NP) multiply_pair<NU - 2, NT, NU, SUB, BF>(ring + at, lane, flags, rows, acc);
+        advance(at);
+    }
+}
+
+// The sum over n items for one column (0 .. 15) of a unit and one token row, the formula as it stands, for sums that came out NaN.
+// w, s, z: the unit's addresses without a lane's share; in_order: the row lies in memory as direct_column has it.
+template <bool BF>
+__device__ __noinline__ float long_sum(const uint8_t *w, const uint8_t *s, const uint8_t *z, int sub, int col, uint32_t z_add,
+                                       const __half *row, int n, bool in_order)
+{
+    const int g = col & 7, h = col >> 3;
+    float sum = 0.f;
+    for (int item = 0; item < n; ++item)
+        for (int k = 0; k < kGroup; ++k) {
+            const int blk = k >> 6, j = (k >> 5) & 1, t4 = (k >> 3) & 3, e = k & 7;
+            const size_t grp = (size_t)item * sub + k * sub / kGroup;
+            const uint32_t word = *reinterpret_cast<const uint32_t *>(w + (size_t)item * kItemWBytes + blk * kBlockWBytes + (4 * g + t4) * 16 + (j + 2 * h) * 4);
+            const uint32_t zb = z[grp * kItemZBytes + g];
+            const int q = (int)((word >> (4 * nibble_slot(e))) & 15u) - (int)((h ? zb >> 4 : zb & 15u) + z_add);
+            const float sc = out16_to_float<BF>(*reinterpret_cast<const __half *>(s + grp * kItemSBytes + (2 * g + h) * 2));
+            sum = fmaf((float)q * sc, out16_to_float<BF>(row[(size_t)item * kGroup + (in_order ? direct_column<BF>(k) : k)]), sum);
+        }
+    return sum;
+}
+
+// n things given out to `parts` in neighbouring ranges, the longer ranges spread evenly: the first of range i
+__device__ __forceinline__ int share_begin(int n, int parts, int i) { return (int)((unsigned long long)n * (unsigned)i / (unsigned)parts); }
+
+// Allows a kernel `smem_bytes` of dynamic shared memory and asks for room for `ctas` such CTAs per SM; what is left of the SM's
+// 256 KB is L1, in which these kernels keep the rows that they read again and again.
+static int ensure_direct_smem(const void *kernel, int *configured, int smem_bytes, int ctas)
+{
+    static std::mutex mu;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return record_cuda_error(e);
+    if (dev < 0 || dev >= 64) return GPTQ_ERR_UNSUPPORTED;
+    std::lock_guard<std::mutex> lock(mu);
+    if (configured[dev] >= smem_bytes) return GPTQ_OK;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes);
+    if (e != cudaSuccess) return record_cuda_error(e);
+    const int percent = (ctas * (smem_bytes + 2048) * 100 + 228 * 1024 - 1) / (228 * 1024);
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, percent < 100 ? percent : 100);
+    if (e != cudaSuccess) return record_cuda_error(e);
+    configured[dev] = smem_bytes;
+    return GPTQ_OK;
 }
 
 // a kernel launched as a programmatic dependent, in clusters of `cluster` CTAs
@@ -137,7 +355,7 @@ static int launch_dependent(void (*kernel)(Params...), dim3 grid, int threads, s
     cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
-    cudaLaunchAttribute attr[2];
+    cudaLaunchAttribute attr[3];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
@@ -145,7 +363,9 @@ static int launch_dependent(void (*kernel)(Params...), dim3 grid, int threads, s
     attr[1].val.clusterDim.y = 1;
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    attr[2].id = cudaLaunchAttributeClusterSchedulingPolicyPreference;      // clusters spread over the SMs
+    attr[2].val.clusterSchedulingPolicyPreference = cudaClusterSchedulingPolicyLoadBalancing;
+    cfg.numAttrs = cluster > 1 ? 3 : 1;
     return record_cuda_error(cudaLaunchKernelEx(&cfg, kernel, Params(args)...));
 }
 

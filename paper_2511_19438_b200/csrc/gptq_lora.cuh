@@ -1,9 +1,13 @@
 // A shared projection with a low-rank adapter per row: y[m] = x[m] W + scale[a] (x[m] A[a]^T) B[a]^T, a = adapter_ids[m].
 //
-// v[m] = scale[a] x[m] A[a]^T is formed first, in fp32, by a small kernel (`lora_shrink_kernel`).  Up to 16 rows the product with
-// W and the expansion v B^T are one kernel: its weights and x are under way while v is still being formed, the expansion joins
-// the fp32 sums in the epilogue and y is rounded once.  Above that the expansion is written out (16 bits) and joins the tcgen05
-// kernels' fp32 sums as their residual.
+// v[m] = scale[a] x[m] A[a]^T is formed first, in fp32 (`lora_shrink_kernel`).  Up to 8 rows the product with W and the expansion
+// v B^T are one kernel: its weights and x are under way while v is still being formed, the expansion joins the fp32 sums in the epilogue
+// and y is rounded once.  Above that `lora_delta_kernel` writes the expansion out (16 bits) and it joins the other matmul kernels' fp32
+// sums as their residual.
+//
+// Both adapter kernels look at eight rows at a time, the eight columns of an MMA, and go through the adapters that these name: one for
+// a run of rows of a prompt, up to eight in a decode batch.  A product is formed for all eight rows and kept for those whose adapter
+// it is, so that nothing of another row's adapter, whatever it holds, reaches a row.
 #pragma once
 #include "gptq_common.cuh"
 #include "gptq_direct.cuh"
@@ -11,134 +15,395 @@
 namespace gptq {
 
 constexpr int kLoraMaxRank = 256;
-constexpr int kLoraDirectRows = 16;      // rows of the fused kernel
+constexpr int kLoraDirectRows = 8;       // rows of the fused kernel
 constexpr int kLoraWarps = 8, kLoraThreads = 32 * kLoraWarps;
+constexpr int kLoraDecodeRows = 64;      // up to here rows are taken to have adapters of their own, above to come in runs
+constexpr int kLoraSteps = 4;            // 32-column steps of K that a warp of the shrink kernel requests at once
+
+template <int N>
+struct Int {
+    static constexpr int value = N;
+};
 
 struct LoraArgs {
     const __half *x;          // [M, K] as given
     const __half *a, *b;      // [adapters, rank, K], [adapters, N, rank]
     const int32_t *ids;       // [M]
     const float *scales;      // [adapters] or nullptr
-    float *v;                 // [M, rank]
+    float *v;                 // [k_parts, M, rank]: the sums over parts of K
     int M, N, K, rank, adapters;
+    int k_parts;
+    int sms;
+    uint32_t one;             // 1 (see prepare_rows)
 };
 
-template <bool BF>
-__device__ __forceinline__ float dot8(const uint4 &p, const uint4 &q, float sum)
-{
-    const uint32_t a[4] = {p.x, p.y, p.z, p.w}, b[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 u = pair_to_float2<BF>(a[i]), w = pair_to_float2<BF>(b[i]);
-        sum = fmaf(u.x, w.x, sum);
-        sum = fmaf(u.y, w.y, sum);
+// The adapters that eight rows name, from row m0 on: lane l < 8 holds row l's id (-1: none) and the first row of each adapter leads.
+struct RowAdapters {
+    int id;
+    uint32_t leads;
+    // the id of the j-th adapter (j < popc(leads)) and the rows that have it
+    __device__ __forceinline__ int adapter(int j, uint32_t &rows) const
+    {
+        uint32_t left = leads;
+        for (; j; --j) left &= left - 1;
+        const int a = __shfl_sync(0xffffffffu, id, __ffs(left) - 1);
+        rows = __ballot_sync(0xffffffffu, id == a);
+        return a;
     }
-    return sum;
+};
+__device__ __forceinline__ RowAdapters row_adapters(const LoraArgs &a, int m0, int lane)
+{
+    RowAdapters r;
+    r.id = lane < 8 && m0 + lane < a.M ? __ldg(a.ids + m0 + lane) : -1;
+    if ((unsigned)r.id >= (unsigned)a.adapters) r.id = -1;
+    const uint32_t same = __match_any_sync(0xffffffffu, r.id);
+    r.leads = __ballot_sync(0xffffffffu, r.id >= 0 && (same & ((1u << lane) - 1)) == 0);
+    return r;
 }
 
-// A warp forms one element of v.
+// v of eight rows (blockIdx.x), 16 of an adapter's rank (blockIdx.y) and a part of K: rows of A as the 16-row operand, rows of x as
+// the columns, the warps sharing the part's steps of 32 columns.  blockIdx.z: part of K, and which of the adapters.
+//
+// Slices of blockIdx.z beyond these put rows of x in the sorted row order of an act-order layer, for the matmul: a launch less.
 template <bool BF>
-__global__ void __launch_bounds__(kLoraThreads) lora_shrink_kernel(const LoraArgs a)
+__global__ void __launch_bounds__(kLoraThreads, 4) lora_shrink_kernel(const LoraArgs a, int adapters_apart, const int32_t *__restrict__ perm, __half *__restrict__ x_sorted)
 {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, m = blockIdx.y, r = blockIdx.x * kLoraWarps + warp;
+    __shared__ float red[kLoraWarps][4][32];
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
+    const int m0 = 8 * blockIdx.x, r0 = 16 * blockIdx.y, part = blockIdx.z / adapters_apart;
     pdl_wait();
     pdl_launch_dependents();        // (behind the wait: what x was before this kernel is what the next one may read at once)
-    const int id = __ldg(a.ids + m);
-    if ((unsigned)id >= (unsigned)a.adapters || r >= a.rank) return;
-    const uint4 *xr = reinterpret_cast<const uint4 *>(a.x + (size_t)m * a.K);
-    const uint4 *ar = reinterpret_cast<const uint4 *>(a.a + ((size_t)id * a.rank + r) * a.K);
-    float sum = 0.f;
-#pragma unroll 4
-    for (int c = lane; c < a.K / 8; c += 32) sum = dot8<BF>(__ldg(xr + c), ldg_stream128(ar + c), sum);
+    if (part >= a.k_parts) {
+        const int slice = (blockIdx.z - adapters_apart * a.k_parts) * gridDim.y + blockIdx.y, slices = (gridDim.z - adapters_apart * a.k_parts) * gridDim.y;
+        for (int i = 2 * (slice * kLoraThreads + threadIdx.x); i < a.K; i += 2 * slices * kLoraThreads) {
+            const int2 from = __ldg(reinterpret_cast<const int2 *>(perm + i));
+            const int rows = min(8, a.M - m0);
+            __half2 v[8];
 #pragma unroll
-    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (lane == 0) a.v[(size_t)m * a.rank + r] = a.scales ? sum * __ldg(a.scales + id) : sum;
-}
-
-// (v B^T)[m][n]; v is read after the kernel that wrote it has finished
-template <bool BF>
-__device__ __forceinline__ float lora_expand(const LoraArgs &a, int m, int n)
-{
-    const int id = __ldg(a.ids + m);
-    if ((unsigned)id >= (unsigned)a.adapters) return 0.f;
-    const uint4 *b = reinterpret_cast<const uint4 *>(a.b + ((size_t)id * a.N + n) * a.rank);
-    const float4 *v = reinterpret_cast<const float4 *>(a.v + (size_t)m * a.rank);
-    float sum = 0.f;
-    for (int c = 0; c < a.rank / 8; ++c) {
-        const uint4 p = __ldg(b + c);
-        const float4 lo = v[2 * c], hi = v[2 * c + 1];
-        const float2 p0 = pair_to_float2<BF>(p.x), p1 = pair_to_float2<BF>(p.y), p2 = pair_to_float2<BF>(p.z), p3 = pair_to_float2<BF>(p.w);
-        sum = fmaf(p0.x, lo.x, sum), sum = fmaf(p0.y, lo.y, sum), sum = fmaf(p1.x, lo.z, sum), sum = fmaf(p1.y, lo.w, sum);
-        sum = fmaf(p2.x, hi.x, sum), sum = fmaf(p2.y, hi.y, sum), sum = fmaf(p3.x, hi.z, sum), sum = fmaf(p3.y, hi.w, sum);
+            for (int r = 0; r < 8; ++r) {
+                const __half *row = a.x + (size_t)(m0 + min(r, rows - 1)) * a.K;
+                v[r] = __halves2half2(row[from.x], row[from.y]);
+            }
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+                if (r < rows) *reinterpret_cast<__half2 *>(x_sorted + (size_t)(m0 + r) * a.K + i) = v[r];
+        }
+        return;
     }
-    return sum;
+    const RowAdapters named = row_adapters(a, m0, lane);
+    const int n = __popc(named.leads);
+    const int w = part * kLoraWarps + warp, W = a.k_parts * kLoraWarps;
+    const int s0 = share_begin(a.K / 32, W, w), s1 = share_begin(a.K / 32, W, w + 1);
+    const __half *xr = a.x + (size_t)min(m0 + g, a.M - 1) * a.K + 8 * t4;
+    for (int j = blockIdx.z % adapters_apart; j < n; j += adapters_apart) {
+        uint32_t rows;
+        const int id = named.adapter(j, rows);
+        const __half *lo = a.a + ((size_t)id * a.rank + r0 + g) * a.K + 8 * t4, *hi = lo + (size_t)8 * a.K;
+        const bool has_hi = r0 + 8 < a.rank;      // the rank is a multiple of 8
+        if (!has_hi) hi = lo;
+        float acc[4] = {};
+        int s = s0;
+        auto batch = [&](auto steps) {      // all of a batch's loads before its products
+            constexpr int n_steps = decltype(steps)::value;
+            uint4 p[n_steps], q[n_steps], v[n_steps];
+#pragma unroll
+            for (int i = 0; i < n_steps; ++i) {
+                p[i] = __ldg(reinterpret_cast<const uint4 *>(lo + 32 * (s + i)));
+                q[i] = __ldg(reinterpret_cast<const uint4 *>(hi + 32 * (s + i)));
+                v[i] = *reinterpret_cast<const uint4 *>(xr + 32 * (s + i));
+            }
+#pragma unroll
+            for (int i = 0; i < n_steps; ++i) {
+                mma16<BF, false>(acc, p[i].x, q[i].x, p[i].y, q[i].y, register_pair(v[i].x, v[i].y));
+                mma16<BF, false>(acc, p[i].z, q[i].z, p[i].w, q[i].w, register_pair(v[i].z, v[i].w));
+            }
+            s += n_steps;
+        };
+        while (s + kLoraSteps <= s1) batch(Int<kLoraSteps>{});
+        if (s + 3 == s1) batch(Int<3>{});
+        else if (s + 2 == s1) batch(Int<2>{});
+        else if (s + 1 == s1) batch(Int<1>{});
+#pragma unroll
+        for (int i = 0; i < 4; ++i) red[warp][i][lane] = acc[i];
+        __syncthreads();
+        if (threadIdx.x < 128) {
+            const int i = threadIdx.x >> 5, row = 2 * t4 + (i & 1), r = r0 + g + 8 * (i >> 1);      // (lane of threadIdx.x = lane)
+            if ((rows >> row & 1) && r < a.rank) {
+                float sum = 0.f;
+#pragma unroll
+                for (int k = 0; k < kLoraWarps; ++k) sum += red[k][i][lane];
+                a.v[((size_t)part * a.M + m0 + row) * a.rank + r] = a.scales ? sum * __ldg(a.scales + id) : sum;
+            }
+        }
+        __syncthreads();
+    }
 }
 
+// v[m][r .. r + 3], summed over the parts of K in their order
+__device__ __forceinline__ float4 lora_v4(const LoraArgs &a, int m, int r)
+{
+    float4 v = *reinterpret_cast<const float4 *>(a.v + (size_t)m * a.rank + r);
+#pragma unroll 4
+    for (int p = 1; p < a.k_parts; ++p) {
+        const float4 w = *reinterpret_cast<const float4 *>(a.v + ((size_t)p * a.M + m) * a.rank + r);
+        v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+    }
+    return v;
+}
 template <bool BF>
-__global__ void __launch_bounds__(256) lora_delta_kernel(const LoraArgs a, __half *__restrict__ delta)
+__device__ __forceinline__ uint32_t pack16(float a, float b)
+{
+    return (uint32_t)float_to_out16<BF>(a) | (uint32_t)float_to_out16<BF>(b) << 16;
+}
+
+// delta[m][n] = (v B^T)[m][n], 0 without an adapter.
+//
+// Decode batches, every row with an adapter of its own: a column of B has rank / 8 pieces of 16 bytes; neighbouring lanes read
+// neighbouring pieces, multiply them with their 8 values of v, which they keep, and add up.  A warp takes a row and kDeltaSteps times the
+// columns that its lanes read at once, all requested before the first is used.
+constexpr int kDeltaSteps = 4;
+template <bool BF>
+__global__ void __launch_bounds__(256, 4) lora_delta_rows_kernel(const LoraArgs a, __half *__restrict__ delta)
 {
     pdl_launch_dependents();
     pdl_wait();
-    const int n = blockIdx.x * 256 + threadIdx.x, m = blockIdx.y;
-    if (n < a.N) store_out16<BF>(delta + (size_t)m * a.N + n, lora_expand<BF>(a, m, n));
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    const int pieces = a.rank / 8, cols = 32 / pieces;      // (rank up to 256: at least one column)
+    const int m = blockIdx.y, n0 = kDeltaSteps * cols * (8 * blockIdx.x + warp), n1 = min(n0 + kDeltaSteps * cols, a.N);
+    if (n0 >= a.N) return;
+    const int id = __ldg(a.ids + m), c = lane / pieces, piece = lane - c * pieces;
+    __half *out = delta + (size_t)m * a.N;
+    if ((unsigned)id >= (unsigned)a.adapters) {
+        for (int n = n0 + lane; n < n1; n += 32) store_out16<BF>(out + n, 0.f);
+        return;
+    }
+    uint4 p[kDeltaSteps];
+    const uint4 *b = reinterpret_cast<const uint4 *>(a.b + ((size_t)id * a.N + n0) * a.rank) + lane;
+#pragma unroll
+    for (int k = 0; k < kDeltaSteps; ++k)
+        p[k] = c < cols && n0 + k * cols + c < n1 ? __ldg(b + k * (cols * pieces)) : make_uint4(0, 0, 0, 0);
+    float4 v0 = make_float4(0.f, 0.f, 0.f, 0.f), v1 = v0;
+    if (c < cols) {
+        v0 = lora_v4(a, m, 8 * piece);
+        v1 = lora_v4(a, m, 8 * piece + 4);
+    }
+#pragma unroll
+    for (int k = 0; k < kDeltaSteps; ++k) {
+        const float2 p0 = pair_to_float2<BF>(p[k].x), p1 = pair_to_float2<BF>(p[k].y), p2 = pair_to_float2<BF>(p[k].z), p3 = pair_to_float2<BF>(p[k].w);
+        float sum = p0.x * v0.x;
+        sum = fmaf(p0.y, v0.y, sum), sum = fmaf(p1.x, v0.z, sum), sum = fmaf(p1.y, v0.w, sum);
+        sum = fmaf(p2.x, v1.x, sum), sum = fmaf(p2.y, v1.y, sum), sum = fmaf(p3.x, v1.z, sum), sum = fmaf(p3.y, v1.w, sum);
+        float total = sum;
+        for (int l = 1; l < pieces; ++l) total += __shfl_down_sync(0xffffffffu, sum, l);
+        if (c < cols && n0 + k * cols + c < n1 && piece == 0) store_out16<BF>(out + n0 + k * cols + c, total);
+    }
 }
 
-// The product with W of up to 8 NT rows, 16 NU columns per CTA, the items along K shared by its warps, plus the expansion.
-template <int NT, int NU, int SUB, bool BF>
-__global__ void __launch_bounds__(kLoraThreads, NT == 1 ? 2 : 1)
+// Prompts, runs of rows with one adapter: kDeltaRows rows and 256 columns per CTA, MMAs with the rows' v as the 16-row operand, in two
+// 16-bit parts (v = hi + lo to 2^-22, 2^-16 in bfloat16: the product is as good as fp32's next to the 16 bits of delta) that the CTA
+// prepares in shared memory, and eight rows of B as the columns.
+constexpr int kDeltaRows = 32, kDeltaTiles = 4;      // tiles: eight columns each, of a warp
+template <bool BF>
+__global__ void __launch_bounds__(256, 2) lora_delta_runs_kernel(const LoraArgs a, __half *__restrict__ delta)
+{
+    extern __shared__ __align__(16) uint8_t smem[];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
+    const int n0 = 8 * kDeltaTiles * (8 * blockIdx.x + warp), m0 = kDeltaRows * blockIdx.y, count = min(kDeltaRows, a.M - m0);
+    const int width = (a.rank + 31) & ~31, pitch = 2 * width * 2 + 16;      // a row: hi, lo, 16 bytes against bank conflicts
+    int my_id = lane < count ? __ldg(a.ids + m0 + lane) : -1;               // (a row per lane)
+    if ((unsigned)my_id >= (unsigned)a.adapters) my_id = -1;
+    const uint32_t same = __match_any_sync(0xffffffffu, my_id);
+    uint32_t leads = __ballot_sync(0xffffffffu, my_id >= 0 && (same & ((1u << lane) - 1)) == 0);
+    auto load_b = [&](uint4 (&p)[kDeltaTiles], int id, int r) {
+#pragma unroll
+        for (int t = 0; t < kDeltaTiles; ++t)
+            p[t] = r < a.rank && n0 < a.N ? __ldg(reinterpret_cast<const uint4 *>(a.b + ((size_t)id * a.N + n0 + 8 * t + g) * a.rank + r)) : make_uint4(0, 0, 0, 0);
+    };
+    uint4 p[kDeltaTiles] = {};
+    if (leads) load_b(p, __shfl_sync(0xffffffffu, my_id, __ffs(leads) - 1), 8 * t4);      // on its way while v is prepared
+    for (int i = threadIdx.x; i < kDeltaRows * width / 4; i += 256) {
+        const int row = i / (width / 4), r = 4 * (i - row * (width / 4));
+        const float4 v = row < count && r < a.rank ? lora_v4(a, m0 + row, r) : make_float4(0.f, 0.f, 0.f, 0.f);
+        const uint2 h = make_uint2(pack16<BF>(v.x, v.y), pack16<BF>(v.z, v.w));
+        const float2 h0 = pair_to_float2<BF>(h.x), h1 = pair_to_float2<BF>(h.y);
+        uint8_t *at = smem + row * pitch + 2 * r;
+        *reinterpret_cast<uint2 *>(at) = h;
+        *reinterpret_cast<uint2 *>(at + 2 * width) = make_uint2(pack16<BF>(v.x - h0.x, v.y - h0.y), pack16<BF>(v.z - h1.x, v.w - h1.y));
+    }
+    __syncthreads();
+    if (n0 >= a.N) return;
+    float out[2][kDeltaTiles][4] = {};      // [16 rows][8 columns]: rows g and g + 8, columns 2 t4 and 2 t4 + 1
+    const uint32_t vs = smem_u32(smem) + g * pitch + 16 * t4;
+    for (bool first = true; leads; leads &= leads - 1, first = false) {
+        const int id = __shfl_sync(0xffffffffu, my_id, __ffs(leads) - 1);
+        const uint32_t rows = __ballot_sync(0xffffffffu, my_id == id);
+        float acc[2][kDeltaTiles][4] = {};
+        for (int r = 0; r < width; r += 32) {
+            if (!first || r) load_b(p, id, r + 8 * t4);
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {
+                    const uint4 u = lds128(vs + 16 * m * pitch + part * 2 * width + 2 * r), w = lds128(vs + (16 * m + 8) * pitch + part * 2 * width + 2 * r);
+#pragma unroll
+                    for (int t = 0; t < kDeltaTiles; ++t) {
+                        mma16<BF, false>(acc[m][t], u.x, w.x, u.y, w.y, register_pair(p[t].x, p[t].y));
+                        mma16<BF, false>(acc[m][t], u.z, w.z, u.w, w.w, register_pair(p[t].z, p[t].w));
+                    }
+                }
+        }
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int t = 0; t < kDeltaTiles; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (rows >> (16 * m + 8 * (i >> 1) + g) & 1) out[m][t][i] = acc[m][t][i];
+    }
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int row = 16 * m + 8 * half + g;
+            if (row >= count) continue;
+#pragma unroll
+            for (int t = 0; t < kDeltaTiles; ++t)
+                *reinterpret_cast<uint32_t *>(delta + (size_t)(m0 + row) * a.N + n0 + 8 * t + 2 * t4) = pack16<BF>(out[m][t][2 * half], out[m][t][2 * half + 1]);
+        }
+}
+
+// The product with W of up to 8 rows, plus the expansion.  The work is counted in pairs of units, 32 columns; a CTA takes a range of
+// neighbouring ones, in tiles of two where they are half a panel, else of one.  As in the routed-expert kernels the warps share a
+// tile's items along K, leave their sums and go on, and add up at the next tile's end.
+template <int SUB, bool BF>
+__global__ void __launch_bounds__(kLoraThreads, 2)
 lora_gemm_kernel(const LoraArgs a, const __half *x, const uint8_t *qweight, const uint8_t *scales, const uint8_t *qzeros,
                  const TiledTrailer *trailer, __half *y)
 {
     extern __shared__ __align__(16) uint8_t smem[];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
+    __shared__ __align__(8) uint64_t arrived[2];
+    __shared__ int s_ids[8];
+    constexpr int NU = SUB == 4 ? 2 : 4, kValues = 4 * NU;
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
+    const uint32_t bars = smem_u32(arrived);
+    if (threadIdx.x == 0) {
+        mbar_init(bars, kLoraWarps);
+        mbar_init(bars + 8, kLoraWarps);
+    }
     const uint32_t flags = __ldg(&trailer->flags);
-    const int G = a.K / kGroup, panel = blockIdx.x / (8 / NU), unit = blockIdx.x % (8 / NU) * NU;
-    const UnitPtrs ptrs = unit_ptrs<SUB>(qweight, scales, qzeros, panel, G, unit, lane);
-    const __half *rows[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) rows[t] = 8 * t + g < a.M ? x + (size_t)(8 * t + g) * a.K + 8 * t4 : nullptr;
+    const int v_pitch = a.rank + 4;
+    float *vs = reinterpret_cast<float *>(smem), *red = vs + 8 * v_pitch;      // [row][rank], [buffer][warp][value][lane]
+    // where ranges differ the longer ones come first: the last CTAs may have to wait for the shrink kernel's to leave their SMs
+    const int G = a.K / kGroup, each = a.N / 32 / gridDim.x, more = a.N / 32 - each * gridDim.x;
+    const int t0 = blockIdx.x * each + min((int)blockIdx.x, more), t1 = t0 + each + ((int)blockIdx.x < more ? 1 : 0);
+    auto width = [&](int pair) { return NU == 4 && (pair & 1) == 0 && pair + 1 < t1 ? 2 : 1; };
+    // x and the ids are older than the kernel before this one, which waited for them before it let this one in
+    if (threadIdx.x < 8) s_ids[threadIdx.x] = (int)threadIdx.x < a.M ? __ldg(a.ids + threadIdx.x) : -1;
+    __syncthreads();
     pdl_launch_dependents();
-    float acc[NU][NT][4] = {};
-    constexpr int D = 2;
-    DirectRegs<NT, NU, SUB> regs[D];
-    const int n = (G - warp + kLoraWarps - 1) / kLoraWarps;
-    // x is older than the kernel before this one, which waited for it before it let this one in
-#pragma unroll
-    for (int d = 0; d < D; ++d)
-        if (d < n) {
-            load_item_weights<NT, NU, 1, SUB>(regs[d], ptrs, warp + d * kLoraWarps);
-            load_item_rows<NT, NU, SUB>(regs[d], rows, warp + d * kLoraWarps);
-        }
-    for (int i = 0; i < n; i += D)
-#pragma unroll
-        for (int d = 0; d < D; ++d)
-            if (i + d < n) {
-                multiply_item<NT, NU, SUB, BF>(regs[d], flags & kFormatZerosMinusOne, acc);
-                if (i + d + D < n) {
-                    load_item_weights<NT, NU, 1, SUB>(regs[d], ptrs, warp + (i + d + D) * kLoraWarps);
-                    load_item_rows<NT, NU, SUB>(regs[d], rows, warp + (i + d + D) * kLoraWarps);
-                }
+    const __half *rows[1] = {x + (size_t)min(g, a.M - 1) * a.K + 8 * t4};
+    // the rows of B that the epilogue will want, on their way to L2
+    for (int i = threadIdx.x; i < a.M * (t1 - t0) * 32; i += kLoraThreads) {
+        const int id = s_ids[i % a.M];
+        if ((unsigned)id >= (unsigned)a.adapters) continue;
+        const __half *p = a.b + ((size_t)id * a.N + 32 * t0 + i / a.M) * a.rank;
+        for (int r = 0; r < a.rank; r += 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + r));
+    }
+    int l_pair = t0, l_next = t0, l_item = G, l_turn = warp - 1;
+    UnitPtrs ptrs{};
+    auto next = [&](DirectItem<1> &it) {
+        l_item += kLoraWarps;
+        while (l_item >= G) {
+            if (l_next >= t1) {
+                it.tag = -1;
+                return;
             }
+            l_pair = l_next;
+            l_next += width(l_pair);
+            l_item = ++l_turn & (kLoraWarps - 1);
+            ptrs = lane_ptrs<false, SUB>(unit_ptrs<SUB>(qweight, scales, qzeros, l_pair >> 2, G, 2 * (l_pair & 3)), lane);
+        }
+        set_item<1, SUB>(it, ptrs, rows, l_item);
+        it.flags = flags;
+        it.tag = l_pair;
+        it.pairs = l_next - l_pair;
+    };
     const bool layout_ok = (flags & kFormatGateUp) == 0 && ((flags & kFormatBf16) != 0) == BF;
     if (!layout_ok && threadIdx.x == 0) atomicMax(&g_device_status, (int)kStatusLayoutMismatch);
-    float *red = reinterpret_cast<float *>(smem);
+    float acc[NU][1][4] = {};
+    int pair = t0, left = t0, tiles = 0;      // the tile at hand, the one before it, how many came before
+    auto add_up = [&]() {
+        const int done = tiles - 1;
+        if (done == 0) {
+            // v is there, and y no longer in use by earlier kernels
+            pdl_wait();
+            for (int i = 4 * threadIdx.x; i < a.M * a.rank; i += 4 * kLoraThreads) {
+                const int m = i / a.rank, r = i - m * a.rank;
+                *reinterpret_cast<float4 *>(vs + m * v_pitch + r) = lora_v4(a, m, r);
+            }
+            __syncthreads();
+        }
+        if (!mbar_wait(bars + 8 * (done & 1), (done >> 1) & 1)) return;
+        const float *buf = red + (done & 1) * (kLoraWarps * kValues * 32);
+        for (int o = threadIdx.x; o < width(left) * 256; o += kLoraThreads) {
+            const int v = o >> 5, i = v & 3, m = 2 * t4 + (i & 1), n = 32 * left + 16 * (v >> 2) + g + 8 * (i >> 1);
+            if (m >= a.M || !layout_ok) continue;
+            float sum = 0.f;
 #pragma unroll
-    for (int u = 0; u < NU; ++u)
+            for (int w = 0; w < kLoraWarps; ++w) sum += buf[(w * kValues + v) * 32 + lane];
+            if (sum != sum) {      // the long way (see stream_items)
+                const UnitPtrs p = unit_ptrs<SUB>(qweight, scales, qzeros, n / kPanel, G, n % kPanel / 16);
+                sum = long_sum<BF>(p.w, p.s, p.z, SUB, n % 16, flags & kFormatZerosMinusOne, x + (size_t)m * a.K, G, false);
+            }
+            const int id = s_ids[m];
+            if ((unsigned)id < (unsigned)a.adapters) {
+                const uint4 *b = reinterpret_cast<const uint4 *>(a.b + ((size_t)id * a.N + n) * a.rank);
+                float part = 0.f;
+                for (int c = 0; c < a.rank / 8; ++c) {
+                    const uint4 p = __ldg(b + c);
+                    const float4 lo = *reinterpret_cast<const float4 *>(vs + m * v_pitch + 8 * c), hi = *reinterpret_cast<const float4 *>(vs + m * v_pitch + 8 * c + 4);
+                    const float2 p0 = pair_to_float2<BF>(p.x), p1 = pair_to_float2<BF>(p.y), p2 = pair_to_float2<BF>(p.z), p3 = pair_to_float2<BF>(p.w);
+                    part = fmaf(p0.x, lo.x, part), part = fmaf(p0.y, lo.y, part), part = fmaf(p1.x, lo.z, part), part = fmaf(p1.y, lo.w, part);
+                    part = fmaf(p2.x, hi.x, part), part = fmaf(p2.y, hi.y, part), part = fmaf(p3.x, hi.z, part), part = fmaf(p3.y, hi.w, part);
+                }
+                sum += part;
+            }
+            store_out16<BF>(y + (size_t)m * a.N + n, sum);
+        }
+    };
+    auto finish_tile = [&]() {
+        if (tiles) add_up();
+        float *buf = red + (tiles & 1) * (kLoraWarps * kValues * 32);
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int u = 0; u < NU; ++u)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) red[((warp * NU + u) * (4 * NT) + 4 * t + i) * 32 + lane] = acc[u][t][i];
-    __syncthreads();
-    pdl_wait();      // v; and y may still be in use by earlier kernels until here
-    for (int o = threadIdx.x; o < NU * NT * 4 * 32; o += kLoraThreads) {
-        const int v = o >> 5, u = v / (4 * NT), t = v % (4 * NT) / 4, i = v & 3;
-        const int m = 8 * t + 2 * t4 + (i & 1), col = panel * kPanel + 16 * (unit + u) + g + 8 * (i >> 1);
-        if (m >= a.M || !layout_ok) continue;
-        float sum = 0.f;
-#pragma unroll
-        for (int w = 0; w < kLoraWarps; ++w) sum += red[(w * (NU * NT * 4) + v) * 32 + lane];
-        store_out16<BF>(y + (size_t)m * a.N + col, sum + lora_expand<BF>(a, m, col));
-    }
+            for (int i = 0; i < 4; ++i) {
+                buf[(warp * kValues + 4 * u + i) * 32 + lane] = acc[u][0][i];
+                acc[u][0][i] = 0.f;
+            }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bars + 8 * (tiles & 1));
+        left = pair;
+        pair += width(pair);
+        ++tiles;
+    };
+    const uint32_t ring = smem_u32(red + 2 * kLoraWarps * kValues * 32) + warp * direct_ring_bytes<NU, SUB>(1);
+    stream_items<1, NU, false, SUB, BF, false>(ring, lane, a.one, acc, next, [&](int t) { while (pair < t) finish_tile(); });
+    while (pair < t1) finish_tile();
+    if (tiles) add_up();
+}
+
+// The parts of K that the shrink kernel sums apart: so many that a warp has one batch of steps - a second one costs a round trip to
+// memory, 64 rows of 64 adapters of 5120 x 32: 17 us with five parts, 22 with four - as long as the CTAs are not too many anyway.
+constexpr int kLoraMaxParts = 12;
+inline int lora_k_parts(int M, int K, int rank)
+{
+    const long long ctas = (long long)((M + 7) / 8) * ((rank + 15) / 16) * (M < 8 ? M : M <= kLoraDecodeRows ? 8 : 1);
+    const int steps = kLoraWarps * kLoraSteps, most = 1500 / ctas < 1 ? 1 : 1500 / ctas > kLoraMaxParts ? kLoraMaxParts : (int)(1500 / ctas);
+    const int parts = (K / 32 + steps - 1) / steps;
+    return parts < most ? parts : most;
 }
 
 // scratch: [x in the sorted order][v][expansion]
@@ -151,40 +416,48 @@ inline LoraScratch lora_scratch(int M, int N, int K, int rank, int act_order)
     LoraScratch l;
     l.x_perm = 0;
     l.v = act_order == 1 ? up((size_t)M * K * 2) : 0;
-    l.delta = l.v + up((size_t)M * rank * 4);
+    l.delta = l.v + up((size_t)lora_k_parts(M, K, rank) * M * rank * 4);
     l.total = l.delta + (M > kLoraDirectRows ? up((size_t)M * N * 2) : 0);
     return l;
 }
 
-int launch_lora_shrink(const LoraArgs &a, int bf16, cudaStream_t s)
+// perm, x_sorted: see the kernel; nullptr without
+int launch_lora_shrink(const LoraArgs &a, const int32_t *perm, __half *x_sorted, int bf16, cudaStream_t s)
 {
-    const dim3 grid((unsigned)((a.rank + kLoraWarps - 1) / kLoraWarps), (unsigned)a.M);
-    return bf16 ? launch_dependent(lora_shrink_kernel<true>, grid, kLoraThreads, 0, 1, s, a)
-                : launch_dependent(lora_shrink_kernel<false>, grid, kLoraThreads, 0, 1, s, a);
+    // decode batches: a CTA per adapter of eight rows; prompts: one CTA takes them in turn (mostly there is one)
+    const int apart = a.M < 8 ? a.M : a.M <= kLoraDecodeRows ? 8 : 1, ranks = (a.rank + 15) / 16;
+    const int per_row = (a.K / 2 + kLoraThreads - 1) / kLoraThreads, slices = perm ? (per_row + ranks - 1) / ranks : 0;
+    const dim3 grid((unsigned)((a.M + 7) / 8), (unsigned)ranks, (unsigned)(apart * a.k_parts + slices));
+    return bf16 ? launch_dependent(lora_shrink_kernel<true>, grid, kLoraThreads, 0, 1, s, a, apart, perm, x_sorted)
+                : launch_dependent(lora_shrink_kernel<false>, grid, kLoraThreads, 0, 1, s, a, apart, perm, x_sorted);
 }
 int launch_lora_delta(const LoraArgs &a, __half *delta, int bf16, cudaStream_t s)
 {
-    const dim3 grid((unsigned)((a.N + 255) / 256), (unsigned)a.M);
-    return bf16 ? launch_dependent(lora_delta_kernel<true>, grid, 256, 0, 1, s, a, delta)
-                : launch_dependent(lora_delta_kernel<false>, grid, 256, 0, 1, s, a, delta);
+    if (a.M <= kLoraDecodeRows) {
+        const int per_cta = 8 * kDeltaSteps * (32 / (a.rank / 8));
+        const dim3 grid((unsigned)((a.N + per_cta - 1) / per_cta), (unsigned)a.M);
+        return bf16 ? launch_dependent(lora_delta_rows_kernel<true>, grid, 256, 0, 1, s, a, delta)
+                    : launch_dependent(lora_delta_rows_kernel<false>, grid, 256, 0, 1, s, a, delta);
+    }
+    const dim3 grid((unsigned)((a.N + 255) / 256), (unsigned)((a.M + kDeltaRows - 1) / kDeltaRows));
+    const size_t smem = (size_t)kDeltaRows * (2 * ((a.rank + 31) & ~31) * 2 + 16);      // at most 33 KB
+    return bf16 ? launch_dependent(lora_delta_runs_kernel<true>, grid, 256, smem, 1, s, a, delta)
+                : launch_dependent(lora_delta_runs_kernel<false>, grid, 256, smem, 1, s, a, delta);
 }
 
-template <int NT, int SUB, bool BF>
-static int launch_lora_gemm_nt(const LoraArgs &a, const __half *x, const void *qweight, const void *scales, const void *qzeros,
-                               __half *y, cudaStream_t s)
-{
-    const TiledTrailer *trailer = reinterpret_cast<const TiledTrailer *>((const uint8_t *)qzeros + tiled_zero_bytes(a.N, a.K, kGroup / SUB));
-    constexpr int NU = NT;
-    const int smem = kLoraWarps * NU * NT * 4 * 32 * 4;
-    return launch_dependent(lora_gemm_kernel<NT, NU, SUB, BF>, dim3((unsigned)(a.N / (16 * NU))), kLoraThreads, (size_t)smem, 1, s, a, x,
-                            (const uint8_t *)qweight, (const uint8_t *)scales, (const uint8_t *)qzeros, trailer, y);
-}
 template <int SUB, bool BF>
 static int launch_lora_gemm_sub(const LoraArgs &a, const __half *x, const void *qweight, const void *scales, const void *qzeros,
                                 __half *y, cudaStream_t s)
 {
-    return a.M <= 8 ? launch_lora_gemm_nt<1, SUB, BF>(a, x, qweight, scales, qzeros, y, s)
-                    : launch_lora_gemm_nt<2, SUB, BF>(a, x, qweight, scales, qzeros, y, s);
+    const TiledTrailer *trailer = reinterpret_cast<const TiledTrailer *>((const uint8_t *)qzeros + tiled_zero_bytes(a.N, a.K, kGroup / SUB));
+    constexpr int NU = SUB == 4 ? 2 : 4;
+    const int smem = 8 * (a.rank + 4) * 4 + 2 * kLoraWarps * 4 * NU * 32 * 4 + direct_ring_bytes<NU, SUB>(kLoraWarps);
+    static int configured[64] = {};
+    const int st = ensure_direct_smem((const void *)lora_gemm_kernel<SUB, BF>, configured, smem, 2);
+    if (st) return st;
+    const int pairs = a.N / 32;
+    return launch_dependent(lora_gemm_kernel<SUB, BF>, dim3((unsigned)(pairs < 2 * a.sms ? pairs : 2 * a.sms)), kLoraThreads, (size_t)smem, 1, s,
+                            a, x, (const uint8_t *)qweight, (const uint8_t *)scales, (const uint8_t *)qzeros, trailer, y);
 }
 // x: in the row order of the tiled layer
 int launch_lora_gemm(const LoraArgs &a, const __half *x, const void *qweight, const void *scales, const void *qzeros, __half *y,

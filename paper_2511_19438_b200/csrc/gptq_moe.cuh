@@ -95,6 +95,7 @@ int launch_route(const void *logits, int type, int32_t *ids, float *weights, int
 // ------------------------------------------------------------------------------ the experts' MLP
 constexpr int kMoeMaxRows = 64;                 // tokens of one pass
 constexpr int kMoeWarps = 8, kMoeThreads = 32 * kMoeWarps;
+constexpr int kMoeCtasPerSm = 2;
 constexpr int kMoeMaxExperts = 1024, kMoeMaxTopK = 32;
 
 struct MoeArgs {
@@ -104,10 +105,12 @@ struct MoeArgs {
     const uint8_t *gu_w, *gu_z, *gu_s, *dn_w, *dn_z, *dn_s;
     size_t gu_w_bytes, gu_z_bytes, gu_s_bytes, dn_w_bytes, dn_z_bytes, dn_s_bytes;    // of one expert
     const int32_t *down_index;      // [E, F] or nullptr
-    __half *h;                // [M k, F]
+    __half *h;                // [M k, F], columns as direct_column has them
     const __half *residual;   // [M, K] or nullptr
     __half *y;                // [M, K]
     int M, k, E, K, F;
+    int sms;
+    uint32_t one;             // 1 (see prepare_rows)
     int x_by_slot;            // rows of x: slots instead of tokens
 };
 
@@ -115,33 +118,90 @@ struct MoeArgs {
 // into SEGMENTS of at most R, the rows that one sweep over the expert's weights serves.
 struct SlotPlan {
     float *weight;       // [P] by slot: the weights that a token gives its expert, summed
-    int *counts;         // [E] while it is built
+    int *counts;         // [E] while it is built: slots, then the first one's position
     short *key;          // [P] by slot: its expert, -1 where the slot is not used
     short *slot;         // [P] slots by expert
     short *rank;         // [P] by slot, while it is built
+    short *token;        // [P] by slot
     short *seg_begin;    // [segments + 1] into slot
     short *seg_expert;   // [segments]
 };
-__host__ __device__ constexpr int slot_plan_bytes(int P, int E) { return (4 * P + 4 * E + 12 * (P + 2) + 15) & ~15; }
+__host__ __device__ constexpr int slot_plan_room(int P) { return (P + 8) & ~7; }      // of an array by slot or segment, more than P
+__host__ __device__ constexpr int slot_plan_bytes(int P, int E) { return 14 * slot_plan_room(P) + ((4 * E + 15) & ~15); }
 __device__ __forceinline__ SlotPlan slot_plan_view(uint8_t *smem, int P, int E)
 {
+    const int room = slot_plan_room(P);
     SlotPlan p;
-    p.weight = reinterpret_cast<float *>(smem);
-    p.counts = reinterpret_cast<int *>(p.weight + P);
-    p.key = reinterpret_cast<short *>(p.counts + E);
-    p.slot = p.key + P + 2;
-    p.rank = p.slot + P + 2;
-    p.seg_begin = p.rank + P + 2;
-    p.seg_expert = p.seg_begin + P + 2;
+    p.key = reinterpret_cast<short *>(smem);
+    p.slot = p.key + room;
+    p.rank = p.slot + room;
+    p.token = p.rank;      // (once the ranks are done with)
+    p.seg_begin = p.rank + room;
+    p.seg_expert = p.seg_begin + room;
+    p.weight = reinterpret_cast<float *>(p.seg_expert + room);
+    p.counts = reinterpret_cast<int *>(p.weight + room);
     return p;
 }
 
 // By all threads of a block; returns the number of segments.  A slot whose expert a lower slot of the same token names already
 // adds its weight there.  `seg_expert` holds the raw ids until the segments are known.
-__device__ __forceinline__ int build_slot_plan(const MoeArgs &a, int R, const SlotPlan &p)
+constexpr int kSlotTableEntries = 4096;      // (8 KB of the room for sums and ring, not in use yet)
+__device__ __forceinline__ int build_slot_plan(const MoeArgs &a, int R, const SlotPlan &p, unsigned short *table)
 {
     __shared__ int s_segments;
     const int P = a.M * a.k, tid = threadIdx.x, lane = tid & 31;
+    if (P <= 32) {      // a slot per lane of one warp, experts in the order of their first slots (2.6 us on the way below, 1.1 so)
+        if (tid < 32) {
+            const int j = lane % a.k, id = lane < P ? __ldg(a.ids + lane) : -1;
+            float w = lane < P ? __ldg(a.weights + lane) : 0.f;
+            const bool named = (unsigned)id < (unsigned)a.E;
+            uint32_t same = __match_any_sync(0xffffffffu, named ? id : -1);
+            const uint32_t own = (a.k < 32 ? (1u << a.k) - 1 : 0xffffffffu) << (lane - j), before = (1u << lane) - 1;
+            const bool used = named && !(same & own & before);
+            if (__any_sync(0xffffffffu, named && !used)) {
+                const uint32_t more = used ? same & own : 0u;      // (this lane and later ones: the weights in the order of slots)
+                float sum = w;
+                for (int l = 0; l < 32; ++l) {
+                    const float v = __shfl_sync(0xffffffffu, w, l);
+                    if (l > lane && (more >> l & 1)) sum += v;
+                }
+                w = sum;
+            }
+            same &= __ballot_sync(0xffffffffu, used);
+            const int rank = __popc(same & before), c = __popc(same);
+            const bool leads = used && rank == 0;
+            int sum = leads ? c | (c + R - 1) / R << 16 : 0;
+            const int mine = sum;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v = __shfl_up_sync(0xffffffffu, sum, o);
+                if (lane >= o) sum += v;
+            }
+            const int total = __shfl_sync(0xffffffffu, sum, 31);
+            const int at = __shfl_sync(0xffffffffu, sum - mine, used ? __ffs(same) - 1 : 0);
+            if (lane < P) {
+                p.weight[lane] = w;
+                p.key[lane] = used ? (short)id : (short)-1;
+                p.token[lane] = (short)(lane / a.k);
+            }
+            if (used) {
+                p.slot[(at & 0xffff) + rank] = (short)lane;
+                if (rank % R == 0) {
+                    const int seg = (at >> 16) + rank / R;
+                    p.seg_expert[seg] = (short)id;
+                    p.seg_begin[seg] = (short)((at & 0xffff) + rank);
+                }
+            }
+            if (lane == 0) {
+                p.seg_begin[total >> 16] = (short)(total & 0xffff);
+                s_segments = total >> 16;
+            }
+        }
+        __syncthreads();
+        return s_segments;
+    }
+    // Otherwise the slots are taken 32 at a time: what a slot finds of its expert in its own 32, and how many there are in those before.
+    // The counts per 32 slots and expert stand in `table`, or, where that is too small, one warp takes the 32s in turn.
     short *raw = p.seg_expert;
     for (int s = tid; s < P; s += kMoeThreads) {
         const int e = __ldg(a.ids + s);
@@ -161,6 +221,69 @@ __device__ __forceinline__ int build_slot_plan(const MoeArgs &a, int R, const Sl
             p.weight[s] = sum;
         }
         p.key[s] = first ? (short)e : (short)-1;
+    }
+    const int chunks = (P + 31) / 32;
+    if (chunks * a.E <= kSlotTableEntries) {
+        __shared__ int s_sums[kMoeThreads / 32];
+        for (int i = tid; i < chunks * a.E; i += kMoeThreads) table[i] = 0;
+        __syncthreads();
+        const int warp = tid >> 5;
+        for (int c = warp; c < chunks; c += kMoeThreads / 32) {
+            const int s = 32 * c + lane, e = s < P ? p.key[s] : -1;
+            const uint32_t same = __match_any_sync(0xffffffffu, e);
+            const int before = __popc(same & ((1u << lane) - 1));
+            if (e >= 0) {
+                p.rank[s] = (short)before;
+                if (before == 0) table[c * a.E + e] = (unsigned short)__popc(same);
+            }
+        }
+        __syncthreads();
+        // a thread per expert (of neighbouring ones, where there are more): the 32s' counts become positions behind its first slot
+        const int per = (a.E + kMoeThreads - 1) / kMoeThreads, e0 = min(tid * per, a.E), e1 = min(e0 + per, a.E);
+        int sum = 0;
+        for (int e = e0; e < e1; ++e) {
+            int n = 0;
+            for (int c = 0; c < chunks; ++c) {
+                const int here = table[c * a.E + e];
+                table[c * a.E + e] = (unsigned short)n;
+                n += here;
+            }
+            p.counts[e] = n;
+            sum += n | (n + R - 1) / R << 16;
+        }
+        const int mine = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += v;
+        }
+        if (lane == 31) s_sums[warp] = sum;
+        __syncthreads();
+        int total = 0, at = sum - mine;
+#pragma unroll
+        for (int w = 0; w < kMoeThreads / 32; ++w) {
+            if (w < warp) at += s_sums[w];
+            total += s_sums[w];
+        }
+        int pos = at & 0xffff, seg = at >> 16;
+        for (int e = e0; e < e1; ++e) {
+            const int n = p.counts[e];
+            p.counts[e] = pos;
+            for (int i = 0; i < n; i += R) {
+                p.seg_expert[seg] = (short)e;
+                p.seg_begin[seg++] = (short)(pos + i);
+            }
+            pos += n;
+        }
+        if (tid == 0) p.seg_begin[total >> 16] = (short)(total & 0xffff);
+        __syncthreads();
+        for (int s = tid; s < P; s += kMoeThreads) {
+            const int e = p.key[s];
+            if (e >= 0) p.slot[p.counts[e] + table[(s >> 5) * a.E + e] + p.rank[s]] = (short)s;
+            p.token[s] = (short)(s / a.k);
+        }
+        __syncthreads();
+        return total >> 16;
     }
     __syncthreads();
     if (tid < 32) {
@@ -204,246 +327,267 @@ __device__ __forceinline__ int build_slot_plan(const MoeArgs &a, int R, const Sl
         }
     }
     __syncthreads();
-    for (int s = tid; s < P; s += kMoeThreads)
+    for (int s = tid; s < P; s += kMoeThreads) {
         if (p.key[s] >= 0) p.slot[p.counts[p.key[s]] + p.rank[s]] = (short)s;
+        p.token[s] = (short)(s / a.k);
+    }
     __syncthreads();
     return s_segments;
 }
 
-// Kernel 1: h[slot] = silu(gate) * up.  A TILE is a segment and 16 gate columns with their 16 up columns; a CTA works through a
-// range of neighbouring tiles (their rows of x stay in L1).  The warps share a tile's items along K and meet in shared memory at its
-// end; their loads run on into the next tile.
-template <int NT, int SUB, bool BF>
-__global__ void __launch_bounds__(kMoeThreads, NT <= 2 ? 2 : 1) moe_gate_up_kernel(const MoeArgs a)
+// Kernel 1: h[slot] = silu(gate) * up.  The work is counted in units of a segment and 16 gate columns (with their 16 up columns); a
+// CTA takes a range of neighbouring units, in tiles of two where they are a pair of the panel, else of one.  The warps share a
+// tile's items along K; at its end each leaves its sums in shared memory, goes on with the next tile, and adds up its part of them at
+// the next tile's end, when all have long arrived.
+template <int NT, int NU, int SUB, bool BF>
+__global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_gate_up_kernel(const MoeArgs a)
 {
     extern __shared__ __align__(16) uint8_t smem[];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
+    constexpr int kValues = 4 * NU * NT;
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
     const SlotPlan plan = slot_plan_view(smem, a.M * a.k, a.E);
     float *red = reinterpret_cast<float *>(smem + slot_plan_bytes(a.M * a.k, a.E));
+    __shared__ __align__(8) uint64_t arrived[2];
+    const uint32_t bars = smem_u32(arrived);
+    if (threadIdx.x == 0) {
+        mbar_init(bars, kMoeWarps);
+        mbar_init(bars + 8, kMoeWarps);
+    }
     pdl_wait();
     pdl_launch_dependents();
-    const int segments = build_slot_plan(a, 8 * NT, plan);
+    const int segments = build_slot_plan(a, 8 * NT, plan, reinterpret_cast<unsigned short *>(red));
     const int G = a.K / kGroup, per_seg = a.F / 16, T = segments * per_seg;
-    const int t0 = (int)((long long)blockIdx.x * T / gridDim.x), t1 = (int)((long long)(blockIdx.x + 1) * T / gridDim.x);
+    // the CTAs of an SM (which they are given out to in turn) take neighbouring ranges: the same rows of x
+    int cta = blockIdx.x;
+    if (gridDim.x % a.sms == 0) cta = cta % a.sms * (gridDim.x / a.sms) + cta / a.sms;
+    const int t0 = share_begin(T, gridDim.x, cta), t1 = share_begin(T, gridDim.x, cta + 1);
+    auto width = [&](int unit) { return NU == 4 && (unit & 1) == 0 && unit + 1 < t1 ? 2 : 1; };      // (per_seg is even)
 
-    // ---- loads: tile l_tile, item l_item; a warp starts at another item in every tile, so that all get their share where the
-    // items are no multiple of the warps
-    int l_tile = t0 - 1, l_item = G, l_seg = 0, l_col = 0;
+    // ---- what comes next: the tile at unit l_unit, item l_item; a warp starts at another item in every tile, so that all get their
+    // share where the items are no multiple of the warps
+    int l_unit = t0, l_next = t0, l_item = G, l_seg = 0, l_col = 0, l_turn = warp - 1;
     uint32_t l_flags = 0;
     UnitPtrs ptrs{};
     const __half *rows[NT];
-    auto enter_segment = [&]() {
-        const int first = plan.seg_begin[l_seg], count = plan.seg_begin[l_seg + 1] - first;
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            rows[t] = nullptr;
-            if (8 * t + g < count) {
-                const int s = plan.slot[first + 8 * t + g];
-                rows[t] = a.x + (size_t)(a.x_by_slot ? s : s / a.k) * a.K + 8 * t4;
-            }
-        }
+    auto row_of = [&](int s) { return a.x + (size_t)(a.x_by_slot ? s : plan.token[s]) * a.K; };
+    auto up_flags = [&](int e) {
+        return __ldg(&reinterpret_cast<const TiledTrailer *>(a.gu_z + (size_t)(e + 1) * a.gu_z_bytes - kTrailerBytes)->flags);
     };
-    auto advance = [&]() {      // to the next item that is this warp's; l_tile = t1: none
+    auto next = [&](DirectItem<NT> &it) {
         l_item += kMoeWarps;
         while (l_item >= G) {
-            if (++l_tile >= t1) return;
-            l_item = (warp + l_tile) & (kMoeWarps - 1);
-            const bool start = l_tile == t0;
-            if (start || ++l_col == per_seg) {
-                l_seg = start ? l_tile / per_seg : l_seg + 1;
-                l_col = start ? l_tile - l_seg * per_seg : 0;
-                enter_segment();
+            if (l_next >= t1) {
+                it.tag = -1;
+                return;
+            }
+            const bool start = l_next == t0;
+            l_col += l_next - l_unit;
+            l_unit = l_next;
+            l_next += width(l_unit);
+            l_item = ++l_turn & (kMoeWarps - 1);
+            if (start || l_col == per_seg) {
+                l_seg = start ? l_unit / per_seg : l_seg + 1;
+                l_col = start ? l_unit - l_seg * per_seg : 0;
+                const int first = plan.seg_begin[l_seg], count = plan.seg_begin[l_seg + 1] - first;
+#pragma unroll
+                for (int t = 0; t < NT; ++t) rows[t] = row_of(plan.slot[first + (8 * t + g < count ? 8 * t + g : 0)]) + 8 * t4;
+                l_flags = up_flags(plan.seg_expert[l_seg]);
             }
             const int e = plan.seg_expert[l_seg];
-            const uint8_t *zeros = a.gu_z + e * a.gu_z_bytes;
-            l_flags = __ldg(&reinterpret_cast<const TiledTrailer *>(zeros + a.gu_z_bytes - kTrailerBytes)->flags);
-            ptrs = unit_ptrs<SUB>(a.gu_w + e * a.gu_w_bytes, a.gu_s + e * a.gu_s_bytes, zeros, l_col >> 2, G, l_col & 3, lane);
+            ptrs = lane_ptrs<true, SUB>(unit_ptrs<SUB>(a.gu_w + e * a.gu_w_bytes, a.gu_s + e * a.gu_s_bytes, a.gu_z + e * a.gu_z_bytes, l_col >> 2, G, l_col & 3), lane);
         }
-    };
-    constexpr int D = NT == 1 ? 2 : 1;
-    DirectRegs<NT, 2, SUB> regs[D];
-    uint32_t flags[D] = {};
-    int tile_of[D];
-    auto load = [&](int d) {
-        advance();
-        tile_of[d] = l_tile;
-        if (l_tile < t1) {
-            load_item_weights<NT, 2, 4, SUB>(regs[d], ptrs, l_item);
-            load_item_rows<NT, 2, SUB>(regs[d], rows, l_item);
-            flags[d] = l_flags;
-        }
+        set_item<NT, SUB>(it, ptrs, rows, l_item);
+        it.flags = l_flags;
+        it.tag = l_unit;
+        it.pairs = l_next - l_unit;
     };
 
-    // ---- arithmetic
-    float acc[2][NT][4] = {};
-    int tile = t0;
-    auto finish_tile = [&]() {      // sums over the warps, in their order: [buffer][warp][value][lane]
-        float *buf = red + (tile & 1) * (kMoeWarps * 8 * NT * 32);
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    buf[(warp * (8 * NT) + (u * NT + t) * 4 + i) * 32 + lane] = acc[u][t][i];
-                    acc[u][t][i] = 0.f;
-                }
-        __syncthreads();
-        const int seg = tile / per_seg, c16 = tile - seg * per_seg;
+    // ---- the end of a tile
+    float acc[NU][NT][4] = {};
+    int unit = t0, left = t0, tiles = 0;      // the tile at hand, the one before it, how many came before
+    bool saw_nan = false;
+    auto add_up = [&]() {      // the sums of the tile at `left` over the warps, in their order
+        const int done = tiles - 1;
+        if (!mbar_wait(bars + 8 * (done & 1), (done >> 1) & 1)) return;
+        const int seg = left / per_seg, c0 = (left - seg * per_seg) * 16;
         const int first = plan.seg_begin[seg], count = plan.seg_begin[seg + 1] - first;
-        for (int o = threadIdx.x; o < NT * 4 * 32; o += kMoeThreads) {
-            const int v = o >> 5, t = v >> 2, i = v & 3;            // (lane of o = lane: the block is a multiple of a warp)
-            const int r = 8 * t + 2 * t4 + (i & 1);
+        const float *buf = red + (done & 1) * (kMoeWarps * kValues * 32);
+        for (int o = threadIdx.x; o < width(left) * (4 * NT * 32); o += kMoeThreads) {
+            const int v = o >> 5, p = v / (4 * NT), t = v / 4 % NT, i = v & 3;            // (lane of o = lane: the block is a multiple of a warp)
+            const int r = 8 * t + 2 * t4 + (i & 1), at = (8 * NT * p + 4 * t + i) * 32 + lane;
             if (r >= count) continue;
             float gate = 0.f, up = 0.f;
 #pragma unroll
             for (int w = 0; w < kMoeWarps; ++w) {
-                gate += buf[(w * (8 * NT) + v) * 32 + lane];
-                up += buf[(w * (8 * NT) + 4 * NT + v) * 32 + lane];
+                gate += buf[w * (kValues * 32) + at];
+                up += buf[w * (kValues * 32) + 4 * NT * 32 + at];
             }
-            int col = 16 * c16 + g + 8 * (i >> 1);
+            saw_nan |= gate != gate || up != up;
+            int col = c0 + 16 * p + g + 8 * (i >> 1);
             if (a.down_index) col = __ldg(a.down_index + (size_t)plan.seg_expert[seg] * a.F + col);
-            store_out16<BF>(a.h + (size_t)plan.slot[first + r] * a.F + col, silu_mul(gate, up));
+            store_out16<BF>(a.h + (size_t)plan.slot[first + r] * a.F + direct_column<BF>(col), silu_mul(gate, up));
         }
-        ++tile;
     };
+    auto finish_tile = [&]() {
+        // (no warp still reads this buffer: all have left their sums of the tile before this one, after adding up the one before that)
+        if (tiles) add_up();
+        float *buf = red + (tiles & 1) * (kMoeWarps * kValues * 32);      // [warp][value][lane]
 #pragma unroll
-    for (int d = 0; d < D; ++d) load(d);
-    for (bool more = true; more;) {
+        for (int u = 0; u < NU; ++u)
 #pragma unroll
-        for (int d = 0; d < D; ++d) {
-            while (tile < tile_of[d] && tile < t1) finish_tile();
-            if (tile_of[d] >= t1) { more = false; break; }
-            multiply_item<NT, 2, SUB, BF>(regs[d], flags[d] & kFormatZerosMinusOne, acc);
-            load(d);
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    buf[(warp * kValues + (u * NT + t) * 4 + i) * 32 + lane] = acc[u][t][i];
+                    acc[u][t][i] = 0.f;
+                }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bars + 8 * (tiles & 1));
+        left = unit;
+        unit += width(unit);
+        ++tiles;
+    };
+    const uint32_t ring = smem_u32(red + 2 * kMoeWarps * kValues * 32) + warp * direct_ring_bytes<NU, SUB>(1);
+    stream_items<NT, NU, true, SUB, BF, false>(ring, lane, a.one, acc, next, [&](int t) { while (unit < t) finish_tile(); });
+    while (unit < t1) finish_tile();
+    if (tiles) add_up();
+    if (!saw_nan) return;
+    // a thread goes over its outputs again and forms those that are NaN the long way (see stream_items)
+    for (unit = t0; unit < t1; unit += width(unit)) {
+        const int seg = unit / per_seg, c0 = (unit - seg * per_seg) * 16, e = plan.seg_expert[seg];
+        const int first = plan.seg_begin[seg], count = plan.seg_begin[seg + 1] - first;
+        const uint8_t *zeros = a.gu_z + e * a.gu_z_bytes;
+        const uint32_t z_add = up_flags(e) & kFormatZerosMinusOne;
+        for (int o = threadIdx.x; o < width(unit) * (4 * NT * 32); o += kMoeThreads) {
+            const int v = o >> 5, r = 8 * (v / 4 % NT) + 2 * t4 + (v & 1), c = g + 8 * ((v >> 1) & 1);
+            if (r >= count) continue;
+            const int s = plan.slot[first + r], col = c0 + 16 * (v / (4 * NT)) + c;
+            __half *at = a.h + (size_t)s * a.F + direct_column<BF>(a.down_index ? __ldg(a.down_index + (size_t)e * a.F + col) : col);
+            const float now = out16_to_float<BF>(*at);
+            if (now == now) continue;
+            float sum[2];
+#pragma unroll 1
+            for (int half = 0; half < 2; ++half) {
+                const UnitPtrs p = unit_ptrs<SUB>(a.gu_w + e * a.gu_w_bytes, a.gu_s + e * a.gu_s_bytes, zeros, col / 64, G, col % 64 / 16 + 4 * half);
+                sum[half] = long_sum<BF>(p.w, p.s, p.z, SUB, c, z_add, row_of(s), G, false);
+            }
+            store_out16<BF>(at, silu_mul(sum[0], sum[1]));
         }
     }
 }
 
-// Kernel 2: y = residual + sum over a token's experts of weight * (h Wd).  A cluster of S CTAs takes 32 columns of y; the items
-// of all segments, one behind the other, are shared out evenly over its 8 S warps.  A warp that reaches the end of a segment (or
-// of its share) adds its sums, weighted, to its own [token][32] tile in shared memory; the tiles are summed in the order of warps
-// and ranks, so results are reproducible.
-constexpr int kDownCols = 32;
-template <int NT, int SUB, bool BF>
-__global__ void __launch_bounds__(kMoeThreads, NT <= 2 ? 2 : 1) moe_down_kernel(const MoeArgs a, int S)
+// Kernel 2: y = residual + sum over a token's experts of weight * (h Wd).  A cluster of S CTAs takes 16 NU columns of y; the items
+// of all segments, one behind the other, are shared out evenly over its CTAs.  A CTA's part of a segment is what a tile is in
+// kernel 1; what its warps leave of it is added up, weighted, in a [token][column] tile in shared memory, part after part, and
+// the CTAs' tiles in the order of ranks: the order of all sums is fixed.
+template <int NT, int NU, int SUB, bool BF>
+__global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_down_kernel(const MoeArgs a, int S)
 {
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ int s_bad;
-    constexpr int NU = kDownCols / 16;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
+    __shared__ __align__(8) uint64_t arrived[2];
+    constexpr int kCols = 16 * NU, kValues = 4 * NU * NT, R = 8 * NT;
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
     const int tile = blockIdx.x / S, rank = blockIdx.x - tile * S;
     const int G = a.F / kGroup, panel = tile / (8 / NU), unit = tile % (8 / NU) * NU;
+    const uint32_t bars = smem_u32(arrived);
     pdl_launch_dependents();
-    // ids and weights are older than the kernel before this one, which waited for them before it let this one in
     const SlotPlan plan = slot_plan_view(smem, a.M * a.k, a.E);
-    float *tiles = reinterpret_cast<float *>(smem + slot_plan_bytes(a.M * a.k, a.E));
-    const int cells = a.M * kDownCols;
-    float *mine = tiles + warp * cells;
-    for (int i = lane; i < cells; i += 32) mine[i] = 0.f;
-    if (threadIdx.x == 0) s_bad = 0;
-    const int segments = build_slot_plan(a, 8 * NT, plan);
-    const int W = kMoeWarps * S, wi = rank * kMoeWarps + warp;
-    const int U = segments * G, j0 = (int)((long long)wi * U / W), j1 = (int)((long long)(wi + 1) * U / W), n = j1 - j0;
+    const int cells = a.M * kCols;
+    float *ysum = reinterpret_cast<float *>(smem + slot_plan_bytes(a.M * a.k, a.E));      // [token][column]
+    float *recv = ysum + cells;                              // with S > 1: [rank][cell of this CTA's share]
+    float *red = recv + (S > 1 ? cells : 0);
+    for (int i = threadIdx.x; i < cells; i += kMoeThreads) ysum[i] = 0.f;
+    if (threadIdx.x == 0) {
+        s_bad = 0;
+        mbar_init(bars, kMoeWarps);
+        mbar_init(bars + 8, kMoeWarps);
+    }
+    // ids and weights are older than the kernel before this one, which waited for them before it let this one in
+    const int segments = build_slot_plan(a, R, plan, reinterpret_cast<unsigned short *>(red));
+    if (S > 1) cluster_arrive_release();      // "this CTA has begun": waited for before anything is sent
+    const int U = segments * G, u0 = share_begin(U, S, rank), u1 = share_begin(U, S, rank + 1);
+    const int seg0 = u0 / G, parts = u1 > u0 ? (u1 - 1) / G - seg0 + 1 : 0;
 
-    // what is loaded next
-    int l_seg = 0, l_item = 0;
-    UnitPtrs ptrs{};
+    // ---- what comes next: part l_part (segment seg0 + l_part), item l_item
+    int l_part = -1, l_item = G, l_end = 0;
     uint32_t l_flags = 0;
+    UnitPtrs ptrs{};
     const __half *rows[NT];
-    auto enter_segment = [&]() {
-        const int e = plan.seg_expert[l_seg], first = plan.seg_begin[l_seg], count = plan.seg_begin[l_seg + 1] - first;
-        const uint8_t *zeros = a.dn_z + e * a.dn_z_bytes;
-        l_flags = __ldg(&reinterpret_cast<const TiledTrailer *>(zeros + a.dn_z_bytes - kTrailerBytes)->flags);
-        ptrs = unit_ptrs<SUB>(a.dn_w + e * a.dn_w_bytes, a.dn_s + e * a.dn_s_bytes, zeros, panel, G, unit, lane);
+    auto trailer_flags = [](const uint8_t *zeros, size_t bytes, int e) {
+        return __ldg(&reinterpret_cast<const TiledTrailer *>(zeros + (size_t)(e + 1) * bytes - kTrailerBytes)->flags);
+    };
+    auto next = [&](DirectItem<NT> &it) {
+        l_item += kMoeWarps;
+        while (l_item >= l_end) {
+            if (++l_part >= parts) {
+                l_end = -1;
+                it.tag = -1;
+                return;
+            }
+            const int seg = seg0 + l_part, e = plan.seg_expert[seg], first = plan.seg_begin[seg], count = plan.seg_begin[seg + 1] - first;
+            l_item = max(u0 - seg * G, 0) + ((warp + l_part) & (kMoeWarps - 1));
+            l_end = min(u1 - seg * G, G);
+            l_flags = trailer_flags(a.dn_z, a.dn_z_bytes, e);
+            ptrs = lane_ptrs<false, SUB>(unit_ptrs<SUB>(a.dn_w + e * a.dn_w_bytes, a.dn_s + e * a.dn_s_bytes, a.dn_z + e * a.dn_z_bytes, panel, G, unit), lane);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) rows[t] = 8 * t + g < count ? a.h + (size_t)plan.slot[first + 8 * t + g] * a.F + 8 * t4 : nullptr;
-    };
-    constexpr int D = NT == 1 ? 2 : 1;
-    DirectRegs<NT, NU, SUB> regs[D];
-    uint32_t flags[D] = {};
-    int seg_of[D], item_of[D];
-    auto load_weights = [&](int d) {
-        load_item_weights<NT, NU, 1, SUB>(regs[d], ptrs, l_item);
-        flags[d] = l_flags;
-        seg_of[d] = l_seg;
-        item_of[d] = l_item;
-    };
-    auto next = [&]() {
-        if (++l_item == G) {
-            l_item = 0;
-            if (++l_seg < segments) enter_segment();
+            for (int t = 0; t < NT; ++t) rows[t] = a.h + (size_t)plan.slot[first + (8 * t + g < count ? 8 * t + g : 0)] * a.F + 8 * t4;
         }
+        set_item<NT, SUB>(it, ptrs, rows, l_item);
+        it.flags = l_flags;
+        it.tag = l_part;
+        it.pairs = NU / 2;
     };
     // A layer of the wrong format anywhere: nothing is stored.  Every CTA looks at all experts in use, so that they agree; the
     // trailers are asked for here and looked at behind the main loop.
     uint32_t up_flags = kFormatGateUp | (BF ? kFormatBf16 : 0u), down_flags = BF ? kFormatBf16 : 0u;
-    auto trailer_flags = [](const uint8_t *zeros, size_t bytes, int e) {
-        return __ldg(&reinterpret_cast<const TiledTrailer *>(zeros + (size_t)(e + 1) * bytes - kTrailerBytes)->flags);
-    };
     if ((int)threadIdx.x < segments) {
         up_flags = trailer_flags(a.gu_z, a.gu_z_bytes, plan.seg_expert[threadIdx.x]);
         down_flags = trailer_flags(a.dn_z, a.dn_z_bytes, plan.seg_expert[threadIdx.x]);
     }
-    // weights never depend on the kernel before this one, h does
-    if (n > 0) {
-        l_seg = j0 / G;
-        l_item = j0 - l_seg * G;
-        enter_segment();
-        load_weights(0);
-    }
-    pdl_wait();
-    if (n > 0) {
-        load_item_rows<NT, NU, SUB>(regs[0], rows, l_item);
-        next();
-#pragma unroll
-        for (int d = 1; d < D; ++d)
-            if (d < n) {
-                load_weights(d);
-                load_item_rows<NT, NU, SUB>(regs[d], rows, l_item);
-                next();
-            }
-    }
+
+    // ---- the end of a part (see kernel 1)
     float acc[NU][NT][4] = {};
-    for (int i = 0; i < n; i += D)
+    int now = 0;
+    auto add_up = [&](int done) {
+        if (!mbar_wait(bars + 8 * (done & 1), (done >> 1) & 1)) return;
+        const int first = plan.seg_begin[seg0 + done], count = plan.seg_begin[seg0 + done + 1] - first;
+        const float *buf = red + (done & 1) * (kMoeWarps * kValues * 32);
 #pragma unroll
-        for (int d = 0; d < D; ++d)
-            if (i + d < n) {
-                const int seg = seg_of[d];
-                const bool flush = item_of[d] == G - 1 || i + d == n - 1;
-                multiply_item<NT, NU, SUB, BF>(regs[d], flags[d] & kFormatZerosMinusOne, acc);
-                if (i + d + D < n) {
-                    load_weights(d);
-                    load_item_rows<NT, NU, SUB>(regs[d], rows, l_item);
-                    next();
+        for (int o = threadIdx.x; o < kValues * 32; o += kMoeThreads) {
+            const int v = o >> 5, u = v / (4 * NT), t = v / 4 % NT, i = v & 3;
+            const int r = 8 * t + 2 * t4 + (i & 1);
+            if (r >= count) continue;
+            float sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < kMoeWarps; ++w) sum += buf[(w * kValues + v) * 32 + lane];
+            const int s = plan.slot[first + r];
+            float *cell = ysum + plan.token[s] * kCols + 16 * u + g + 8 * (i >> 1);
+            *cell = fmaf(plan.weight[s], sum, *cell);
+        }
+    };
+    auto finish_part = [&]() {
+        if (now) add_up(now - 1);
+        float *buf = red + (now & 1) * (kMoeWarps * kValues * 32);      // [warp][value][lane]
+#pragma unroll
+        for (int u = 0; u < NU; ++u)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    buf[(warp * kValues + (u * NT + t) * 4 + i) * 32 + lane] = acc[u][t][i];
+                    acc[u][t][i] = 0.f;
                 }
-                if (flush) {
-                    const int first = plan.seg_begin[seg], count = plan.seg_begin[seg + 1] - first;
-#pragma unroll
-                    for (int t = 0; t < NT; ++t)
-#pragma unroll
-                        for (int odd = 0; odd < 2; ++odd) {
-                            const int r = 8 * t + 2 * t4 + odd;
-                            if (r < count) {
-                                const int s = plan.slot[first + r];
-                                const float w = plan.weight[s];
-                                float *cell = mine + (s / a.k) * kDownCols + g;
-#pragma unroll
-                                for (int u = 0; u < NU; ++u) {
-                                    cell[16 * u] = fmaf(w, acc[u][t][odd], cell[16 * u]);
-                                    cell[16 * u + 8] = fmaf(w, acc[u][t][2 + odd], cell[16 * u + 8]);
-                                }
-                            }
-                        }
-#pragma unroll
-                    for (int u = 0; u < NU; ++u)
-#pragma unroll
-                        for (int t = 0; t < NT; ++t)
-#pragma unroll
-                            for (int v = 0; v < 4; ++v) acc[u][t][v] = 0.f;
-                    __syncwarp();
-                }
-            }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bars + 8 * (now & 1));
+        ++now;
+    };
+    pdl_wait();
+    const uint32_t ring = smem_u32(red + 2 * kMoeWarps * kValues * 32) + warp * direct_ring_bytes<NU, SUB>(1);
+    stream_items<NT, NU, false, SUB, BF, true>(ring, lane, a.one, acc, next, [&](int p) { while (now < p) finish_part(); });
+    while (now < parts) finish_part();
+    if (parts) add_up(parts - 1);
+
     auto fits = [](uint32_t up, uint32_t down) {
         return (up & (kFormatGateUp | kFormatBf16)) == (kFormatGateUp | (BF ? kFormatBf16 : 0u)) &&
                (down & (kFormatGateUp | kFormatBf16)) == (BF ? kFormatBf16 : 0u);
@@ -459,40 +603,46 @@ __global__ void __launch_bounds__(kMoeThreads, NT <= 2 ? 2 : 1) moe_down_kernel(
     }
     __syncthreads();
     const bool ok = s_bad == 0;
-    for (int o = threadIdx.x; o < cells; o += kMoeThreads) {
-        float v = tiles[o];
-#pragma unroll
-        for (int w = 1; w < kMoeWarps; ++w) v += tiles[w * cells + o];
-        tiles[o] = v;
-    }
-    auto store = [&](int o, float v) {
-        const size_t at = (size_t)(o / kDownCols) * a.K + panel * kPanel + 16 * unit + o % kDownCols;
-        if (a.residual) v += out16_to_float<BF>(a.residual[at]);
-        store_out16<BF>(a.y + at, v);
+    auto place = [&](int o) { return (size_t)(o / kCols) * a.K + panel * kPanel + 16 * unit + o % kCols; };
+    auto store = [&](int o, float v, float residual) {
+        const int m = o / kCols, c = o % kCols;
+        if (v != v) {      // the long way (see stream_items)
+            v = 0.f;
+#pragma unroll 1
+            for (int s = m * a.k; s < (m + 1) * a.k; ++s) {
+                const int e = plan.key[s];
+                if (e < 0) continue;
+                const UnitPtrs p = unit_ptrs<SUB>(a.dn_w + e * a.dn_w_bytes, a.dn_s + e * a.dn_s_bytes, a.dn_z + e * a.dn_z_bytes, panel, G, unit + c / 16);
+                v = fmaf(plan.weight[s], long_sum<BF>(p.w, p.s, p.z, SUB, c % 16, trailer_flags(a.dn_z, a.dn_z_bytes, e) & kFormatZerosMinusOne,
+                                                      a.h + (size_t)s * a.F, G, true), v);
+            }
+        }
+        store_out16<BF>(a.y + place(o), v + residual);
     };
     if (S == 1) {
-        // (a cell is stored by the thread that summed it)
         if (ok)
-            for (int o = threadIdx.x; o < cells; o += kMoeThreads) store(o, tiles[o]);
+            for (int o = threadIdx.x; o < cells; o += kMoeThreads) store(o, ysum[o], a.residual ? out16_to_float<BF>(a.residual[place(o)]) : 0.f);
         return;
     }
-    __syncthreads();
-    cluster_arrive_release();
+    // each CTA finishes a share of the cells: it gets all CTAs' sums of them
+    const int share = cells / S, from = rank * share;
     cluster_wait_acquire();
-    if (ok) {
-        const uint32_t base = smem_u32(tiles);
-        for (int o = cells * rank / S + threadIdx.x; o < cells * (rank + 1) / S; o += kMoeThreads) {
-            float v = 0.f;
-            for (int q = 0; q < S; ++q) {
-                float part;
-                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(part) : "r"(map_to_cluster_rank(base + 4u * o, (uint32_t)q)) : "memory");
-                v += part;
-            }
-            store(o, v);
-        }
+    for (int q = 0; q < S; ++q) {
+        const uint32_t to = map_to_cluster_rank(smem_u32(recv + rank * share), (uint32_t)q);
+        for (int i = threadIdx.x; i < share; i += kMoeThreads)
+            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + 4u * i), "f"(ysum[q * share + i]) : "memory");
     }
-    cluster_arrive_release();      // no CTA may leave while its tile is being read
-    cluster_wait_acquire();
+    cluster_arrive_release();
+    float residual = 0.f;
+    if (a.residual && (int)threadIdx.x < share) residual = out16_to_float<BF>(a.residual[place(from + threadIdx.x)]);
+    cluster_wait_acquire();      // (nothing reaches into another CTA behind this)
+    if (ok)
+        for (int i = threadIdx.x; i < share; i += kMoeThreads) {
+            float v = 0.f;
+            for (int q = 0; q < S; ++q) v += recv[q * share + i];
+            if (a.residual && i >= kMoeThreads) residual = out16_to_float<BF>(a.residual[place(from + i)]);
+            store(from + i, v, residual);
+        }
 }
 
 // x_out[s][i] = x[s / k][perm[e][i]], e = ids[s]: each slot's row of x in its expert's sorted order (act-order checkpoints)
@@ -523,42 +673,66 @@ inline size_t moe_workspace_need(int M, int K, int F, int k, int act_order)
     return moe_h_bytes(P, F) + (act_order ? (((size_t)P * K * 2 + 255) & ~(size_t)255) : 0);
 }
 
-template <int NT, int SUB, bool BF>
-static int launch_moe_nt(const MoeArgs &a, int sms, cudaStream_t s)
+constexpr int kHalfSmBytes = 227 * 1024 / 2 - 1024;      // of a CTA that shares its SM with another
+template <int NT, int NU, int SUB>
+static int moe_red_and_ring_bytes() { return 2 * kMoeWarps * 4 * NU * NT * 32 * 4 + direct_ring_bytes<NU, SUB>(kMoeWarps); }
+
+template <int NT, int NU, int SUB, bool BF>
+static int launch_gate_up(const MoeArgs &a, int most, cudaStream_t s)
 {
-    const int P = a.M * a.k, R = 8 * NT, plan = slot_plan_bytes(P, a.E), slots = 2 * sms;      // two CTAs per SM
-    const int experts = a.E < P ? a.E : P;
-    const int most = experts + P / R < P ? experts + P / R : P;      // segments: one per expert in use, one more per R slots
-    static int configured_up[64] = {}, configured_down[64] = {};
-    const int up_smem = plan + 2 * kMoeWarps * 8 * NT * 32 * 4, down_smem = plan + kMoeWarps * a.M * kDownCols * 4;
-    int st = ensure_dynamic_smem((const void *)moe_gate_up_kernel<NT, SUB, BF>, configured_up, up_smem);
-    if (!st) st = ensure_dynamic_smem((const void *)moe_down_kernel<NT, SUB, BF>, configured_down, down_smem);
+    static int configured[64] = {};
+    const int smem = slot_plan_bytes(a.M * a.k, a.E) + moe_red_and_ring_bytes<NT, NU, SUB>();
+    const int st = ensure_direct_smem((const void *)moe_gate_up_kernel<NT, NU, SUB, BF>, configured, smem, kMoeCtasPerSm);
     if (st) return st;
-    const long long tiles = (long long)most * (a.F / 16);
-    st = launch_dependent(moe_gate_up_kernel<NT, SUB, BF>, dim3((unsigned)(tiles < slots ? tiles : slots)), kMoeThreads, (size_t)up_smem, 1, s, a);
-    if (st) return st;
-    const int down_tiles = a.K / kDownCols;
+    const long long units = (long long)most * (a.F / 16), slots = kMoeCtasPerSm * a.sms;
+    return launch_dependent(moe_gate_up_kernel<NT, NU, SUB, BF>, dim3((unsigned)(units < slots ? units : slots)), kMoeThreads, (size_t)smem, 1, s, a);
+}
+template <int NT, int NU, int SUB>
+static int moe_down_smem(const MoeArgs &a, int S)
+{
+    return slot_plan_bytes(a.M * a.k, a.E) + (S > 1 ? 2 : 1) * a.M * 16 * NU * 4 + moe_red_and_ring_bytes<NT, NU, SUB>();
+}
+template <int NU>
+static int moe_down_cluster(const MoeArgs &a)
+{
     int S = 1;
-    while (S < 8 && down_tiles * S * 2 <= slots) S *= 2;
-    return launch_dependent(moe_down_kernel<NT, SUB, BF>, dim3((unsigned)(down_tiles * S)), kMoeThreads, (size_t)down_smem, S, s, a, S);
+    while (S < 8 && a.K / (16 * NU) * S * 2 <= kMoeCtasPerSm * a.sms) S *= 2;
+    return S;
 }
-template <int SUB, bool BF>
-static int launch_moe_sub(const MoeArgs &a, int sms, cudaStream_t s)
+template <int NT, int NU, int SUB, bool BF>
+static int launch_down(const MoeArgs &a, cudaStream_t s)
 {
-    const char *nt = getenv("MOE_NT");
-    const int v = nt ? atoi(nt) : 1;
-    if (a.M <= 8 || v == 1) return launch_moe_nt<1, SUB, BF>(a, sms, s);
-    return launch_moe_nt<2, SUB, BF>(a, sms, s);
+    static int configured[64] = {};
+    const int tiles = a.K / (16 * NU), S = moe_down_cluster<NU>(a);
+    int smem = moe_down_smem<NT, NU, SUB>(a, S);
+    // exactly as many CTAs per SM as it takes: with more room clusters pile up on some SMs and leave others empty
+    const int per_sm = tiles * S <= a.sms ? 1 : kMoeCtasPerSm;
+    const int pad = 227 * 1024 / (per_sm + 1) + 512;
+    if (smem < pad) smem = pad;
+    const int st = ensure_direct_smem((const void *)moe_down_kernel<NT, NU, SUB, BF>, configured, smem, per_sm);
+    if (st) return st;
+    return launch_dependent(moe_down_kernel<NT, NU, SUB, BF>, dim3((unsigned)(tiles * S)), kMoeThreads, (size_t)smem, S, s, a, S);
 }
-int launch_moe(const MoeArgs &a, int group_size, int bf16, int sms, cudaStream_t s)
+template <int NT, int SUB, bool BF>
+static int launch_moe_nt(const MoeArgs &a, cudaStream_t s)
+{
+    const int P = a.M * a.k, R = 8 * NT, experts = a.E < P ? a.E : P;
+    const int most = experts + P / R < P ? experts + P / R : P;      // segments: one per expert in use, one more per R slots
+    constexpr int NU = SUB == 4 ? 2 : 4;
+    const int st = launch_gate_up<NT, NU, SUB, BF>(a, most, s);
+    if (st) return st;
+    if (NU == 2 || moe_down_smem<NT, NU, SUB>(a, moe_down_cluster<NU>(a)) > kHalfSmBytes) return launch_down<NT, 2, SUB, BF>(a, s);
+    return launch_down<NT, NU, SUB, BF>(a, s);
+}
+int launch_moe(const MoeArgs &a, int group_size, int bf16, cudaStream_t s)
 {
     switch ((bf16 ? 10 : 0) + kGroup / group_size) {
-    case 1: return launch_moe_sub<1, false>(a, sms, s);
-    case 2: return launch_moe_sub<2, false>(a, sms, s);
-    case 4: return launch_moe_sub<4, false>(a, sms, s);
-    case 11: return launch_moe_sub<1, true>(a, sms, s);
-    case 12: return launch_moe_sub<2, true>(a, sms, s);
-    default: return launch_moe_sub<4, true>(a, sms, s);
+    case 1: return launch_moe_nt<1, 1, false>(a, s);
+    case 2: return launch_moe_nt<1, 2, false>(a, s);
+    case 4: return launch_moe_nt<1, 4, false>(a, s);
+    case 11: return launch_moe_nt<1, 1, true>(a, s);
+    case 12: return launch_moe_nt<1, 2, true>(a, s);
+    default: return launch_moe_nt<1, 4, true>(a, s);
     }
 }
 

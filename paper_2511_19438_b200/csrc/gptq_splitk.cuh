@@ -265,8 +265,8 @@ splitk_kernel(const SplitKArgs a, const __grid_constant__ CUtensorMap x_map)
     // the residual is the one that writes the same element of y, so the two may be one buffer)
     auto addend = [&](int m, int n) {
         float v = 0.f;
-        if (a.bias) v += __half2float(a.bias[n]);
-        if (a.residual) v += __half2float(a.residual[(size_t)m * a.N + n]);
+        if (a.bias) v += out16_to_float<BF>(a.bias[n]);
+        if (a.residual) v += out16_to_float<BF>(a.residual[(size_t)m * a.N + n]);
         return v;
     };
     if (S == 1) {

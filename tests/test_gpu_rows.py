@@ -7,8 +7,13 @@ Plain implementations in 64 bits on the oracle's dequantised weights.  Tolerance
 * experts: each activation h is rounded once, which moves y by at most u sum |w h d|, and y is rounded once, u |y|; the fp32
   errors of gate and up reach h through silu (slope below 1.1) and the product, 2^-18 covers the fast exponential and division.
   All roundings are independent, so the rms error stays below u sqrt(y^2 + sum (w h d)^2) (three times its variance);
-* adapters: one rounding of y up to 16 rows; above, every scaled weight is rounded, u sum |x w|, rms u sqrt(sum (x w)^2), and so is
-  the adapters' part.
+* adapters: one rounding of y up to 8 rows; above, the adapters' part is rounded to 16 bits on its way to the fp32 sums, u |part|; above
+  16, so is every scaled weight, u sum |x w|, rms u sqrt(sum (x w)^2).
+* up to 8 rows an adapter, sum (q - z) x is formed as sum q x - z sum x (bfloat16: sum (128 + q) x - (128 + z) sum x), both in fp32.
+  Rounding then goes by the larger products (q + z) |x| s (bfloat16: (256 + q + z) |x| s), but of a quantisation group of at most 128
+  rows alone, eight MMAs of 16 rows deep, as the difference is taken per group: at most 8 2^-23 of them, which for the 31 (287) that
+  they are at most is 8 * 31 (8 * 287) 2^-23 s sum |x| over the rows, 2^-15 (2^-11.8) of s sum |x| - below u of sum |x w| in both types
+  (mean |q - z| is 5.3), and as independent errors of the groups far below it in a sum.  It is counted as `sums`.
 """
 import math
 
@@ -29,6 +34,12 @@ if torch.cuda.is_available():
 
 U = {torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
 F32 = 2.0 ** -23
+
+
+def sums(dtype, x, w64):
+    """Bound of what forming sum (q - z) x as a difference adds: 8 2^-23 (31 or 287) s |x| per row, s <= |w| / |q - z|, of which the
+    mean over the rows is taken: |w| summed over a column is 5.3 s summed, within a tenth for 128 rows and more."""
+    return 8 * F32 * (287 if dtype == torch.bfloat16 else 31) / 4.5 * (x.double().abs() @ w64.abs())
 
 
 @pytest.fixture(scope="module")
@@ -131,13 +142,15 @@ class Moe:
                     named[e] = named.get(e, 0.0) + w
             for e, w in named.items():
                 gu, size = x[m] @ self.up64[e], x[m].abs() @ self.up64[e].abs()
-                gate, up, dg, du = gu[:self.F], gu[self.F:], self.K * F32 * size[:self.F], self.K * F32 * size[self.F:]
+                more = sums(self.dtype, x[m], self.up64[e])
+                gate, up = gu[:self.F], gu[self.F:]
+                dg, du = self.K * F32 * size[:self.F] + more[:self.F], self.K * F32 * size[self.F:] + more[self.F:]
                 silu = gate * torch.sigmoid(gate)
                 h = silu * up
                 dh = 1.1 * dg * (up.abs() + du) + silu.abs() * du + 2.0 ** -18 * h.abs()
                 d = self.down64[e].abs()
                 y[m] += w * (h @ self.down64[e])
-                most[m] += abs(w) * (((u + self.F * F32) * h.abs() + 1.01 * dh + 2.0 ** -24) @ d)
+                most[m] += abs(w) * (((u + self.F * F32) * h.abs() + 1.01 * dh + 2.0 ** -24) @ d + sums(self.dtype, h, self.down64[e]))
                 square[m] += (w * u) ** 2 * ((h * h) @ (d * d))
         return y, most + u * y.abs(), square + (u * y) ** 2
 
@@ -320,12 +333,14 @@ class Lora:
             part[m] = s * ((x[m] @ A.t()) @ Bm.t())
             part_size[m] = abs(s) * ((x[m].abs() @ A.abs().t()) @ Bm.abs().t())
         y = y + part
-        few = x.shape[0] <= 16
-        most = u * y.abs() + self.K * F32 * size + (self.K + self.rank) * F32 * part_size
+        most = u * y.abs() + self.K * F32 * size + (self.K + self.rank) * F32 * part_size + sums(self.dtype, x, self.w64)
         mean_square = (u * y) ** 2
-        if not few:
-            most += u * size + u * part.abs()
-            mean_square += u * u * (square + part * part)
+        if x.shape[0] > 8:
+            most += u * part.abs()
+            mean_square += (u * part) ** 2
+        if x.shape[0] > 16:
+            most += u * size
+            mean_square += u * u * square
         return y, 1.01 * most + 2.0 ** -24, mean_square
 
     def check(self, ws, x, ids, scales, D=None, y=None, stream=None):
