@@ -71,6 +71,12 @@ __host__ __device__ constexpr int unit_offset(int u)
 struct UnitPtrs {
     const uint8_t *w, *s, *z;
 };
+// a lane's share of a warp's units: 16 bytes of weights per unit and K64 block; 8 bytes of a pair's scales (lanes below 8 SUB) or zero points
+// (the next 2 SUB lanes; with SUB = 4, where these are no longer in the warp, the first 8 lanes have both)
+template <int SUB>
+struct LanePtrs {
+    const uint8_t *w, *m, *z;      // (z: SUB = 4 only)
+};
 // a unit in item 0 of a panel
 template <int SUB>
 __device__ __forceinline__ UnitPtrs unit_ptrs(const uint8_t *qweight, const uint8_t *scales, const uint8_t *qzeros, int panel, int G, int unit)
@@ -78,32 +84,30 @@ __device__ __forceinline__ UnitPtrs unit_ptrs(const uint8_t *qweight, const uint
     const size_t item = (size_t)panel * G;
     return {qweight + item * kItemWBytes + unit * kUnitBytes, scales + item * (SUB * kItemSBytes) + unit * 32, qzeros + item * (SUB * kItemZBytes) + unit * 8};
 }
-// The same with a lane's share added: 16 bytes of weights; of the pair's scales 8 bytes for a lane below 8 SUB, of its zero points for a
-// lane below 2 SUB.
 template <bool GATE_UP, int SUB>
-__device__ __forceinline__ UnitPtrs lane_ptrs(UnitPtrs p, int lane)
+__device__ __forceinline__ LanePtrs<SUB> lane_ptrs(const UnitPtrs &p, int lane)
 {
-    p.w += lane * 16;
-    p.s += (lane >> 3) * kItemSBytes + unit_offset<GATE_UP>(lane >> 2 & 1) * 32 + (lane & 3) * 8;
-    p.z += (lane >> 1) * kItemZBytes + unit_offset<GATE_UP>(lane & 1) * 8;
-    return p;
+    const int zl = SUB == 4 ? lane : lane - 8 * SUB;
+    const uint8_t *s = p.s + (lane >> 3) * kItemSBytes + unit_offset<GATE_UP>(lane >> 2 & 1) * 32 + (lane & 3) * 8;
+    const uint8_t *z = p.z + (zl >> 1) * kItemZBytes + unit_offset<GATE_UP>(zl & 1) * 8;
+    return {p.w + lane * 16, SUB == 4 || lane < 8 * SUB ? s : z, z};
 }
 // What a warp multiplies next: the item's addresses, the lane's token rows at the item's first column + 8 t4, the layer's
 // format flags as loaded (looked at only when the item is multiplied), a number of the caller's
 // (not negative), and how many of the warp's pairs of units are wanted (the others' sums stay as they are).
-template <int NT>
+template <int NT, int SUB>
 struct DirectItem {
-    UnitPtrs p;
+    LanePtrs<SUB> p;
     const __half *x[NT];
     uint32_t flags;
     int tag, pairs;
 };
 template <int NT, int SUB>
-__device__ __forceinline__ void set_item(DirectItem<NT> &it, const UnitPtrs &p, const __half *const (&rows)[NT], int item)
+__device__ __forceinline__ void set_item(DirectItem<NT, SUB> &it, const LanePtrs<SUB> &p, const __half *const (&rows)[NT], int item, int lane)
 {
     it.p.w = p.w + (size_t)item * kItemWBytes;
-    it.p.s = p.s + (size_t)item * (SUB * kItemSBytes);
-    it.p.z = p.z + (size_t)item * (SUB * kItemZBytes);
+    it.p.m = p.m + (size_t)item * (SUB == 4 || lane < 8 * SUB ? SUB * kItemSBytes : SUB * kItemZBytes);
+    if constexpr (SUB == 4) it.p.z = p.z + (size_t)item * (SUB * kItemZBytes);
 #pragma unroll
     for (int t = 0; t < NT; ++t) it.x[t] = rows[t] + (size_t)item * kGroup;
 }
@@ -114,8 +118,8 @@ struct DirectRows {
     uint32_t flags;
     int tag, pairs;
 };
-template <int NT>
-__device__ __forceinline__ void load_rows(DirectRows<NT> &r, const DirectItem<NT> &it)
+template <int NT, int SUB>
+__device__ __forceinline__ void load_rows(DirectRows<NT> &r, const DirectItem<NT, SUB> &it)
 {
     r.tag = it.tag;
     r.flags = it.flags;
@@ -127,6 +131,12 @@ __device__ __forceinline__ void load_rows(DirectRows<NT> &r, const DirectItem<NT
         for (int q = 0; q < 4; ++q) r.x[t][q] = ldg_rows128(it.x[t] + 32 * q);
 }
 
+// a value that the compiler keeps instead of working it out again
+__device__ __forceinline__ uint32_t kept(uint32_t v)
+{
+    asm volatile("mov.b32 %0, %1;" : "=r"(v) : "r"(v));
+    return v;
+}
 __device__ __forceinline__ uint64_t register_pair(uint32_t lo, uint32_t hi)
 {
     uint64_t p;
@@ -245,17 +255,21 @@ __device__ __forceinline__ void multiply_pair(uint32_t stage, int lane, uint32_t
     }
 }
 
-// Works through the items that `next` yields (it fills a DirectItem, tag < 0 at the end); `before(tag)` is called ahead of each
-// item's product.  `ring`: the warp's part of the ring.
+// Works through the items that `next` yields (it fills a DirectItem, tag < 0 at the end); `ready()` is called once,
+// between the first requests for weights and the first for activations, `before(tag)` ahead of each item's product.  `ring`: the warp's part of the ring.
 // A stage is filled again a pair after it was read: the reads are over.
-template <int NT, int NU, bool GATE_UP, int SUB, bool BF, bool IN_ORDER, typename Next, typename Before>
-__device__ __forceinline__ void stream_items(uint32_t ring, int lane, uint32_t one, float (&acc)[NU][NT][4], Next next, Before before)
+template <int NT, int NU, bool GATE_UP, int SUB, bool BF, bool IN_ORDER, typename Next, typename Ready, typename Before>
+__device__ __forceinline__ void stream_items(uint32_t ring, int lane, uint32_t one, float (&acc)[NU][NT][4], Next next, Ready ready, Before before)
 {
     static_assert(NU == 2 || NU == 4, "one or two pairs of units");
     constexpr int NP = NU / 2, kStages = NP + 2;
     constexpr uint32_t kStage = direct_stage_bytes<SUB>(), kEnd = kStages * kStage;
-    DirectItem<NT> it{};
+    DirectItem<NT, SUB> it{};
     DirectRows<NT> x;
+    const int zl = SUB == 4 ? lane : lane - 8 * SUB;
+    const uint32_t m_at = kept(kPairW + (SUB == 4 || lane < 8 * SUB ? (lane >> 3) * kPairMeta + (lane & 7) * 8 : (zl >> 1) * kPairMeta + 64 + (zl & 1) * 8));
+    const uint32_t w_at = kept(lane * 16);
+    const int m_step = kept(GATE_UP ? (SUB == 4 || lane < 8 * SUB ? 32 : 8) : (SUB == 4 || lane < 8 * SUB ? 64 : 16));      // from pair to pair
     uint32_t fill = 0, at = 0;      // offsets into the ring
     auto advance = [&](uint32_t &offset) { offset = offset == kEnd - kStage ? 0 : offset + kStage; };
     auto copy_pair = [&](int pair) {
@@ -264,11 +278,11 @@ __device__ __forceinline__ void stream_items(uint32_t ring, int lane, uint32_t o
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const uint8_t *src = it.p.w + unit_offset<GATE_UP>(2 * pair + u) * kUnitBytes;
-                cp_async16(to + lane * 16 + u * 2 * kUnitBytes, src);
-                cp_async16(to + lane * 16 + u * 2 * kUnitBytes + kUnitBytes, src + kBlockWBytes);
+                cp_async16(to + w_at + u * 2 * kUnitBytes, src);
+                cp_async16(to + w_at + u * 2 * kUnitBytes + kUnitBytes, src + kBlockWBytes);
             }
-            cp_async8_if(lane < 8 * SUB, to + kPairW + (lane >> 3) * kPairMeta + (lane & 7) * 8, it.p.s + unit_offset<GATE_UP>(2 * pair) * 32);
-            cp_async8_if(lane < 2 * SUB, to + kPairW + (lane >> 1) * kPairMeta + 64 + (lane & 1) * 8, it.p.z + unit_offset<GATE_UP>(2 * pair) * 8);
+            cp_async8_if(SUB == 4 || lane < 10 * SUB, to + m_at, it.p.m + pair * m_step);
+            if constexpr (SUB == 4) cp_async8_if(lane < 8, to + kPairW + (lane >> 1) * kPairMeta + 64 + (lane & 1) * 8, it.p.z + unit_offset<GATE_UP>(2 * pair) * 8);
         }
         cp_async_commit();
         advance(fill);
@@ -276,16 +290,18 @@ __device__ __forceinline__ void stream_items(uint32_t ring, int lane, uint32_t o
     next(it);
 #pragma unroll
     for (int p = 0; p < NP; ++p) copy_pair(p);
-    load_rows<NT>(x, it);
+    const DirectItem<NT, SUB> first = it;
     next(it);
     copy_pair(0);
+    ready();
+    load_rows<NT, SUB>(x, first);
     while (x.tag >= 0) {
         before(x.tag);
         ItemRows<NT, SUB> rows;
         prepare_rows<NT, SUB, BF, IN_ORDER>(rows, x.x, one);
         const uint32_t flags = x.flags;
         const int pairs = x.pairs;
-        load_rows<NT>(x, it);
+        load_rows<NT, SUB>(x, it);
         if constexpr (NP == 2) {
             copy_pair(1);
             cp_async_wait<NP + 1>();

@@ -312,8 +312,8 @@ lora_gemm_kernel(const LoraArgs a, const __half *x, const uint8_t *qweight, cons
         for (int r = 0; r < a.rank; r += 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + r));
     }
     int l_pair = t0, l_next = t0, l_item = G, l_turn = warp - 1;
-    UnitPtrs ptrs{};
-    auto next = [&](DirectItem<1> &it) {
+    LanePtrs<SUB> ptrs{};
+    auto next = [&](DirectItem<1, SUB> &it) {
         l_item += kLoraWarps;
         while (l_item >= G) {
             if (l_next >= t1) {
@@ -325,7 +325,7 @@ lora_gemm_kernel(const LoraArgs a, const __half *x, const uint8_t *qweight, cons
             l_item = ++l_turn & (kLoraWarps - 1);
             ptrs = lane_ptrs<false, SUB>(unit_ptrs<SUB>(qweight, scales, qzeros, l_pair >> 2, G, 2 * (l_pair & 3)), lane);
         }
-        set_item<1, SUB>(it, ptrs, rows, l_item);
+        set_item<1, SUB>(it, ptrs, rows, l_item, lane);
         it.flags = flags;
         it.tag = l_pair;
         it.pairs = l_next - l_pair;
@@ -390,7 +390,7 @@ lora_gemm_kernel(const LoraArgs a, const __half *x, const uint8_t *qweight, cons
         ++tiles;
     };
     const uint32_t ring = smem_u32(red + 2 * kLoraWarps * kValues * 32) + warp * direct_ring_bytes<NU, SUB>(1);
-    stream_items<1, NU, false, SUB, BF, false>(ring, lane, a.one, acc, next, [&](int t) { while (pair < t) finish_tile(); });
+    stream_items<1, NU, false, SUB, BF, false>(ring, lane, a.one, acc, next, [] {}, [&](int t) { while (pair < t) finish_tile(); });
     while (pair < t1) finish_tile();
     if (tiles) add_up();
 }

@@ -367,13 +367,13 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_gate_up_kernel
     // share where the items are no multiple of the warps
     int l_unit = t0, l_next = t0, l_item = G, l_seg = 0, l_col = 0, l_turn = warp - 1;
     uint32_t l_flags = 0;
-    UnitPtrs ptrs{};
+    LanePtrs<SUB> ptrs{};
     const __half *rows[NT];
     auto row_of = [&](int s) { return a.x + (size_t)(a.x_by_slot ? s : plan.token[s]) * a.K; };
     auto up_flags = [&](int e) {
         return __ldg(&reinterpret_cast<const TiledTrailer *>(a.gu_z + (size_t)(e + 1) * a.gu_z_bytes - kTrailerBytes)->flags);
     };
-    auto next = [&](DirectItem<NT> &it) {
+    auto next = [&](DirectItem<NT, SUB> &it) {
         l_item += kMoeWarps;
         while (l_item >= G) {
             if (l_next >= t1) {
@@ -396,7 +396,7 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_gate_up_kernel
             const int e = plan.seg_expert[l_seg];
             ptrs = lane_ptrs<true, SUB>(unit_ptrs<SUB>(a.gu_w + e * a.gu_w_bytes, a.gu_s + e * a.gu_s_bytes, a.gu_z + e * a.gu_z_bytes, l_col >> 2, G, l_col & 3), lane);
         }
-        set_item<NT, SUB>(it, ptrs, rows, l_item);
+        set_item<NT, SUB>(it, ptrs, rows, l_item, lane);
         it.flags = l_flags;
         it.tag = l_unit;
         it.pairs = l_next - l_unit;
@@ -404,12 +404,13 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_gate_up_kernel
 
     // ---- the end of a tile
     float acc[NU][NT][4] = {};
-    int unit = t0, left = t0, tiles = 0;      // the tile at hand, the one before it, how many came before
+    // the tile at hand, the one before it (its segment and column), how many came before
+    int unit = t0, seg_at = t0 / per_seg, col_at = t0 - seg_at * per_seg, left = t0, left_seg = 0, left_col = 0, tiles = 0;
     bool saw_nan = false;
     auto add_up = [&]() {      // the sums of the tile at `left` over the warps, in their order
         const int done = tiles - 1;
         if (!mbar_wait(bars + 8 * (done & 1), (done >> 1) & 1)) return;
-        const int seg = left / per_seg, c0 = (left - seg * per_seg) * 16;
+        const int seg = left_seg, c0 = left_col * 16;
         const int first = plan.seg_begin[seg], count = plan.seg_begin[seg + 1] - first;
         const float *buf = red + (done & 1) * (kMoeWarps * kValues * 32);
         for (int o = threadIdx.x; o < width(left) * (4 * NT * 32); o += kMoeThreads) {
@@ -443,12 +444,14 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_gate_up_kernel
                 }
         __syncwarp();
         if (lane == 0) mbar_arrive(bars + 8 * (tiles & 1));
-        left = unit;
+        left = unit, left_seg = seg_at, left_col = col_at;
         unit += width(unit);
+        col_at += unit - left;
+        if (col_at == per_seg) col_at = 0, ++seg_at;
         ++tiles;
     };
     const uint32_t ring = smem_u32(red + 2 * kMoeWarps * kValues * 32) + warp * direct_ring_bytes<NU, SUB>(1);
-    stream_items<NT, NU, true, SUB, BF, false>(ring, lane, a.one, acc, next, [&](int t) { while (unit < t) finish_tile(); });
+    stream_items<NT, NU, true, SUB, BF, false>(ring, lane, a.one, acc, next, [] {}, [&](int t) { while (unit < t) finish_tile(); });
     while (unit < t1) finish_tile();
     if (tiles) add_up();
     if (!saw_nan) return;
@@ -512,12 +515,12 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_down_kernel(co
     // ---- what comes next: part l_part (segment seg0 + l_part), item l_item
     int l_part = -1, l_item = G, l_end = 0;
     uint32_t l_flags = 0;
-    UnitPtrs ptrs{};
+    LanePtrs<SUB> ptrs{};
     const __half *rows[NT];
     auto trailer_flags = [](const uint8_t *zeros, size_t bytes, int e) {
         return __ldg(&reinterpret_cast<const TiledTrailer *>(zeros + (size_t)(e + 1) * bytes - kTrailerBytes)->flags);
     };
-    auto next = [&](DirectItem<NT> &it) {
+    auto next = [&](DirectItem<NT, SUB> &it) {
         l_item += kMoeWarps;
         while (l_item >= l_end) {
             if (++l_part >= parts) {
@@ -533,7 +536,7 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_down_kernel(co
 #pragma unroll
             for (int t = 0; t < NT; ++t) rows[t] = a.h + (size_t)plan.slot[first + (8 * t + g < count ? 8 * t + g : 0)] * a.F + 8 * t4;
         }
-        set_item<NT, SUB>(it, ptrs, rows, l_item);
+        set_item<NT, SUB>(it, ptrs, rows, l_item, lane);
         it.flags = l_flags;
         it.tag = l_part;
         it.pairs = NU / 2;
@@ -582,9 +585,8 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_down_kernel(co
         if (lane == 0) mbar_arrive(bars + 8 * (now & 1));
         ++now;
     };
-    pdl_wait();
     const uint32_t ring = smem_u32(red + 2 * kMoeWarps * kValues * 32) + warp * direct_ring_bytes<NU, SUB>(1);
-    stream_items<NT, NU, false, SUB, BF, true>(ring, lane, a.one, acc, next, [&](int p) { while (now < p) finish_part(); });
+    stream_items<NT, NU, false, SUB, BF, true>(ring, lane, a.one, acc, next, [] { pdl_wait(); }, [&](int p) { while (now < p) finish_part(); });
     while (now < parts) finish_part();
     if (parts) add_up(parts - 1);
 
