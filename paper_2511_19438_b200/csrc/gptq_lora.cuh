@@ -276,21 +276,22 @@ __global__ void __launch_bounds__(256, 2) lora_delta_runs_kernel(const LoraArgs 
 
 // The product with W of up to 8 rows, plus the expansion.  The work is counted in pairs of units, 32 columns; a CTA takes a range of
 // neighbouring ones, in tiles of two where they are half a panel, else of one.  As in the routed-expert kernels the warps share a
-// tile's items along K, leave their sums and go on, and add up at the next tile's end.
-template <int SUB, bool BF>
-__global__ void __launch_bounds__(kLoraThreads, 2)
+// tile's items along K, leave their sums and go on, and add up at the next tile's end.  W: 8 warps, two CTAs per SM; where there is no
+// more than a pair of units for each SM (N up to 4736), 16 warps and one.
+template <int W, int NU, int SUB, bool BF>
+__global__ void __launch_bounds__(32 * W, 16 / W)
 lora_gemm_kernel(const LoraArgs a, const __half *x, const uint8_t *qweight, const uint8_t *scales, const uint8_t *qzeros,
                  const TiledTrailer *trailer, __half *y)
 {
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ __align__(8) uint64_t arrived[2];
     __shared__ int s_ids[8];
-    constexpr int NU = SUB == 4 ? 2 : 4, kValues = 4 * NU;
+    constexpr int kValues = 4 * NU, kThreads = 32 * W;
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
     const uint32_t bars = smem_u32(arrived);
     if (threadIdx.x == 0) {
-        mbar_init(bars, kLoraWarps);
-        mbar_init(bars + 8, kLoraWarps);
+        mbar_init(bars, W);
+        mbar_init(bars + 8, W);
     }
     const uint32_t flags = __ldg(&trailer->flags);
     const int v_pitch = a.rank + 4;
@@ -305,7 +306,7 @@ lora_gemm_kernel(const LoraArgs a, const __half *x, const uint8_t *qweight, cons
     pdl_launch_dependents();
     const __half *rows[1] = {x + (size_t)min(g, a.M - 1) * a.K + 8 * t4};
     // the rows of B that the epilogue will want, on their way to L2
-    for (int i = threadIdx.x; i < a.M * (t1 - t0) * 32; i += kLoraThreads) {
+    for (int i = threadIdx.x; i < a.M * (t1 - t0) * 32; i += kThreads) {
         const int id = s_ids[i % a.M];
         if ((unsigned)id >= (unsigned)a.adapters) continue;
         const __half *p = a.b + ((size_t)id * a.N + 32 * t0 + i / a.M) * a.rank;
@@ -314,7 +315,7 @@ lora_gemm_kernel(const LoraArgs a, const __half *x, const uint8_t *qweight, cons
     int l_pair = t0, l_next = t0, l_item = G, l_turn = warp - 1;
     LanePtrs<SUB> ptrs{};
     auto next = [&](DirectItem<1, SUB> &it) {
-        l_item += kLoraWarps;
+        l_item += W;
         while (l_item >= G) {
             if (l_next >= t1) {
                 it.tag = -1;
@@ -322,7 +323,7 @@ lora_gemm_kernel(const LoraArgs a, const __half *x, const uint8_t *qweight, cons
             }
             l_pair = l_next;
             l_next += width(l_pair);
-            l_item = ++l_turn & (kLoraWarps - 1);
+            l_item = ++l_turn & (W - 1);
             ptrs = lane_ptrs<false, SUB>(unit_ptrs<SUB>(qweight, scales, qzeros, l_pair >> 2, G, 2 * (l_pair & 3)), lane);
         }
         set_item<1, SUB>(it, ptrs, rows, l_item, lane);
@@ -339,20 +340,20 @@ lora_gemm_kernel(const LoraArgs a, const __half *x, const uint8_t *qweight, cons
         if (done == 0) {
             // v is there, and y no longer in use by earlier kernels
             pdl_wait();
-            for (int i = 4 * threadIdx.x; i < a.M * a.rank; i += 4 * kLoraThreads) {
+            for (int i = 4 * threadIdx.x; i < a.M * a.rank; i += 4 * kThreads) {
                 const int m = i / a.rank, r = i - m * a.rank;
                 *reinterpret_cast<float4 *>(vs + m * v_pitch + r) = lora_v4(a, m, r);
             }
             __syncthreads();
         }
         if (!mbar_wait(bars + 8 * (done & 1), (done >> 1) & 1)) return;
-        const float *buf = red + (done & 1) * (kLoraWarps * kValues * 32);
-        for (int o = threadIdx.x; o < width(left) * 256; o += kLoraThreads) {
+        const float *buf = red + (done & 1) * (W * kValues * 32);
+        for (int o = threadIdx.x; o < width(left) * 256; o += kThreads) {
             const int v = o >> 5, i = v & 3, m = 2 * t4 + (i & 1), n = 32 * left + 16 * (v >> 2) + g + 8 * (i >> 1);
             if (m >= a.M || !layout_ok) continue;
             float sum = 0.f;
 #pragma unroll
-            for (int w = 0; w < kLoraWarps; ++w) sum += buf[(w * kValues + v) * 32 + lane];
+            for (int w = 0; w < W; ++w) sum += buf[(w * kValues + v) * 32 + lane];
             if (sum != sum) {      // the long way (see stream_items)
                 const UnitPtrs p = unit_ptrs<SUB>(qweight, scales, qzeros, n / kPanel, G, n % kPanel / 16);
                 sum = long_sum<BF>(p.w, p.s, p.z, SUB, n % 16, flags & kFormatZerosMinusOne, x + (size_t)m * a.K, G, false);
@@ -375,7 +376,7 @@ lora_gemm_kernel(const LoraArgs a, const __half *x, const uint8_t *qweight, cons
     };
     auto finish_tile = [&]() {
         if (tiles) add_up();
-        float *buf = red + (tiles & 1) * (kLoraWarps * kValues * 32);
+        float *buf = red + (tiles & 1) * (W * kValues * 32);
 #pragma unroll
         for (int u = 0; u < NU; ++u)
 #pragma unroll
@@ -389,7 +390,7 @@ lora_gemm_kernel(const LoraArgs a, const __half *x, const uint8_t *qweight, cons
         pair += width(pair);
         ++tiles;
     };
-    const uint32_t ring = smem_u32(red + 2 * kLoraWarps * kValues * 32) + warp * direct_ring_bytes<NU, SUB>(1);
+    const uint32_t ring = smem_u32(red + 2 * W * kValues * 32) + warp * direct_ring_bytes<NU, SUB>(1);
     stream_items<1, NU, false, SUB, BF, false>(ring, lane, a.one, acc, next, [] {}, [&](int t) { while (pair < t) finish_tile(); });
     while (pair < t1) finish_tile();
     if (tiles) add_up();
@@ -445,19 +446,25 @@ int launch_lora_delta(const LoraArgs &a, __half *delta, int bf16, cudaStream_t s
                 : launch_dependent(lora_delta_runs_kernel<false>, grid, 256, smem, 1, s, a, delta);
 }
 
+template <int W, int NU, int SUB, bool BF>
+static int launch_lora_gemm_warps(const LoraArgs &a, const __half *x, const void *qweight, const void *scales, const void *qzeros,
+                                  __half *y, cudaStream_t s)
+{
+    const TiledTrailer *trailer = reinterpret_cast<const TiledTrailer *>((const uint8_t *)qzeros + tiled_zero_bytes(a.N, a.K, kGroup / SUB));
+    const int smem = 8 * (a.rank + 4) * 4 + 2 * W * 4 * NU * 32 * 4 + direct_ring_bytes<NU, SUB>(W);
+    static int configured[64] = {};
+    const int st = ensure_direct_smem((const void *)lora_gemm_kernel<W, NU, SUB, BF>, configured, smem, 16 / W);
+    if (st) return st;
+    const int pairs = a.N / 32, slots = 16 / W * a.sms;
+    return launch_dependent(lora_gemm_kernel<W, NU, SUB, BF>, dim3((unsigned)(pairs < slots ? pairs : slots)), 32 * W, (size_t)smem, 1, s, a, x,
+                            (const uint8_t *)qweight, (const uint8_t *)scales, (const uint8_t *)qzeros, trailer, y);
+}
 template <int SUB, bool BF>
 static int launch_lora_gemm_sub(const LoraArgs &a, const __half *x, const void *qweight, const void *scales, const void *qzeros,
                                 __half *y, cudaStream_t s)
 {
-    const TiledTrailer *trailer = reinterpret_cast<const TiledTrailer *>((const uint8_t *)qzeros + tiled_zero_bytes(a.N, a.K, kGroup / SUB));
-    constexpr int NU = SUB == 4 ? 2 : 4;
-    const int smem = 8 * (a.rank + 4) * 4 + 2 * kLoraWarps * 4 * NU * 32 * 4 + direct_ring_bytes<NU, SUB>(kLoraWarps);
-    static int configured[64] = {};
-    const int st = ensure_direct_smem((const void *)lora_gemm_kernel<SUB, BF>, configured, smem, 2);
-    if (st) return st;
-    const int pairs = a.N / 32;
-    return launch_dependent(lora_gemm_kernel<SUB, BF>, dim3((unsigned)(pairs < 2 * a.sms ? pairs : 2 * a.sms)), kLoraThreads, (size_t)smem, 1, s,
-                            a, x, (const uint8_t *)qweight, (const uint8_t *)scales, (const uint8_t *)qzeros, trailer, y);
+    if (a.N / 32 <= a.sms) return launch_lora_gemm_warps<16, 2, SUB, BF>(a, x, qweight, scales, qzeros, y, s);
+    return launch_lora_gemm_warps<8, SUB == 4 ? 2 : 4, SUB, BF>(a, x, qweight, scales, qzeros, y, s);
 }
 // x: in the row order of the tiled layer
 int launch_lora_gemm(const LoraArgs &a, const __half *x, const void *qweight, const void *scales, const void *qzeros, __half *y,
