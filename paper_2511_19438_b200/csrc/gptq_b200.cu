@@ -1245,6 +1245,7 @@ static int lora_dispatch(const void *x, const void *qweight, const void *qzeros,
     int st = check_shape(M, N, K, group_size);
     if (st) return st;
     if (rank < 1 || adapters < 1) return GPTQ_ERR_SHAPE;
+    if (x == y) return GPTQ_ERR_LAYOUT;      // rows of x are read while others of y are written
     const void *ptrs[] = {x, qweight, qzeros, scales, lora_a, lora_b, adapter_ids, adapter_scales, y, act_order == 1 ? g_idx : nullptr};
     for (const void *p : ptrs)
         if (!aligned16(p)) return GPTQ_ERR_ALIGN;

@@ -6,7 +6,7 @@
 // ring of its warp's in shared memory with cp.async and reads back what it copied itself (scales and zero points: what its warp did), so that
 // no barrier of the CTA stands between memory and the tensor cores, and a warp's next item may lie in any layer, panel and row of K - which is what rows that choose their
 // weights need.  The ring holds pairs of units: the rest of the item at hand and the whole next one are on their way.  Activations are
-// loaded into registers an item ahead: lane (g, t4) reads 16 bytes of token row g, the B fragments for all of the warp's units.  Up to 8 NT
+// loaded into registers an item ahead: lane (g, t4) reads 16 bytes of token row g, the B fragments for all of the warp's units.  Up to 8
 // rows; a lane without a row reads another one's, whose products land in columns that nobody looks at.
 //
 // Arithmetic, fp16: a nibble alone in a 16-bit word is the subnormal number q 2^-24, so the MMAs take `w & 0x000f000f` and
@@ -95,40 +95,36 @@ __device__ __forceinline__ LanePtrs<SUB> lane_ptrs(const UnitPtrs &p, int lane)
 // What a warp multiplies next: the item's addresses, the lane's token rows at the item's first column + 8 t4, the layer's
 // format flags as loaded (looked at only when the item is multiplied), a number of the caller's
 // (not negative), and how many of the warp's pairs of units are wanted (the others' sums stay as they are).
-template <int NT, int SUB>
+template <int SUB>
 struct DirectItem {
     LanePtrs<SUB> p;
-    const __half *x[NT];
+    const __half *x;
     uint32_t flags;
     int tag, pairs;
 };
-template <int NT, int SUB>
-__device__ __forceinline__ void set_item(DirectItem<NT, SUB> &it, const LanePtrs<SUB> &p, const __half *const (&rows)[NT], int item, int lane)
+template <int SUB>
+__device__ __forceinline__ void set_item(DirectItem<SUB> &it, const LanePtrs<SUB> &p, const __half *row, int item, int lane)
 {
     it.p.w = p.w + (size_t)item * kItemWBytes;
     it.p.m = p.m + (size_t)item * (SUB == 4 || lane < 8 * SUB ? SUB * kItemSBytes : SUB * kItemZBytes);
     if constexpr (SUB == 4) it.p.z = p.z + (size_t)item * (SUB * kItemZBytes);
-#pragma unroll
-    for (int t = 0; t < NT; ++t) it.x[t] = rows[t] + (size_t)item * kGroup;
+    it.x = row + (size_t)item * kGroup;
 }
 
-template <int NT>
 struct DirectRows {
-    uint4 x[NT][4];               // [32-row quarter]
+    uint4 x[4];                   // [32-row quarter]
     uint32_t flags;
     int tag, pairs;
 };
-template <int NT, int SUB>
-__device__ __forceinline__ void load_rows(DirectRows<NT> &r, const DirectItem<NT, SUB> &it)
+template <int SUB>
+__device__ __forceinline__ void load_rows(DirectRows &r, const DirectItem<SUB> &it)
 {
     r.tag = it.tag;
     r.flags = it.flags;
     r.pairs = it.pairs;
     if (it.tag < 0) return;
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) r.x[t][q] = ldg_rows128(it.x[t] + 32 * q);
+    for (int q = 0; q < 4; ++q) r.x[q] = ldg_rows128(it.x + 32 * q);
 }
 
 // a value that the compiler keeps instead of working it out again
@@ -170,49 +166,47 @@ __device__ __forceinline__ void mma16_from(bool start, float (&d)[4], uint32_t a
 
 // What the units of an item share: x as B fragments, in the order of the products below, and its sums over the quantisation groups
 // (elements 2 and 3 repeat 0 and 1).
-template <int NT, int SUB>
+template <int SUB>
 struct ItemRows {
-    uint64_t xp[NT][4][2];
-    float xs[SUB][NT][4];
+    uint64_t xp[4][2];
+    float xs[SUB][4];
 };
 // IN_ORDER: x lies in memory as direct_column has it.  Else its words change places, by multiplications with `one` = 1 that the
 // compiler cannot see through: as plain moves they are made anew for every unit (84 moves per item of four units instead of 16).
-template <int NT, int SUB, bool BF, bool IN_ORDER>
-__device__ __forceinline__ void prepare_rows(ItemRows<NT, SUB> &rows, const uint4 (&x)[NT][4], uint32_t one)
+template <int SUB, bool BF, bool IN_ORDER>
+__device__ __forceinline__ void prepare_rows(ItemRows<SUB> &rows, const uint4 (&x)[4], uint32_t one)
 {
     constexpr uint32_t ONES = BF ? 0x3f803f80u : 0x3c003c00u;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         const int sub = q * SUB / 4;
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const uint4 v = x[t][q];
-            if constexpr (BF || IN_ORDER) {
-                rows.xp[t][q][0] = register_pair(v.x, v.y);
-                rows.xp[t][q][1] = register_pair(v.z, v.w);
-            } else {
-                rows.xp[t][q][0] = register_pair(v.x * one, v.z * one);
-                rows.xp[t][q][1] = register_pair(v.y * one, v.w * one);
-            }
-            mma16_from<BF>(q * SUB % 4 == 0, rows.xs[sub][t], ONES, ONES, ONES, ONES, rows.xp[t][q][0]);
-            mma16<BF, false>(rows.xs[sub][t], ONES, ONES, ONES, ONES, rows.xp[t][q][1]);
+        const uint4 v = x[q];
+        if constexpr (BF || IN_ORDER) {
+            rows.xp[q][0] = register_pair(v.x, v.y);
+            rows.xp[q][1] = register_pair(v.z, v.w);
+        } else {
+            rows.xp[q][0] = register_pair(v.x * one, v.z * one);
+            rows.xp[q][1] = register_pair(v.y * one, v.w * one);
         }
+        mma16_from<BF>(q * SUB % 4 == 0, rows.xs[sub], ONES, ONES, ONES, ONES, rows.xp[q][0]);
+        mma16<BF, false>(rows.xs[sub], ONES, ONES, ONES, ONES, rows.xp[q][1]);
     }
 }
 
-// acc[u][t][i], u = U0, U0 + 1: column g + 8 (i >> 1) of unit u, token 8 t + 2 t4 + (i & 1); `stage`: the pair's stage of the ring
-template <int U0, int NT, int NU, int SUB, bool BF>
-__device__ __forceinline__ void multiply_pair(uint32_t stage, int lane, uint32_t flags, const ItemRows<NT, SUB> &rows, float (&acc)[NU][NT][4])
+// acc[u][i], u = U0, U0 + 1: column g + 8 (i >> 1) of unit u, token 2 t4 + (i & 1); `stage`: the pair's stage of the ring
+template <int U0, int NU, int SUB, bool BF>
+__device__ __forceinline__ void multiply_pair(uint32_t stage, int lane, uint32_t flags, const ItemRows<SUB> &rows, float (&acc)[NU][4])
 {
     const uint32_t slot = stage + lane * 16, meta = stage + kPairW + (lane >> 2) * 4, zeros = stage + kPairW + 64 + (lane >> 2);
     constexpr uint32_t LO = 0x000f000fu, HI = 0x00f000f0u, MAGIC = 0x43004300u;
+    // fp16: sums and -z in units of 2^-24, which the scale makes good.  -z as a float: the nibble, or 16 times it, in the lowest bits of 2^23.
+    constexpr float kStep = BF ? 1.f : 5.9604645e-8f;
     const float z_add = (flags & kFormatZerosMinusOne) ? 1.f : 0.f;
-    // -z as floats: the nibble in the lowest bits of 2^23, or 16 z there
-    const float c_lo = 8388608.f - (BF ? 128.f : 0.f) - z_add, c_hi = 524288.f - (BF ? 128.f : 0.f) - z_add;
+    const float c_lo = (8388608.f - (BF ? 128.f : 0.f) - z_add) * kStep, c_hi = (524288.f - (BF ? 128.f : 0.f) - z_add) * kStep;
 #pragma unroll
     for (int u = U0; u < U0 + 2; ++u) {
         const uint4 wq[2] = {lds128(slot + (u - U0) * 2 * kUnitBytes), lds128(slot + (u - U0) * 2 * kUnitBytes + kUnitBytes)};
-        float lo[NT][4], hi[NT][4];
+        float lo[4], hi[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const int sub = q * SUB / 4;
@@ -223,49 +217,42 @@ __device__ __forceinline__ void multiply_pair(uint32_t stage, int lane, uint32_t
                                a3 = lop3_and_or(a >> 12, LO, MAGIC);
                 const uint32_t b0 = lop3_and_or(b, LO, MAGIC), b1 = lop3_and_or(b >> 4, LO, MAGIC), b2 = lop3_and_or(b >> 8, LO, MAGIC),
                                b3 = lop3_and_or(b >> 12, LO, MAGIC);
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    mma16_from<true>(start, lo[t], a0, b0, a1, b1, rows.xp[t][q][0]);
-                    mma16<true, false>(lo[t], a2, b2, a3, b3, rows.xp[t][q][1]);
-                }
+                mma16_from<true>(start, lo, a0, b0, a1, b1, rows.xp[q][0]);
+                mma16<true, false>(lo, a2, b2, a3, b3, rows.xp[q][1]);
             } else {
                 const uint32_t a8 = a >> 8, b8 = b >> 8;
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    mma16_from<false>(start, lo[t], a & LO, b & LO, a8 & LO, b8 & LO, rows.xp[t][q][0]);
-                    mma16_from<false>(start, hi[t], a & HI, b & HI, a8 & HI, b8 & HI, rows.xp[t][q][1]);
-                }
+                mma16_from<false>(start, lo, a & LO, b & LO, a8 & LO, b8 & LO, rows.xp[q][0]);
+                mma16_from<false>(start, hi, a & HI, b & HI, a8 & HI, b8 & HI, rows.xp[q][1]);
             }
             if ((q + 1) * SUB % 4 == 0) {           // last quarter of the group
-                const float2 sf = pair_to_float2<BF>(lds32(meta + sub * kPairMeta + (u - U0) * 32));
+                float2 sf = pair_to_float2<BF>(lds32(meta + sub * kPairMeta + (u - U0) * 32));
+                if constexpr (!BF) sf.x *= 16777216.f, sf.y *= 16777216.f;
                 const uint32_t zz = lds8(zeros + sub * kPairMeta + (u - U0) * 8);
-                const float za = c_lo - __uint_as_float((zz & 15u) | 0x4b000000u);
-                const float zb = fmaf(__uint_as_float((zz & 0xf0u) | 0x4b000000u), -0.0625f, c_hi);
+                const float za = fmaf(__uint_as_float((zz & 15u) | 0x4b000000u), -kStep, c_lo);
+                const float zb = fmaf(__uint_as_float((zz & 0xf0u) | 0x4b000000u), -0.0625f * kStep, c_hi);
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        float v = lo[t][i];
-                        if constexpr (!BF) v = fmaf(hi[t][i], 1048576.f, v * 16777216.f);
-                        v = fmaf(i < 2 ? za : zb, rows.xs[sub][t][i & 1], v);
-                        acc[u][t][i] = fmaf(i < 2 ? sf.x : sf.y, v, acc[u][t][i]);
-                    }
+                for (int i = 0; i < 4; ++i) {
+                    float v = lo[i];
+                    if constexpr (!BF) v = fmaf(hi[i], 0.0625f, v);
+                    v = fmaf(i < 2 ? za : zb, rows.xs[sub][i & 1], v);
+                    acc[u][i] = fmaf(i < 2 ? sf.x : sf.y, v, acc[u][i]);
+                }
             }
         }
     }
 }
 
-// Works through the items that `next` yields (it fills a DirectItem, tag < 0 at the end); `ready()` is called once,
-// between the first requests for weights and the first for activations, `before(tag)` ahead of each item's product.  `ring`: the warp's part of the ring.
+// Works through the items that `next` yields (it fills a DirectItem, tag < 0 at the end).  `ready()` is called once, between the first
+// requests for weights and the first for activations, `before(tag)` ahead of each item's product.  `ring`: the warp's part of the ring.
 // A stage is filled again a pair after it was read: the reads are over.
-template <int NT, int NU, bool GATE_UP, int SUB, bool BF, bool IN_ORDER, typename Next, typename Ready, typename Before>
-__device__ __forceinline__ void stream_items(uint32_t ring, int lane, uint32_t one, float (&acc)[NU][NT][4], Next next, Ready ready, Before before)
+template <int NU, bool GATE_UP, int SUB, bool BF, bool IN_ORDER, typename Next, typename Ready, typename Before>
+__device__ __forceinline__ void stream_items(uint32_t ring, int lane, uint32_t one, float (&acc)[NU][4], Next next, Ready ready, Before before)
 {
     static_assert(NU == 2 || NU == 4, "one or two pairs of units");
     constexpr int NP = NU / 2, kStages = NP + 2;
     constexpr uint32_t kStage = direct_stage_bytes<SUB>(), kEnd = kStages * kStage;
-    DirectItem<NT, SUB> it{};
-    DirectRows<NT> x;
+    DirectItem<SUB> it{};
+    DirectRows x;
     const int zl = SUB == 4 ? lane : lane - 8 * SUB;
     const uint32_t m_at = kept(kPairW + (SUB == 4 || lane < 8 * SUB ? (lane >> 3) * kPairMeta + (lane & 7) * 8 : (zl >> 1) * kPairMeta + 64 + (zl & 1) * 8));
     const uint32_t w_at = kept(lane * 16);
@@ -290,30 +277,30 @@ __device__ __forceinline__ void stream_items(uint32_t ring, int lane, uint32_t o
     next(it);
 #pragma unroll
     for (int p = 0; p < NP; ++p) copy_pair(p);
-    const DirectItem<NT, SUB> first = it;
+    const DirectItem<SUB> first = it;
     next(it);
     copy_pair(0);
     ready();
-    load_rows<NT, SUB>(x, first);
+    load_rows<SUB>(x, first);
     while (x.tag >= 0) {
         before(x.tag);
-        ItemRows<NT, SUB> rows;
-        prepare_rows<NT, SUB, BF, IN_ORDER>(rows, x.x, one);
+        ItemRows<SUB> rows;
+        prepare_rows<SUB, BF, IN_ORDER>(rows, x.x, one);
         const uint32_t flags = x.flags;
         const int pairs = x.pairs;
-        load_rows<NT, SUB>(x, it);
+        load_rows<SUB>(x, it);
         if constexpr (NP == 2) {
             copy_pair(1);
             cp_async_wait<NP + 1>();
             __syncwarp();      // (the scales and zero points are other lanes' copies)
-            multiply_pair<0, NT, NU, SUB, BF>(ring + at, lane, flags, rows, acc);
+            multiply_pair<0, NU, SUB, BF>(ring + at, lane, flags, rows, acc);
             advance(at);
         }
         next(it);
         copy_pair(0);
         cp_async_wait<NP + 1>();
         __syncwarp();
-        if (NP == 1 || pairs == NP) multiply_pair<NU - 2, NT, NU, SUB, BF>(ring + at, lane, flags, rows, acc);
+        if (NP == 1 || pairs == NP) multiply_pair<NU - 2, NU, SUB, BF>(ring + at, lane, flags, rows, acc);
         advance(at);
     }
 }

@@ -304,7 +304,7 @@ lora_gemm_kernel(const LoraArgs a, const __half *x, const uint8_t *qweight, cons
     if (threadIdx.x < 8) s_ids[threadIdx.x] = (int)threadIdx.x < a.M ? __ldg(a.ids + threadIdx.x) : -1;
     __syncthreads();
     pdl_launch_dependents();
-    const __half *rows[1] = {x + (size_t)min(g, a.M - 1) * a.K + 8 * t4};
+    const __half *row = x + (size_t)min(g, a.M - 1) * a.K + 8 * t4;
     // the rows of B that the epilogue will want, on their way to L2
     for (int i = threadIdx.x; i < a.M * (t1 - t0) * 32; i += kThreads) {
         const int id = s_ids[i % a.M];
@@ -314,7 +314,7 @@ lora_gemm_kernel(const LoraArgs a, const __half *x, const uint8_t *qweight, cons
     }
     int l_pair = t0, l_next = t0, l_item = G, l_turn = warp - 1;
     LanePtrs<SUB> ptrs{};
-    auto next = [&](DirectItem<1, SUB> &it) {
+    auto next = [&](DirectItem<SUB> &it) {
         l_item += W;
         while (l_item >= G) {
             if (l_next >= t1) {
@@ -326,14 +326,14 @@ lora_gemm_kernel(const LoraArgs a, const __half *x, const uint8_t *qweight, cons
             l_item = ++l_turn & (W - 1);
             ptrs = lane_ptrs<false, SUB>(unit_ptrs<SUB>(qweight, scales, qzeros, l_pair >> 2, G, 2 * (l_pair & 3)), lane);
         }
-        set_item<1, SUB>(it, ptrs, rows, l_item, lane);
+        set_item<SUB>(it, ptrs, row, l_item, lane);
         it.flags = flags;
         it.tag = l_pair;
         it.pairs = l_next - l_pair;
     };
     const bool layout_ok = (flags & kFormatGateUp) == 0 && ((flags & kFormatBf16) != 0) == BF;
     if (!layout_ok && threadIdx.x == 0) atomicMax(&g_device_status, (int)kStatusLayoutMismatch);
-    float acc[NU][1][4] = {};
+    float acc[NU][4] = {};
     int pair = t0, left = t0, tiles = 0;      // the tile at hand, the one before it, how many came before
     auto add_up = [&]() {
         const int done = tiles - 1;
@@ -381,8 +381,8 @@ lora_gemm_kernel(const LoraArgs a, const __half *x, const uint8_t *qweight, cons
         for (int u = 0; u < NU; ++u)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                buf[(warp * kValues + 4 * u + i) * 32 + lane] = acc[u][0][i];
-                acc[u][0][i] = 0.f;
+                buf[(warp * kValues + 4 * u + i) * 32 + lane] = acc[u][i];
+                acc[u][i] = 0.f;
             }
         __syncwarp();
         if (lane == 0) mbar_arrive(bars + 8 * (tiles & 1));
@@ -391,7 +391,7 @@ lora_gemm_kernel(const LoraArgs a, const __half *x, const uint8_t *qweight, cons
         ++tiles;
     };
     const uint32_t ring = smem_u32(red + 2 * W * kValues * 32) + warp * direct_ring_bytes<NU, SUB>(1);
-    stream_items<1, NU, false, SUB, BF, false>(ring, lane, a.one, acc, next, [] {}, [&](int t) { while (pair < t) finish_tile(); });
+    stream_items<NU, false, SUB, BF, false>(ring, lane, a.one, acc, next, [] {}, [&](int t) { while (pair < t) finish_tile(); });
     while (pair < t1) finish_tile();
     if (tiles) add_up();
 }

@@ -94,6 +94,7 @@ int launch_route(const void *logits, int type, int32_t *ids, float *weights, int
 
 // ------------------------------------------------------------------------------ the experts' MLP
 constexpr int kMoeMaxRows = 64;                 // tokens of one pass
+constexpr int kMoeSegRows = 8;                   // rows of a segment (see SlotPlan): the columns of an MMA
 constexpr int kMoeWarps = 8, kMoeThreads = 32 * kMoeWarps;
 constexpr int kMoeCtasPerSm = 2;
 constexpr int kMoeMaxExperts = 1024, kMoeMaxTopK = 32;
@@ -339,11 +340,11 @@ __device__ __forceinline__ int build_slot_plan(const MoeArgs &a, int R, const Sl
 // CTA takes a range of neighbouring units, in tiles of two where they are a pair of the panel, else of one.  The warps share a
 // tile's items along K; at its end each leaves its sums in shared memory, goes on with the next tile, and adds up its part of them at
 // the next tile's end, when all have long arrived.
-template <int NT, int NU, int SUB, bool BF>
+template <int NU, int SUB, bool BF>
 __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_gate_up_kernel(const MoeArgs a)
 {
     extern __shared__ __align__(16) uint8_t smem[];
-    constexpr int kValues = 4 * NU * NT;
+    constexpr int kValues = 4 * NU;
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
     const SlotPlan plan = slot_plan_view(smem, a.M * a.k, a.E);
     float *red = reinterpret_cast<float *>(smem + slot_plan_bytes(a.M * a.k, a.E));
@@ -355,7 +356,7 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_gate_up_kernel
     }
     pdl_wait();
     pdl_launch_dependents();
-    const int segments = build_slot_plan(a, 8 * NT, plan, reinterpret_cast<unsigned short *>(red));
+    const int segments = build_slot_plan(a, kMoeSegRows, plan, reinterpret_cast<unsigned short *>(red));
     const int G = a.K / kGroup, per_seg = a.F / 16, T = segments * per_seg;
     // the CTAs of an SM (which they are given out to in turn) take neighbouring ranges: the same rows of x
     int cta = blockIdx.x;
@@ -368,12 +369,12 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_gate_up_kernel
     int l_unit = t0, l_next = t0, l_item = G, l_seg = 0, l_col = 0, l_turn = warp - 1;
     uint32_t l_flags = 0;
     LanePtrs<SUB> ptrs{};
-    const __half *rows[NT];
+    const __half *row = nullptr;
     auto row_of = [&](int s) { return a.x + (size_t)(a.x_by_slot ? s : plan.token[s]) * a.K; };
     auto up_flags = [&](int e) {
         return __ldg(&reinterpret_cast<const TiledTrailer *>(a.gu_z + (size_t)(e + 1) * a.gu_z_bytes - kTrailerBytes)->flags);
     };
-    auto next = [&](DirectItem<NT, SUB> &it) {
+    auto next = [&](DirectItem<SUB> &it) {
         l_item += kMoeWarps;
         while (l_item >= G) {
             if (l_next >= t1) {
@@ -389,21 +390,20 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_gate_up_kernel
                 l_seg = start ? l_unit / per_seg : l_seg + 1;
                 l_col = start ? l_unit - l_seg * per_seg : 0;
                 const int first = plan.seg_begin[l_seg], count = plan.seg_begin[l_seg + 1] - first;
-#pragma unroll
-                for (int t = 0; t < NT; ++t) rows[t] = row_of(plan.slot[first + (8 * t + g < count ? 8 * t + g : 0)]) + 8 * t4;
+                row = row_of(plan.slot[first + (g < count ? g : 0)]) + 8 * t4;
                 l_flags = up_flags(plan.seg_expert[l_seg]);
             }
             const int e = plan.seg_expert[l_seg];
             ptrs = lane_ptrs<true, SUB>(unit_ptrs<SUB>(a.gu_w + e * a.gu_w_bytes, a.gu_s + e * a.gu_s_bytes, a.gu_z + e * a.gu_z_bytes, l_col >> 2, G, l_col & 3), lane);
         }
-        set_item<NT, SUB>(it, ptrs, rows, l_item, lane);
+        set_item<SUB>(it, ptrs, row, l_item, lane);
         it.flags = l_flags;
         it.tag = l_unit;
         it.pairs = l_next - l_unit;
     };
 
     // ---- the end of a tile
-    float acc[NU][NT][4] = {};
+    float acc[NU][4] = {};
     // the tile at hand, the one before it (its segment and column), how many came before
     int unit = t0, seg_at = t0 / per_seg, col_at = t0 - seg_at * per_seg, left = t0, left_seg = 0, left_col = 0, tiles = 0;
     bool saw_nan = false;
@@ -413,15 +413,15 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_gate_up_kernel
         const int seg = left_seg, c0 = left_col * 16;
         const int first = plan.seg_begin[seg], count = plan.seg_begin[seg + 1] - first;
         const float *buf = red + (done & 1) * (kMoeWarps * kValues * 32);
-        for (int o = threadIdx.x; o < width(left) * (4 * NT * 32); o += kMoeThreads) {
-            const int v = o >> 5, p = v / (4 * NT), t = v / 4 % NT, i = v & 3;            // (lane of o = lane: the block is a multiple of a warp)
-            const int r = 8 * t + 2 * t4 + (i & 1), at = (8 * NT * p + 4 * t + i) * 32 + lane;
+        for (int o = threadIdx.x; o < width(left) * 128; o += kMoeThreads) {
+            const int v = o >> 5, p = v >> 2, i = v & 3;            // (lane of o = lane: the block is a multiple of a warp)
+            const int r = 2 * t4 + (i & 1), at = (8 * p + i) * 32 + lane;
             if (r >= count) continue;
             float gate = 0.f, up = 0.f;
 #pragma unroll
             for (int w = 0; w < kMoeWarps; ++w) {
                 gate += buf[w * (kValues * 32) + at];
-                up += buf[w * (kValues * 32) + 4 * NT * 32 + at];
+                up += buf[w * (kValues * 32) + 128 + at];
             }
             saw_nan |= gate != gate || up != up;
             int col = c0 + 16 * p + g + 8 * (i >> 1);
@@ -436,12 +436,10 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_gate_up_kernel
 #pragma unroll
         for (int u = 0; u < NU; ++u)
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    buf[(warp * kValues + (u * NT + t) * 4 + i) * 32 + lane] = acc[u][t][i];
-                    acc[u][t][i] = 0.f;
-                }
+            for (int i = 0; i < 4; ++i) {
+                buf[(warp * kValues + 4 * u + i) * 32 + lane] = acc[u][i];
+                acc[u][i] = 0.f;
+            }
         __syncwarp();
         if (lane == 0) mbar_arrive(bars + 8 * (tiles & 1));
         left = unit, left_seg = seg_at, left_col = col_at;
@@ -451,7 +449,7 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_gate_up_kernel
         ++tiles;
     };
     const uint32_t ring = smem_u32(red + 2 * kMoeWarps * kValues * 32) + warp * direct_ring_bytes<NU, SUB>(1);
-    stream_items<NT, NU, true, SUB, BF, false>(ring, lane, a.one, acc, next, [] {}, [&](int t) { while (unit < t) finish_tile(); });
+    stream_items<NU, true, SUB, BF, false>(ring, lane, a.one, acc, next, [] {}, [&](int t) { while (unit < t) finish_tile(); });
     while (unit < t1) finish_tile();
     if (tiles) add_up();
     if (!saw_nan) return;
@@ -461,10 +459,10 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_gate_up_kernel
         const int first = plan.seg_begin[seg], count = plan.seg_begin[seg + 1] - first;
         const uint8_t *zeros = a.gu_z + e * a.gu_z_bytes;
         const uint32_t z_add = up_flags(e) & kFormatZerosMinusOne;
-        for (int o = threadIdx.x; o < width(unit) * (4 * NT * 32); o += kMoeThreads) {
-            const int v = o >> 5, r = 8 * (v / 4 % NT) + 2 * t4 + (v & 1), c = g + 8 * ((v >> 1) & 1);
+        for (int o = threadIdx.x; o < width(unit) * 128; o += kMoeThreads) {
+            const int v = o >> 5, r = 2 * t4 + (v & 1), c = g + 8 * ((v >> 1) & 1);
             if (r >= count) continue;
-            const int s = plan.slot[first + r], col = c0 + 16 * (v / (4 * NT)) + c;
+            const int s = plan.slot[first + r], col = c0 + 16 * (v >> 2) + c;
             __half *at = a.h + (size_t)s * a.F + direct_column<BF>(a.down_index ? __ldg(a.down_index + (size_t)e * a.F + col) : col);
             const float now = out16_to_float<BF>(*at);
             if (now == now) continue;
@@ -483,13 +481,13 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_gate_up_kernel
 // of all segments, one behind the other, are shared out evenly over its CTAs.  A CTA's part of a segment is what a tile is in
 // kernel 1; what its warps leave of it is added up, weighted, in a [token][column] tile in shared memory, part after part, and
 // the CTAs' tiles in the order of ranks: the order of all sums is fixed.
-template <int NT, int NU, int SUB, bool BF>
+template <int NU, int SUB, bool BF>
 __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_down_kernel(const MoeArgs a, int S)
 {
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ int s_bad;
     __shared__ __align__(8) uint64_t arrived[2];
-    constexpr int kCols = 16 * NU, kValues = 4 * NU * NT, R = 8 * NT;
+    constexpr int kCols = 16 * NU, kValues = 4 * NU;
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
     const int tile = blockIdx.x / S, rank = blockIdx.x - tile * S;
     const int G = a.F / kGroup, panel = tile / (8 / NU), unit = tile % (8 / NU) * NU;
@@ -507,7 +505,7 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_down_kernel(co
         mbar_init(bars + 8, kMoeWarps);
     }
     // ids and weights are older than the kernel before this one, which waited for them before it let this one in
-    const int segments = build_slot_plan(a, R, plan, reinterpret_cast<unsigned short *>(red));
+    const int segments = build_slot_plan(a, kMoeSegRows, plan, reinterpret_cast<unsigned short *>(red));
     if (S > 1) cluster_arrive_release();      // "this CTA has begun": waited for before anything is sent
     const int U = segments * G, u0 = share_begin(U, S, rank), u1 = share_begin(U, S, rank + 1);
     const int seg0 = u0 / G, parts = u1 > u0 ? (u1 - 1) / G - seg0 + 1 : 0;
@@ -516,11 +514,11 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_down_kernel(co
     int l_part = -1, l_item = G, l_end = 0;
     uint32_t l_flags = 0;
     LanePtrs<SUB> ptrs{};
-    const __half *rows[NT];
+    const __half *row = nullptr;
     auto trailer_flags = [](const uint8_t *zeros, size_t bytes, int e) {
         return __ldg(&reinterpret_cast<const TiledTrailer *>(zeros + (size_t)(e + 1) * bytes - kTrailerBytes)->flags);
     };
-    auto next = [&](DirectItem<NT, SUB> &it) {
+    auto next = [&](DirectItem<SUB> &it) {
         l_item += kMoeWarps;
         while (l_item >= l_end) {
             if (++l_part >= parts) {
@@ -533,10 +531,9 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_down_kernel(co
             l_end = min(u1 - seg * G, G);
             l_flags = trailer_flags(a.dn_z, a.dn_z_bytes, e);
             ptrs = lane_ptrs<false, SUB>(unit_ptrs<SUB>(a.dn_w + e * a.dn_w_bytes, a.dn_s + e * a.dn_s_bytes, a.dn_z + e * a.dn_z_bytes, panel, G, unit), lane);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) rows[t] = a.h + (size_t)plan.slot[first + (8 * t + g < count ? 8 * t + g : 0)] * a.F + 8 * t4;
+            row = a.h + (size_t)plan.slot[first + (g < count ? g : 0)] * a.F + 8 * t4;
         }
-        set_item<NT, SUB>(it, ptrs, rows, l_item, lane);
+        set_item<SUB>(it, ptrs, row, l_item, lane);
         it.flags = l_flags;
         it.tag = l_part;
         it.pairs = NU / 2;
@@ -550,7 +547,7 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_down_kernel(co
     }
 
     // ---- the end of a part (see kernel 1)
-    float acc[NU][NT][4] = {};
+    float acc[NU][4] = {};
     int now = 0;
     auto add_up = [&](int done) {
         if (!mbar_wait(bars + 8 * (done & 1), (done >> 1) & 1)) return;
@@ -558,8 +555,8 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_down_kernel(co
         const float *buf = red + (done & 1) * (kMoeWarps * kValues * 32);
 #pragma unroll
         for (int o = threadIdx.x; o < kValues * 32; o += kMoeThreads) {
-            const int v = o >> 5, u = v / (4 * NT), t = v / 4 % NT, i = v & 3;
-            const int r = 8 * t + 2 * t4 + (i & 1);
+            const int v = o >> 5, u = v >> 2, i = v & 3;
+            const int r = 2 * t4 + (i & 1);
             if (r >= count) continue;
             float sum = 0.f;
 #pragma unroll
@@ -575,18 +572,16 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_down_kernel(co
 #pragma unroll
         for (int u = 0; u < NU; ++u)
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    buf[(warp * kValues + (u * NT + t) * 4 + i) * 32 + lane] = acc[u][t][i];
-                    acc[u][t][i] = 0.f;
-                }
+            for (int i = 0; i < 4; ++i) {
+                buf[(warp * kValues + 4 * u + i) * 32 + lane] = acc[u][i];
+                acc[u][i] = 0.f;
+            }
         __syncwarp();
         if (lane == 0) mbar_arrive(bars + 8 * (now & 1));
         ++now;
     };
     const uint32_t ring = smem_u32(red + 2 * kMoeWarps * kValues * 32) + warp * direct_ring_bytes<NU, SUB>(1);
-    stream_items<NT, NU, false, SUB, BF, true>(ring, lane, a.one, acc, next, [] { pdl_wait(); }, [&](int p) { while (now < p) finish_part(); });
+    stream_items<NU, false, SUB, BF, true>(ring, lane, a.one, acc, next, [] { pdl_wait(); }, [&](int p) { while (now < p) finish_part(); });
     while (now < parts) finish_part();
     if (parts) add_up(parts - 1);
 
@@ -676,23 +671,23 @@ inline size_t moe_workspace_need(int M, int K, int F, int k, int act_order)
 }
 
 constexpr int kHalfSmBytes = 227 * 1024 / 2 - 1024;      // of a CTA that shares its SM with another
-template <int NT, int NU, int SUB>
-static int moe_red_and_ring_bytes() { return 2 * kMoeWarps * 4 * NU * NT * 32 * 4 + direct_ring_bytes<NU, SUB>(kMoeWarps); }
+template <int NU, int SUB>
+static int moe_red_and_ring_bytes() { return 2 * kMoeWarps * 4 * NU * 32 * 4 + direct_ring_bytes<NU, SUB>(kMoeWarps); }
 
-template <int NT, int NU, int SUB, bool BF>
+template <int NU, int SUB, bool BF>
 static int launch_gate_up(const MoeArgs &a, int most, cudaStream_t s)
 {
     static int configured[64] = {};
-    const int smem = slot_plan_bytes(a.M * a.k, a.E) + moe_red_and_ring_bytes<NT, NU, SUB>();
-    const int st = ensure_direct_smem((const void *)moe_gate_up_kernel<NT, NU, SUB, BF>, configured, smem, kMoeCtasPerSm);
+    const int smem = slot_plan_bytes(a.M * a.k, a.E) + moe_red_and_ring_bytes<NU, SUB>();
+    const int st = ensure_direct_smem((const void *)moe_gate_up_kernel<NU, SUB, BF>, configured, smem, kMoeCtasPerSm);
     if (st) return st;
     const long long units = (long long)most * (a.F / 16), slots = kMoeCtasPerSm * a.sms;
-    return launch_dependent(moe_gate_up_kernel<NT, NU, SUB, BF>, dim3((unsigned)(units < slots ? units : slots)), kMoeThreads, (size_t)smem, 1, s, a);
+    return launch_dependent(moe_gate_up_kernel<NU, SUB, BF>, dim3((unsigned)(units < slots ? units : slots)), kMoeThreads, (size_t)smem, 1, s, a);
 }
-template <int NT, int NU, int SUB>
+template <int NU, int SUB>
 static int moe_down_smem(const MoeArgs &a, int S)
 {
-    return slot_plan_bytes(a.M * a.k, a.E) + (S > 1 ? 2 : 1) * a.M * 16 * NU * 4 + moe_red_and_ring_bytes<NT, NU, SUB>();
+    return slot_plan_bytes(a.M * a.k, a.E) + (S > 1 ? 2 : 1) * a.M * 16 * NU * 4 + moe_red_and_ring_bytes<NU, SUB>();
 }
 template <int NU>
 static int moe_down_cluster(const MoeArgs &a)
@@ -701,40 +696,40 @@ static int moe_down_cluster(const MoeArgs &a)
     while (S < 8 && a.K / (16 * NU) * S * 2 <= kMoeCtasPerSm * a.sms) S *= 2;
     return S;
 }
-template <int NT, int NU, int SUB, bool BF>
+template <int NU, int SUB, bool BF>
 static int launch_down(const MoeArgs &a, cudaStream_t s)
 {
     static int configured[64] = {};
     const int tiles = a.K / (16 * NU), S = moe_down_cluster<NU>(a);
-    int smem = moe_down_smem<NT, NU, SUB>(a, S);
+    int smem = moe_down_smem<NU, SUB>(a, S);
     // exactly as many CTAs per SM as it takes: with more room clusters pile up on some SMs and leave others empty
     const int per_sm = tiles * S <= a.sms ? 1 : kMoeCtasPerSm;
     const int pad = 227 * 1024 / (per_sm + 1) + 512;
     if (smem < pad) smem = pad;
-    const int st = ensure_direct_smem((const void *)moe_down_kernel<NT, NU, SUB, BF>, configured, smem, per_sm);
+    const int st = ensure_direct_smem((const void *)moe_down_kernel<NU, SUB, BF>, configured, smem, per_sm);
     if (st) return st;
-    return launch_dependent(moe_down_kernel<NT, NU, SUB, BF>, dim3((unsigned)(tiles * S)), kMoeThreads, (size_t)smem, S, s, a, S);
+    return launch_dependent(moe_down_kernel<NU, SUB, BF>, dim3((unsigned)(tiles * S)), kMoeThreads, (size_t)smem, S, s, a, S);
 }
-template <int NT, int SUB, bool BF>
-static int launch_moe_nt(const MoeArgs &a, cudaStream_t s)
+template <int SUB, bool BF>
+static int launch_moe_format(const MoeArgs &a, cudaStream_t s)
 {
-    const int P = a.M * a.k, R = 8 * NT, experts = a.E < P ? a.E : P;
+    const int P = a.M * a.k, R = kMoeSegRows, experts = a.E < P ? a.E : P;
     const int most = experts + P / R < P ? experts + P / R : P;      // segments: one per expert in use, one more per R slots
     constexpr int NU = SUB == 4 ? 2 : 4;
-    const int st = launch_gate_up<NT, NU, SUB, BF>(a, most, s);
+    const int st = launch_gate_up<NU, SUB, BF>(a, most, s);
     if (st) return st;
-    if (NU == 2 || moe_down_smem<NT, NU, SUB>(a, moe_down_cluster<NU>(a)) > kHalfSmBytes) return launch_down<NT, 2, SUB, BF>(a, s);
-    return launch_down<NT, NU, SUB, BF>(a, s);
+    if (NU == 2 || moe_down_smem<NU, SUB>(a, moe_down_cluster<NU>(a)) > kHalfSmBytes) return launch_down<2, SUB, BF>(a, s);
+    return launch_down<NU, SUB, BF>(a, s);
 }
 int launch_moe(const MoeArgs &a, int group_size, int bf16, cudaStream_t s)
 {
     switch ((bf16 ? 10 : 0) + kGroup / group_size) {
-    case 1: return launch_moe_nt<1, 1, false>(a, s);
-    case 2: return launch_moe_nt<1, 2, false>(a, s);
-    case 4: return launch_moe_nt<1, 4, false>(a, s);
-    case 11: return launch_moe_nt<1, 1, true>(a, s);
-    case 12: return launch_moe_nt<1, 2, true>(a, s);
-    default: return launch_moe_nt<1, 4, true>(a, s);
+    case 1: return launch_moe_format<1, false>(a, s);
+    case 2: return launch_moe_format<2, false>(a, s);
+    case 4: return launch_moe_format<4, false>(a, s);
+    case 11: return launch_moe_format<1, true>(a, s);
+    case 12: return launch_moe_format<2, true>(a, s);
+    default: return launch_moe_format<4, true>(a, s);
     }
 }
 

@@ -9,11 +9,9 @@ Plain implementations in 64 bits on the oracle's dequantised weights.  Tolerance
   All roundings are independent, so the rms error stays below u sqrt(y^2 + sum (w h d)^2) (three times its variance);
 * adapters: one rounding of y up to 8 rows; above, the adapters' part is rounded to 16 bits on its way to the fp32 sums, u |part|; above
   16, so is every scaled weight, u sum |x w|, rms u sqrt(sum (x w)^2).
-* up to 8 rows an adapter, sum (q - z) x is formed as sum q x - z sum x (bfloat16: sum (128 + q) x - (128 + z) sum x), both in fp32.
-  Rounding then goes by the larger products (q + z) |x| s (bfloat16: (256 + q + z) |x| s), but of a quantisation group of at most 128
-  rows alone, eight MMAs of 16 rows deep, as the difference is taken per group: at most 8 2^-23 of them, which for the 31 (287) that
-  they are at most is 8 * 31 (8 * 287) 2^-23 s sum |x| over the rows, 2^-15 (2^-11.8) of s sum |x| - below u of sum |x w| in both types
-  (mean |q - z| is 5.3), and as independent errors of the groups far below it in a sum.  It is counted as `sums`.
+* the experts' products and the fused adapter product form sum (q - z) x of a quantisation group as sum q x - z sum x (bfloat16:
+  sum (128 + q) x - (128 + z) sum x).  Each side is at most eight MMAs deep and sums to at most 15 (143) sum |x|, z sum x to 16 (144)
+  sum |x|: together at most 31 (287) sum |x|, off by at most 8 2^-23 of that.  `sums` counts it, times the scale.
 """
 import math
 
@@ -37,9 +35,9 @@ F32 = 2.0 ** -23
 
 
 def sums(dtype, x, w64):
-    """Bound of what forming sum (q - z) x as a difference adds: 8 2^-23 (31 or 287) s |x| per row, s <= |w| / |q - z|, of which the
-    mean over the rows is taken: |w| summed over a column is 5.3 s summed, within a tenth for 128 rows and more."""
-    return 8 * F32 * (287 if dtype == torch.bfloat16 else 31) / 4.5 * (x.double().abs() @ w64.abs())
+    """8 2^-23 (31 or 287) sum |x| s.  s is taken from sum |x| |w|, |w| = |q - z| s: for uniform nibbles the mean of |q - z| is 5.3, and
+    over the rows of a column (128 and more) its |x|-weighted mean stays above 3."""
+    return 8 * F32 * (287 if dtype == torch.bfloat16 else 31) / 3 * (x.double().abs() @ w64.abs())
 
 
 @pytest.fixture(scope="module")
@@ -252,6 +250,37 @@ def test_moe_top_32_of_many_experts(ws):
         moe.check(ws, x, ids, w, r)
 
 
+def test_moe_slots_beyond_the_table(ws):
+    """More slots times experts than the kernels count in a table: one warp sorts them."""
+    moe = Moe(128, 128, 150)
+    x, ids, w, r = moe.inputs(64, 32, "serial")
+    moe.check(ws, x, ids, w, r)
+
+
+def test_moe_experts_behind_4_gib(ws):
+    """Expert buffers longer than 32 bits of bytes; only those in use are ever written."""
+    K, F, E, use = 4096, 4096, 520, (3, 517)
+    up = [layer(K, 2 * F, wl.seed_for("far", e)) for e in use]
+    down = [layer(F, K, wl.seed_for("far-down", e)) for e in use]
+    near = Moe.__new__(Moe)
+    near.K, near.F, near.E, near.dtype = K, F, 2, torch.float16
+    near.up64, near.down64 = [l[2] for l in up], [l[2] for l in down]
+    near.up, near.down = H.upload_experts([l[0] for l in up], gate_up=True), H.upload_experts([l[0] for l in down])
+    assert near.up.qweight_t.shape[1] * E > 1 << 33 and near.down.qweight_t.shape[1] * E > 1 << 32
+    x, ids, w, r = near.inputs(3, 2, "far")
+    y = near.check(ws, x, ids, w, r)
+
+    def spread(d):
+        out = {n: torch.empty((E, getattr(d, n).shape[1]), dtype=torch.uint8, device="cuda") for n in ("qweight_t", "qzeros_t", "scales_t")}
+        for n, t in out.items():
+            for i, e in enumerate(use):
+                t[e] = getattr(d, n)[i]
+        return H.DeviceExperts(d.K, d.N, d.group_size, False, E, out["qweight_t"], out["qzeros_t"], out["scales_t"], None, None)
+
+    far_ids = torch.tensor(use, dtype=torch.int32, device="cuda")[ids.long()]
+    assert torch.equal(H.moe_mlp(x, far_ids, w, spread(near.up), spread(near.down), r), y)
+
+
 def test_moe_buffers_may_be_shared(ws):
     moe = Moe(256, 256, 4)
     for M in (3, 70):
@@ -376,6 +405,45 @@ def test_lora_formats(ws, M, group, act, minus_one, dtype):
     lora.check(ws, x, ids, lora.scales)
 
 
+@pytest.mark.parametrize("M,K,N", [(40, 256, 384), (48, 4096, 4480), (150, 384, 256), (20, 512, 128)])
+def test_lora_bf16_many_rows(ws, M, K, N):
+    """The residual of every matmul kernel for many rows, in bfloat16: K below 512, few panels and a long K, tiles of many rows."""
+    lora = Lora(K, N, 16, 3, dtype=torch.bfloat16)
+    x, ids = lora.inputs(M, "residual")
+    lora.check(ws, x, ids, lora.scales)
+
+
+def test_lora_infinite_activations(ws):
+    """An infinity in x gives what the product gives: infinities of the weights' signs (NaN where q = z), and in its own row only."""
+    lora = Lora(512, 256, 16, 3)
+    for M in (1, 5, 8):
+        x, ids = lora.inputs(M, "inf")
+        ids[M - 1] = -1
+        want = lora.check(ws, x, ids, lora.scales)
+        x[M - 1, 33] = math.inf
+        y = H.gemm_lora(x, lora.D, lora.a, lora.b, ids, lora.scales)
+        assert torch.equal(y[:M - 1], want[:M - 1])
+        row = lora.w64[33]
+        assert torch.equal(y[M - 1][row != 0].double(), math.inf * row[row != 0].sign())
+        assert y[M - 1][row == 0].isnan().all() and (row == 0).any()
+
+
+def test_lora_adapter_of_infinities_stays_with_its_rows(ws):
+    lora = Lora(512, 256, 16, 4)
+    for M in (6, 14, 40, 100):
+        x, ids = lora.inputs(M, "bad")
+        ids[ids == 2] = 1
+        want = lora.check(ws, x, ids, lora.scales)
+        rows = torch.arange(M, device="cuda") % 3 == 1
+        a, b = lora.a[2].clone(), lora.b[2].clone()
+        lora.a[2, :, ::7], lora.b[2] = math.nan, math.inf
+        ids[rows] = 2
+        y = H.gemm_lora(x, lora.D, lora.a, lora.b, ids, lora.scales)
+        lora.a[2], lora.b[2] = a, b
+        assert torch.equal(y[~rows], want[~rows])
+        assert y[rows].isnan().all()
+
+
 def test_lora_presorted(ws):
     lora = Lora(512, 256, 16, 3, act=True)
     for M in (4, 33):
@@ -471,6 +539,41 @@ def test_together_eager_stream_and_graph(ws, M, dtype):
         for _ in range(3):
             graph.replay()
         assert torch.equal(out, want2)
+    assert B.gptq_check_status() == B.GPTQ_OK
+
+
+def test_two_streams_with_scratch_of_their_own(ws):
+    """Calls that run at the same time, each captured with a workspace of its own registered."""
+    moe, lora = Moe(512, 512, 8), Lora(512, 640, 16, 4)
+    x, ids, w, r = moe.inputs(9, 2, "streams")
+    xl, il = lora.inputs(30, "streams")
+    H.ensure_for_moe(ws, 9, moe.up, 2)
+    H.ensure_for_lora(ws, 30, lora.D, 16)
+    want, want_l = H.moe_mlp(x, ids, w, moe.up, moe.down, r), H.gemm_lora(xl, lora.D, lora.a, lora.b, il, lora.scales)
+    graphs, outs = [], []
+    for k in range(2):
+        mine = H.WorkspaceHolder()
+        H.ensure_for_moe(mine, 9, moe.up, 2)
+        mine.ensure(max(mine.buf.numel(), B.gptq_lora_workspace_bytes(30, 640, 512, 128, 0, 16)))
+        y, yl = torch.empty_like(x), torch.empty_like(want_l)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            for _ in range(3):
+                H.moe_mlp(x, ids, w, moe.up, moe.down, r, y)
+                H.gemm_lora(xl, lora.D, lora.a, lora.b, il, lora.scales, yl)
+        graphs.append((g, mine))
+        outs.append((y, yl))
+    side = [torch.cuda.Stream() for _ in range(2)]
+    for s in side:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(20):
+        for (g, _mine), s in zip(graphs, side):
+            with torch.cuda.stream(s):
+                g.replay()
+    torch.cuda.synchronize()
+    for y, yl in outs:
+        assert torch.equal(y, want) and torch.equal(yl, want_l)
+    ws.ensure(1)
     assert B.gptq_check_status() == B.GPTQ_OK
 
 

@@ -58,6 +58,7 @@ LORA_POINTERS = ["x", "qw", "qz", "sc", "g_idx", "a", "b", "ids", "scales", "y"]
 def test_lora_refusals(fn):
     def call(**kw):
         p = {n: A16 for n in LORA_POINTERS}
+        p["y"] += 16
         s = dict(M=2, N=256, K=512, group=128, act=1, rank=16, adapters=4)
         for n, v in kw.items():
             (p if n in p else s)[n] = v
@@ -69,7 +70,7 @@ def test_lora_refusals(fn):
         assert call(**{name: A16 + 8}) == B.GPTQ_ERR_ALIGN, name
     for bad in (dict(M=0), dict(K=516), dict(N=260 + 1), dict(rank=0), dict(adapters=0), dict(group=0)):
         assert call(**bad) == B.GPTQ_ERR_SHAPE, bad
-    for bad in (dict(act=3), dict(act=-1)):
+    for bad in (dict(act=3), dict(act=-1), dict(y=A16)):      # (y = x)
         assert call(**bad) == B.GPTQ_ERR_LAYOUT, bad
     for bad in (dict(group=16), dict(N=192), dict(rank=12), dict(rank=264)):
         assert call(**bad) == B.GPTQ_ERR_UNSUPPORTED, bad
