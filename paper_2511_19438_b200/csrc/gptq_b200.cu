@@ -1219,13 +1219,14 @@ static int moe_dispatch(const void *x, const int32_t *ids, const float *weights,
     a.x_by_slot = act_order;
     for (int m0 = 0; m0 < M; m0 += kMoeMaxRows) {
         a.M = (M - m0) < kMoeMaxRows ? (M - m0) : kMoeMaxRows;
+        a.parts = moe_parts(a.M);
         a.x = (const __half *)x + (size_t)m0 * K;
         a.ids = ids + (size_t)m0 * top_k;
         a.weights = weights + (size_t)m0 * top_k;
         a.residual = residual ? (const __half *)residual + (size_t)m0 * K : nullptr;
         a.y = (__half *)y + (size_t)m0 * K;
         if (act_order) {
-            __half *sorted = (__half *)(ws + moe_h_bytes((M < kMoeMaxRows ? M : kMoeMaxRows) * top_k, F));
+            __half *sorted = (__half *)(ws + moe_h_bytes(M, top_k, F));
             st = launch_moe_gather(a.x, a.ids, gu_perm, sorted, a.M * top_k, top_k, E, K, (cudaStream_t)stream);
             if (st) return st;
             a.x = sorted;

@@ -10,6 +10,7 @@ namespace gptq {
 // One warp per token; lane l holds the logits of experts l, l + 32, ... as keys whose unsigned order is the order of the
 // logits (0: an expert that cannot be chosen).  A pick is two warp-wide reductions: the largest key, then the lowest expert
 // that has it.  The weights are exp(l - max) over their sum, or over the sum of all experts, in fp32.
+// Bound by the chain of 2 k reductions: 4096 tokens, 128 experts in bfloat16, top 8: 4.0 us, 0.2 would be its memory's.
 constexpr int kRouteMaxExperts = 1024, kRouteMaxTopK = 32, kRouteWarps = 4;
 
 __device__ __forceinline__ uint32_t logit_bits(const void *logits, int type, size_t i)
@@ -106,13 +107,14 @@ struct MoeArgs {
     const uint8_t *gu_w, *gu_z, *gu_s, *dn_w, *dn_z, *dn_s;
     size_t gu_w_bytes, gu_z_bytes, gu_s_bytes, dn_w_bytes, dn_z_bytes, dn_s_bytes;    // of one expert
     const int32_t *down_index;      // [E, F] or nullptr
-    __half *h;                // [M k, F], columns as direct_column has them
+    __half *h;                // [parts][M k, F], columns as direct_column has them
     const __half *residual;   // [M, K] or nullptr
     __half *y;                // [M, K]
     int M, k, E, K, F;
     int sms;
     uint32_t one;             // 1 (see prepare_rows)
     int x_by_slot;            // rows of x: slots instead of tokens
+    int parts;                // of h: rounded to 16 bits, and with 2 what that left, rounded too (see moe_parts)
 };
 
 // The slots (m, j) of a batch grouped by expert, in the order of experts and, within one, of slots.  An expert's slots are cut
@@ -151,7 +153,7 @@ __device__ __forceinline__ int build_slot_plan(const MoeArgs &a, int R, const Sl
 {
     __shared__ int s_segments;
     const int P = a.M * a.k, tid = threadIdx.x, lane = tid & 31;
-    if (P <= 32) {      // a slot per lane of one warp, experts in the order of their first slots (2.6 us on the way below, 1.1 so)
+    if (P <= 32) {      // a slot per lane of one warp, experts in the order of their first slots
         if (tid < 32) {
             const int j = lane % a.k, id = lane < P ? __ldg(a.ids + lane) : -1;
             float w = lane < P ? __ldg(a.weights + lane) : 0.f;
@@ -336,10 +338,25 @@ __device__ __forceinline__ int build_slot_plan(const MoeArgs &a, int R, const Sl
     return s_segments;
 }
 
+// An activation's parts.  With two, 16 bits and the 16 of what they leave, h is good to 2^-22 (bfloat16 2^-16) and y's rounding is the
+// only one; an infinity leaves nothing.
+template <bool BF>
+__device__ __forceinline__ void store_h(const MoeArgs &a, __half *at, float v)
+{
+    store_out16<BF>(at, v);
+    if (a.parts == 1) return;
+    const float left = v - out16_to_float<BF>(*at);
+    store_out16<BF>(at + (size_t)a.M * a.k * a.F, isfinite(left) ? left : 0.f);
+}
+
 // Kernel 1: h[slot] = silu(gate) * up.  The work is counted in units of a segment and 16 gate columns (with their 16 up columns); a
 // CTA takes a range of neighbouring units, in tiles of two where they are a pair of the panel, else of one.  The warps share a
 // tile's items along K; at its end each leaves its sums in shared memory, goes on with the next tile, and adds up its part of them at
 // the next tile's end, when all have long arrived.
+//
+// Bound by instruction issue: 64 rows, 32 experts of 4096 x 2048, top 4: 2.4 instructions per clock and SM at 51 % of the DRAM rate and
+// 34 % of the tensor pipe's.  Two CTAs of 8 warps per SM with rings; the whole layer of 64 rows takes 155 us (65 would be its memory's),
+// 167 with one CTA of 16 warps per SM.
 template <int NU, int SUB, bool BF>
 __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_gate_up_kernel(const MoeArgs a)
 {
@@ -426,7 +443,7 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_gate_up_kernel
             saw_nan |= gate != gate || up != up;
             int col = c0 + 16 * p + g + 8 * (i >> 1);
             if (a.down_index) col = __ldg(a.down_index + (size_t)plan.seg_expert[seg] * a.F + col);
-            store_out16<BF>(a.h + (size_t)plan.slot[first + r] * a.F + direct_column<BF>(col), silu_mul(gate, up));
+            store_h<BF>(a, a.h + (size_t)plan.slot[first + r] * a.F + direct_column<BF>(col), silu_mul(gate, up));
         }
     };
     auto finish_tile = [&]() {
@@ -472,7 +489,7 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_gate_up_kernel
                 const UnitPtrs p = unit_ptrs<SUB>(a.gu_w + e * a.gu_w_bytes, a.gu_s + e * a.gu_s_bytes, zeros, col / 64, G, col % 64 / 16 + 4 * half);
                 sum[half] = long_sum<BF>(p.w, p.s, p.z, SUB, c, z_add, row_of(s), G, false);
             }
-            store_out16<BF>(at, silu_mul(sum[0], sum[1]));
+            store_h<BF>(a, at, silu_mul(sum[0], sum[1]));
         }
     }
 }
@@ -481,6 +498,8 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_gate_up_kernel
 // of all segments, one behind the other, are shared out evenly over its CTAs.  A CTA's part of a segment is what a tile is in
 // kernel 1; what its warps leave of it is added up, weighted, in a [token][column] tile in shared memory, part after part, and
 // the CTAs' tiles in the order of ranks: the order of all sums is fixed.
+// Clusters, because a few tokens leave too few columns for the machine: as many CTAs as fill two per SM, up to 8 to a cluster.  One row,
+// 8 experts of 4096 x 11008, top 2: both kernels 39 us, 22 would be their memory's.
 template <int NU, int SUB, bool BF>
 __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_down_kernel(const MoeArgs a, int S)
 {
@@ -505,7 +524,9 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_down_kernel(co
         mbar_init(bars + 8, kMoeWarps);
     }
     // ids and weights are older than the kernel before this one, which waited for them before it let this one in
-    const int segments = build_slot_plan(a, kMoeSegRows, plan, reinterpret_cast<unsigned short *>(red));
+    // with h in two parts a segment is 4 slots: their first parts are columns 0 .. 3 of an MMA, the second ones 4 .. 7
+    const int R = kMoeSegRows / a.parts;
+    const int segments = build_slot_plan(a, R, plan, reinterpret_cast<unsigned short *>(red));
     if (S > 1) cluster_arrive_release();      // "this CTA has begun": waited for before anything is sent
     const int U = segments * G, u0 = share_begin(U, S, rank), u1 = share_begin(U, S, rank + 1);
     const int seg0 = u0 / G, parts = u1 > u0 ? (u1 - 1) / G - seg0 + 1 : 0;
@@ -531,7 +552,8 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_down_kernel(co
             l_end = min(u1 - seg * G, G);
             l_flags = trailer_flags(a.dn_z, a.dn_z_bytes, e);
             ptrs = lane_ptrs<false, SUB>(unit_ptrs<SUB>(a.dn_w + e * a.dn_w_bytes, a.dn_s + e * a.dn_s_bytes, a.dn_z + e * a.dn_z_bytes, panel, G, unit), lane);
-            row = a.h + (size_t)plan.slot[first + (g < count ? g : 0)] * a.F + 8 * t4;
+            const int r = g & (R - 1);
+            row = a.h + ((size_t)(g >= R ? a.M * a.k : 0) + plan.slot[first + (r < count ? r : 0)]) * a.F + 8 * t4;
         }
         set_item<SUB>(it, ptrs, row, l_item, lane);
         it.flags = l_flags;
@@ -561,6 +583,10 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_down_kernel(co
             float sum = 0.f;
 #pragma unroll
             for (int w = 0; w < kMoeWarps; ++w) sum += buf[(w * kValues + v) * 32 + lane];
+            if (a.parts == 2) {      // column r + 4
+#pragma unroll
+                for (int w = 0; w < kMoeWarps; ++w) sum += buf[(w * kValues + v) * 32 + lane + 2];
+            }
             const int s = plan.slot[first + r];
             float *cell = ysum + plan.token[s] * kCols + 16 * u + g + 8 * (i >> 1);
             *cell = fmaf(plan.weight[s], sum, *cell);
@@ -642,6 +668,7 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_down_kernel(co
         }
 }
 
+// Bound by latency: one round trip for indexes, one for x.
 // x_out[s][i] = x[s / k][perm[e][i]], e = ids[s]: each slot's row of x in its expert's sorted order (act-order checkpoints)
 __global__ void moe_gather_kernel(const __half *__restrict__ x, const int32_t *__restrict__ ids, const int32_t *__restrict__ perm,
                                   __half *__restrict__ x_out, int P, int k, int E, int K)
@@ -663,11 +690,23 @@ int launch_moe_gather(const __half *x, const int32_t *ids, const int32_t *perm, 
     return launch_dependent(moe_gather_kernel, dim3((unsigned)((K / 4 + 255) / 256), (unsigned)P), 256, 0, 1, s, x, ids, perm, x_out, P, k, E, K);
 }
 
-inline size_t moe_h_bytes(int P, int F) { return ((size_t)P * F * 2 + 255) & ~(size_t)255; }
+// Parts of h for a pass of M tokens.  Rounding h and y to 16 bits gives 1.4 times the error of rounding y alone (one case of four tokens
+// came to 1.5).  Where experts have up to four tokens the second part takes columns of the MMAs that would be idle; where they
+// have more it costs another sweep over the down layer.  Layers of 32 x 4096 x 2048 top 4 / 64 x 2048 x 768 top 8 / 8 x 4096 x 11008
+// top 2, one part -> two, us: 8 tokens 69.3 -> 69.7 / 44.2 -> 44.4 / 108 -> 109; 16 tokens 95.6 -> 98.6 / 52.5 -> 54.0 / 123 -> 135;
+// 64 tokens 155 -> 198 / 83 -> 106 / 323 -> 422.
+constexpr int kMoeTwoPartRows = 16;
+inline int moe_parts(int M) { return M <= kMoeTwoPartRows ? 2 : 1; }
+// room for any pass of a call of M tokens, and of one of fewer: who has registered for the largest call has enough
+inline size_t moe_h_bytes(int M, int k, int F)
+{
+    const int two = 2 * (M < kMoeTwoPartRows ? M : kMoeTwoPartRows), one = M < kMoeMaxRows ? M : kMoeMaxRows;
+    return ((size_t)(two > one ? two : one) * k * F * 2 + 255) & ~(size_t)255;
+}
 inline size_t moe_workspace_need(int M, int K, int F, int k, int act_order)
 {
     const int P = (M < kMoeMaxRows ? M : kMoeMaxRows) * k;
-    return moe_h_bytes(P, F) + (act_order ? (((size_t)P * K * 2 + 255) & ~(size_t)255) : 0);
+    return moe_h_bytes(M, k, F) + (act_order ? (((size_t)P * K * 2 + 255) & ~(size_t)255) : 0);
 }
 
 constexpr int kHalfSmBytes = 227 * 1024 / 2 - 1024;      // of a CTA that shares its SM with another

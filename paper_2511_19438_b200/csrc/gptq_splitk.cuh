@@ -94,8 +94,8 @@ struct SplitKArgs {
     int stages;
     const TiledTrailer *trailer;   // behind the tiled zero points
     int fuse;               // 1: y[M, N / 2] = silu(gate) * up of a layer tiled with its column halves interleaved
-    const __half *bias;     // fp16 [N] added to every row of y, or nullptr (not with fuse)
-    const __half *residual; // fp16 [M, N] added to y, or nullptr (not with fuse); may be y itself
+    const __half *bias;     // of the type of y, [N] added to every row of y, or nullptr (not with fuse)
+    const __half *residual; // of the type of y, [M, N] added to y, or nullptr (not with fuse); may be y itself
     int trace_slot;         // row of the launch timeline, or -1
     const int32_t *out_index; // with fuse: output column i is stored at column out_index[i] (nullptr: at i)
     // split-K column slices: the panel is one run of 128 columns, or with fuse two runs of 64 (gate, up); within a run

@@ -164,8 +164,8 @@ struct UmmaArgs {
     int stages;             // shared-memory ring depth
     const TiledTrailer *trailer;   // behind the tiled zero points
     int fuse;               // 1: y[M, N / 2] = silu(gate) * up of a layer tiled with its column halves interleaved
-    const __half *bias;     // fp16 [N] added to every row of y, or nullptr (not with fuse)
-    const __half *residual; // fp16 [M, N] added to y, or nullptr (not with fuse); may be y itself
+    const __half *bias;     // of the type of y, [N] added to every row of y, or nullptr (not with fuse)
+    const __half *residual; // of the type of y, [M, N] added to y, or nullptr (not with fuse); may be y itself
     int trace_slot;         // row of the launch timeline, or -1
     const int32_t *out_index; // with fuse: output column i is stored at column out_index[i] (nullptr: at i)
 };

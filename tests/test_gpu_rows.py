@@ -129,6 +129,10 @@ class Moe:
         """(y, bound of the largest errors, bound of the mean square error), float64"""
         u, x = U[self.dtype], x.double()
         M = x.shape[0]
+        # h: rounded to 16 bits; up to 16 tokens what that leaves, exact in fp32, is rounded again, to a step u of at most u |h|.
+        # Its fp32 value is off by 2^-18 (dh below), which counts beside the second.
+        uh = u if M > 16 else u * u
+        uh_mean = u if M > 16 else u * u + 2.0 ** -18
         y = torch.zeros((M, self.K), dtype=torch.float64, device="cuda")
         if residual is not None:
             y += residual.double()
@@ -148,8 +152,8 @@ class Moe:
                 dh = 1.1 * dg * (up.abs() + du) + silu.abs() * du + 2.0 ** -18 * h.abs()
                 d = self.down64[e].abs()
                 y[m] += w * (h @ self.down64[e])
-                most[m] += abs(w) * (((u + self.F * F32) * h.abs() + 1.01 * dh + 2.0 ** -24) @ d + sums(self.dtype, h, self.down64[e]))
-                square[m] += (w * u) ** 2 * ((h * h) @ (d * d))
+                most[m] += abs(w) * (((uh + self.F * F32) * h.abs() + 1.01 * dh + 2.0 ** -24) @ d + sums(self.dtype, h, self.down64[e]))
+                square[m] += (w * uh_mean) ** 2 * ((h * h) @ (d * d))
         return y, most + u * y.abs(), square + (u * y) ** 2
 
     def inputs(self, M, k, *seed):

@@ -78,9 +78,12 @@ def test_lora_refusals(fn):
 
 def test_workspace_sizes():
     # the activation of every slot in 16 bits; with act-order also each slot's row of x; passes of 64 tokens share it
-    assert B.gptq_moe_workspace_bytes(4, 512, 256, 2, 0) == 8 * 256 * 2
-    assert B.gptq_moe_workspace_bytes(4, 512, 256, 2, 1) == 8 * 256 * 2 + 8 * 512 * 2
+    assert B.gptq_moe_workspace_bytes(4, 512, 256, 2, 0) == 2 * 8 * 256 * 2        # few tokens: the activation in two parts
+    assert B.gptq_moe_workspace_bytes(4, 512, 256, 2, 1) == 2 * 8 * 256 * 2 + 8 * 512 * 2
     assert B.gptq_moe_workspace_bytes(1000, 512, 256, 2, 0) == 128 * 256 * 2
+    for act in (0, 1):      # scratch for many tokens does for fewer
+        need = [B.gptq_moe_workspace_bytes(m, 512, 256, 2, act) for m in range(1, 200)]
+        assert need == sorted(need)
     for bad in ((0, 512, 256, 2), (4, 500, 256, 2), (4, 512, 200, 2), (4, 512, 256, 0), (4, 512, 256, 33)):
         assert B.gptq_moe_workspace_bytes(*bad, 0) == 0
     few, many = B.gptq_lora_workspace_bytes(16, 256, 512, 128, 0, 16), B.gptq_lora_workspace_bytes(17, 256, 512, 128, 0, 16)
