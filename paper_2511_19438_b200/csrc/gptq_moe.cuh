@@ -757,7 +757,13 @@ static int launch_moe_format(const MoeArgs &a, cudaStream_t s)
     constexpr int NU = SUB == 4 ? 2 : 4;
     const int st = launch_gate_up<NU, SUB, BF>(a, most, s);
     if (st) return st;
-    if (NU == 2 || moe_down_smem<NU, SUB>(a, moe_down_cluster<NU>(a)) > kHalfSmBytes) return launch_down<2, SUB, BF>(a, s);
+    // The down kernel: half the columns per cluster where that keeps two CTAs on an SM, where otherwise SMs were left without one (32 of
+    // 1024 x 512 top 4: one token 16.7 -> 12.2 us, 16 tokens 35 -> 23), and where a CTA has an item per warp at most, so that the smaller
+    // cluster counts for more than x read twice (60 of 2048 x 1408 top 4, one token: 15.8 -> 14.1, 64 of 2048 x 768 top 8: 16.1 -> 15.2).
+    // With more to do four units are ahead (32 of 4096 x 2048 top 4, one token: 23.4 against 24.1, 16 tokens 99 against 106).
+    const int S = moe_down_cluster<NU>(a);
+    const bool narrow = a.K / (16 * NU) * S <= a.sms || (long long)most * (a.F / kGroup) <= (long long)kMoeWarps * S;
+    if (NU == 2 || narrow || moe_down_smem<NU, SUB>(a, S) > kHalfSmBytes) return launch_down<2, SUB, BF>(a, s);
     return launch_down<NU, SUB, BF>(a, s);
 }
 int launch_moe(const MoeArgs &a, int group_size, int bf16, cudaStream_t s)
