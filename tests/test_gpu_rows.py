@@ -185,6 +185,23 @@ def test_moe(ws, M, K, F, E, k):
     moe.check(ws, x, ids, w, r)
 
 
+# the down kernel with 64 columns per cluster: enough columns and items, clusters of 8 (h in one part and in two), 4, 2 and 1
+@pytest.mark.parametrize("M,group,dtype", [(5, 128, torch.float16), (16, 64, torch.float16), (17, 128, torch.float16), (20, 64, torch.float16),
+                                           (5, 64, torch.bfloat16), (16, 128, torch.bfloat16), (17, 64, torch.bfloat16), (20, 128, torch.bfloat16)])
+def test_moe_wide_columns(ws, M, group, dtype):
+    moe = Moe(1280, 1024, 8, group, dtype=dtype)
+    x, ids, w, r = moe.inputs(M, 2, "wide", group)
+    moe.check(ws, x, ids, w, r)
+
+
+@pytest.mark.parametrize("M", [3, 18])
+@pytest.mark.parametrize("K,F", [(2432, 2176), (4864, 1280), (9600, 1280)])
+def test_moe_wide_columns_small_clusters(ws, M, K, F):
+    moe = Moe(K, F, 2)
+    x, ids, w, r = moe.inputs(M, 2, "clusters")
+    moe.check(ws, x, ids, w, r)
+
+
 @pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
 @pytest.mark.parametrize("group,act,minus_one", [(128, True, False), (64, False, True), (64, True, False), (32, False, False),
                                                  (32, True, True), (256, False, False)])
