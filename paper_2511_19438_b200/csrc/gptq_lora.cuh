@@ -140,16 +140,28 @@ __global__ void __launch_bounds__(kLoraThreads, 4) lora_shrink_kernel(const Lora
     }
 }
 
-// v[m][r .. r + 3], summed over the parts of K in their order
-__device__ __forceinline__ float4 lora_v4(const LoraArgs &a, int m, int r)
+// v[m][r .. r + 4 NV - 1], summed over the parts of K in their order; a batch of parts is requested before the first is added: a loop
+// over as many as there are waits for each in turn (4096 x 4096, rank 16, four parts, one row: 6.8 -> 6.3 us; 1000 rows 42.0 -> 41.1).
+constexpr int kLoraPartBatch = 4;
+template <int NV>
+__device__ __forceinline__ void lora_v(const LoraArgs &a, int m, int r, float4 (&v)[NV])
 {
-    float4 v = *reinterpret_cast<const float4 *>(a.v + (size_t)m * a.rank + r);
-#pragma unroll 4
-    for (int p = 1; p < a.k_parts; ++p) {
-        const float4 w = *reinterpret_cast<const float4 *>(a.v + ((size_t)p * a.M + m) * a.rank + r);
-        v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+    for (int p = 0; p < a.k_parts; p += kLoraPartBatch) {
+        float4 w[kLoraPartBatch][NV];
+#pragma unroll
+        for (int b = 0; b < kLoraPartBatch; ++b)
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                w[b][i] = p + b < a.k_parts ? *reinterpret_cast<const float4 *>(a.v + ((size_t)(p + b) * a.M + m) * a.rank + r + 4 * i)
+                                            : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int b = 0; b < kLoraPartBatch; ++b)
+#pragma unroll
+            for (int i = 0; i < NV; ++i) v[i].x += w[b][i].x, v[i].y += w[b][i].y, v[i].z += w[b][i].z, v[i].w += w[b][i].w;
     }
-    return v;
 }
 template <bool BF>
 __device__ __forceinline__ uint32_t pack16(float a, float b)
@@ -184,11 +196,9 @@ __global__ void __launch_bounds__(256, 4) lora_delta_rows_kernel(const LoraArgs 
 #pragma unroll
     for (int k = 0; k < kDeltaSteps; ++k)
         p[k] = c < cols && n0 + k * cols + c < n1 ? __ldg(b + k * (cols * pieces)) : make_uint4(0, 0, 0, 0);
-    float4 v0 = make_float4(0.f, 0.f, 0.f, 0.f), v1 = v0;
-    if (c < cols) {
-        v0 = lora_v4(a, m, 8 * piece);
-        v1 = lora_v4(a, m, 8 * piece + 4);
-    }
+    float4 v[2] = {};
+    if (c < cols) lora_v(a, m, 8 * piece, v);
+    const float4 v0 = v[0], v1 = v[1];
 #pragma unroll
     for (int k = 0; k < kDeltaSteps; ++k) {
         const float2 p0 = pair_to_float2<BF>(p[k].x), p1 = pair_to_float2<BF>(p[k].y), p2 = pair_to_float2<BF>(p[k].z), p3 = pair_to_float2<BF>(p[k].w);
@@ -203,7 +213,7 @@ __global__ void __launch_bounds__(256, 4) lora_delta_rows_kernel(const LoraArgs 
 
 // Prompts, runs of rows with one adapter: kDeltaRows rows and 256 columns per CTA, MMAs with the rows' v as the 16-row operand, in two
 // 16-bit parts (v = hi + lo to 2^-22, 2^-16 in bfloat16: the product is as good as fp32's next to the 16 bits of delta) that the CTA
-// prepares in shared memory, and eight rows of B as the columns.  1000 rows of 4096 x 4096 in five runs, rank 16: 42 us with the shrink
+// prepares in shared memory, and eight rows of B as the columns.  1000 rows of 4096 x 4096 in five runs, rank 16: 41 us with the shrink
 // kernel and the matmul, which alone takes 27.
 constexpr int kDeltaRows = 32, kDeltaTiles = 4;      // tiles: eight columns each, of a warp
 template <bool BF>
@@ -228,7 +238,9 @@ __global__ void __launch_bounds__(256, 2) lora_delta_runs_kernel(const LoraArgs 
     if (leads) load_b(p, __shfl_sync(0xffffffffu, my_id, __ffs(leads) - 1), 8 * t4);      // on its way while v is prepared
     for (int i = threadIdx.x; i < kDeltaRows * width / 4; i += 256) {
         const int row = i / (width / 4), r = 4 * (i - row * (width / 4));
-        const float4 v = row < count && r < a.rank ? lora_v4(a, m0 + row, r) : make_float4(0.f, 0.f, 0.f, 0.f);
+        float4 w[1] = {};
+        if (row < count && r < a.rank) lora_v(a, m0 + row, r, w);
+        const float4 v = w[0];
         const uint2 h = make_uint2(pack16<BF>(v.x, v.y), pack16<BF>(v.z, v.w));
         const float2 h0 = pair_to_float2<BF>(h.x), h1 = pair_to_float2<BF>(h.y);
         uint8_t *at = smem + row * pitch + 2 * r;
@@ -280,8 +292,9 @@ __global__ void __launch_bounds__(256, 2) lora_delta_runs_kernel(const LoraArgs 
 // The product with W of up to 8 rows, plus the expansion.  The work is counted in pairs of units, 32 columns; a CTA takes a range of
 // neighbouring ones, in tiles of two where they are half a panel, else of one.  As in the routed-expert kernels the warps share a
 // tile's items along K, leave their sums and go on, and add up at the next tile's end.  W: 8 warps, two CTAs per SM; where there is no
-// more than a pair of units for each SM, 16 warps and one (4096 x 4096, rank 16, one row: 6.7 us with the shrink kernel, 7.0 with 8 warps).
-// 8 rows of 8 adapters, 4096 x 12288: 13.1 us, bound by instruction issue; the shared matmul alone takes 8.5 in the decode kernel.
+// more than a pair of units for each SM, 16 warps and one (4096 x 4096, rank 16, one row, with the shrink kernel: 0.3 us
+// less, now 6.3).
+// 8 rows of 8 adapters, 4096 x 12288: 13.0 us, bound by instruction issue; the shared matmul alone takes 8.5 in the decode kernel.
 template <int W, int NU, int SUB, bool BF>
 __global__ void __launch_bounds__(32 * W, 16 / W)
 lora_gemm_kernel(const LoraArgs a, const __half *x, const uint8_t *qweight, const uint8_t *scales, const uint8_t *qzeros,
@@ -346,7 +359,9 @@ lora_gemm_kernel(const LoraArgs a, const __half *x, const uint8_t *qweight, cons
             pdl_wait();
             for (int i = 4 * threadIdx.x; i < a.M * a.rank; i += 4 * kThreads) {
                 const int m = i / a.rank, r = i - m * a.rank;
-                *reinterpret_cast<float4 *>(vs + m * v_pitch + r) = lora_v4(a, m, r);
+                float4 v[1];
+                lora_v(a, m, r, v);
+                *reinterpret_cast<float4 *>(vs + m * v_pitch + r) = v[0];
             }
             __syncthreads();
         }
