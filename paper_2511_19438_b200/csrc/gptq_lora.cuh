@@ -169,7 +169,8 @@ __device__ __forceinline__ uint32_t pack16(float a, float b)
     return (uint32_t)float_to_out16<BF>(a) | (uint32_t)float_to_out16<BF>(b) << 16;
 }
 
-// delta[m][n] = (v B^T)[m][n], 0 without an adapter.
+// delta[m][n] = (v B^T)[m][n], 0 without an adapter.  The ids and B are older than the shrink kernel, which waited for what was before it
+// when it let these kernels in: they are read while v is still being formed.
 //
 // Decode batches, every row with an adapter of its own: a column of B has rank / 8 pieces of 16 bytes; neighbouring lanes read
 // neighbouring pieces, multiply them with their 8 values of v, which they keep, and add up.  A warp takes a row and kDeltaSteps times the
@@ -180,7 +181,6 @@ template <bool BF>
 __global__ void __launch_bounds__(256, 4) lora_delta_rows_kernel(const LoraArgs a, __half *__restrict__ delta)
 {
     pdl_launch_dependents();
-    pdl_wait();
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int pieces = a.rank / 8, cols = 32 / pieces;      // (rank up to 256: at least one column)
     const int m = blockIdx.y, n0 = kDeltaSteps * cols * (8 * blockIdx.x + warp), n1 = min(n0 + kDeltaSteps * cols, a.N);
@@ -188,6 +188,7 @@ __global__ void __launch_bounds__(256, 4) lora_delta_rows_kernel(const LoraArgs 
     const int id = __ldg(a.ids + m), c = lane / pieces, piece = lane - c * pieces;
     __half *out = delta + (size_t)m * a.N;
     if ((unsigned)id >= (unsigned)a.adapters) {
+        pdl_wait();
         for (int n = n0 + lane; n < n1; n += 32) store_out16<BF>(out + n, 0.f);
         return;
     }
@@ -197,6 +198,7 @@ __global__ void __launch_bounds__(256, 4) lora_delta_rows_kernel(const LoraArgs 
     for (int k = 0; k < kDeltaSteps; ++k)
         p[k] = c < cols && n0 + k * cols + c < n1 ? __ldg(b + k * (cols * pieces)) : make_uint4(0, 0, 0, 0);
     float4 v[2] = {};
+    pdl_wait();
     if (c < cols) lora_v(a, m, 8 * piece, v);
     const float4 v0 = v[0], v1 = v[1];
 #pragma unroll
@@ -221,7 +223,6 @@ __global__ void __launch_bounds__(256, 2) lora_delta_runs_kernel(const LoraArgs 
 {
     extern __shared__ __align__(16) uint8_t smem[];
     pdl_launch_dependents();
-    pdl_wait();
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
     const int n0 = 8 * kDeltaTiles * (8 * blockIdx.x + warp), m0 = kDeltaRows * blockIdx.y, count = min(kDeltaRows, a.M - m0);
     const int width = (a.rank + 31) & ~31, pitch = 2 * width * 2 + 16;      // a row: hi, lo, 16 bytes against bank conflicts
@@ -236,6 +237,7 @@ __global__ void __launch_bounds__(256, 2) lora_delta_runs_kernel(const LoraArgs 
     };
     uint4 p[kDeltaTiles] = {};
     if (leads) load_b(p, __shfl_sync(0xffffffffu, my_id, __ffs(leads) - 1), 8 * t4);      // on its way while v is prepared
+    pdl_wait();
     for (int i = threadIdx.x; i < kDeltaRows * width / 4; i += 256) {
         const int row = i / (width / 4), r = 4 * (i - row * (width / 4));
         float4 w[1] = {};
