@@ -244,7 +244,8 @@ __device__ __forceinline__ void multiply_pair(uint32_t stage, int lane, uint32_t
 
 // Works through the items that `next` yields (it fills a DirectItem, tag < 0 at the end).  `ready()` is called once, between the first
 // requests for weights and the first for activations, `before(tag)` ahead of each item's product.  `ring`: the warp's part of the ring.
-// A stage is filled again a pair after it was read: the reads are over.
+// A copy goes to the stage that was read last.  A lane's weights are its own copies, but its scales and zero points are other lanes': the
+// warp meets behind each product, so that no lane refills a stage that another one still reads.
 template <int NU, bool GATE_UP, int SUB, bool BF, bool IN_ORDER, typename Next, typename Ready, typename Before>
 __device__ __forceinline__ void stream_items(uint32_t ring, int lane, uint32_t one, float (&acc)[NU][4], Next next, Ready ready, Before before)
 {
@@ -294,6 +295,7 @@ __device__ __forceinline__ void stream_items(uint32_t ring, int lane, uint32_t o
             cp_async_wait<NP + 1>();
             __syncwarp();      // (the scales and zero points are other lanes' copies)
             multiply_pair<0, NU, SUB, BF>(ring + at, lane, flags, rows, acc);
+            __syncwarp();
             advance(at);
         }
         next(it);
@@ -301,6 +303,7 @@ __device__ __forceinline__ void stream_items(uint32_t ring, int lane, uint32_t o
         cp_async_wait<NP + 1>();
         __syncwarp();
         if (NP == 1 || pairs == NP) multiply_pair<NU - 2, NU, SUB, BF>(ring + at, lane, flags, rows, acc);
+        __syncwarp();
         advance(at);
     }
 }

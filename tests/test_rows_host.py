@@ -1,5 +1,8 @@
 """Argument checks of the operators whose rows choose their weights (routing, routed experts, adapters): no GPU needed, nothing
 is launched."""
+import os
+import re
+
 import pytest
 
 from paper_2511_19438_b200 import build as libbuild
@@ -92,3 +95,22 @@ def test_workspace_sizes():
     assert B.gptq_lora_workspace_bytes(16, 256, 512, 128, 2, 16) == few
     for bad in ((0, 256, 512, 128, 0, 16), (4, 200, 512, 128, 0, 16), (4, 256, 512, 128, 0, 12), (4, 256, 512, 16, 0, 16)):
         assert B.gptq_lora_workspace_bytes(*bad) == 0
+
+
+def test_a_ring_stage_is_refilled_behind_the_whole_warps_reads():
+    """stream_items copies into the stage that was read last.  Scales and zero points in it are read by other lanes than those that copied
+    them, so that between a product and the next copy the warp has to meet.  Followed through two turns of the loop in the source."""
+    source = os.path.join(os.path.dirname(libbuild.CSRC), "csrc", "gptq_direct.cuh")
+    body = re.sub(r"//[^\n]*", "", open(source).read())
+    body = body[body.index("stream_items("):body.index("long_sum(")]
+    loop = body[body.index("while (x.tag >= 0)"):]
+    steps = re.findall(r"multiply_pair<|copy_pair\(\d\)|__syncwarp\(\)", loop) * 2
+    assert sum(s.startswith("multiply") for s in steps) == 4 and sum(s.startswith("copy") for s in steps) == 4
+    read = False
+    for s in steps:
+        if s.startswith("multiply"):
+            read = True
+        elif s.startswith("__syncwarp"):
+            read = False
+        else:
+            assert not read, "a copy stands behind a product without a barrier of the warp between them"
