@@ -338,7 +338,7 @@ int gptq_moe_mlp_bf16(const void *x, const int32_t *expert_ids, const float *exp
  * act_order = 1 x and lora_a are in the checkpoint's row order, with GPTQ_ACT_ORDER_PRESORTED both are in the sorted one.
  * x A^T, scaled, is summed and kept in fp32.  Up to 8 rows the expansion joins the fp32 sums before the one rounding of y (two
  * kernels, three with act_order = 1; the products are those of gptq_gemm's one and two rows: sum q x and z sum x apart); above, it
- * is rounded to 16 bits on its way to them (two kernels and gptq_gemm's).  A row's result does not depend on the other rows'
+ * is rounded to 16 bits on its way to them (a value beyond 65504 becomes an infinity; two kernels and gptq_gemm's).  A row's result does not depend on the other rows'
  * adapters, whatever these hold.  y must not be x (GPTQ_ERR_LAYOUT).  Scratch: gptq_lora_workspace_bytes of the registered workspace, always needed,
  * under the rules of gptq_set_workspace.  A layer tiled with GPTQ_FORMAT_GATE_UP or GPTQ_FORMAT_BF16 is refused as by gptq_gemm. */
 size_t gptq_lora_workspace_bytes(int M, int N, int K, int group_size, int act_order, int rank);

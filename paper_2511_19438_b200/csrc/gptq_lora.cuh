@@ -213,15 +213,33 @@ __global__ void __launch_bounds__(256, 4) lora_delta_rows_kernel(const LoraArgs 
     }
 }
 
-// Prompts, runs of rows with one adapter: kDeltaRows rows and 256 columns per CTA, MMAs with the rows' v as the 16-row operand, in two
-// 16-bit parts (v = hi + lo to 2^-22, 2^-16 in bfloat16: the product is as good as fp32's next to the 16 bits of delta) that the CTA
-// prepares in shared memory, and eight rows of B as the columns.  1000 rows of 4096 x 4096 in five runs, rank 16: 41 us with the shrink
-// kernel and the matmul, which alone takes 27.
+// Prompts, runs of rows with one adapter: kDeltaRows rows and 256 columns per CTA, MMAs with the rows' v as the 16-row operand and
+// eight rows of B as the columns.  v is taken in two 16-bit parts that the CTA prepares in shared memory, each row times the power of two
+// that brings its largest value to 2^14 .. 2^15: hi + lo is then v to 2^-22 (bfloat16 2^-16) wherever v lies in fp32's range (fp16: of values
+// below 2^-17 of the row's largest, to 2^-39 of the largest).  The product is as good as fp32's next to the 16 bits of delta; the power is taken
+// out of the fp32 sums.  A sum that is not finite is formed again in fp32: an infinity times a part that is 0 is NaN.
+// 1000 rows of 4096 x 4096 in five runs, rank 16: 41.6 us with the shrink kernel and the matmul, which alone takes 27
+// (41.1 without the powers of two and the test for infinities).
 constexpr int kDeltaRows = 32, kDeltaTiles = 4;      // tiles: eight columns each, of a warp
 template <bool BF>
-__global__ void __launch_bounds__(256, 2) lora_delta_runs_kernel(const LoraArgs a, __half *__restrict__ delta)
+__device__ __noinline__ float long_expansion(const LoraArgs &a, int m, int n)
+{
+    const __half *b = a.b + ((size_t)__ldg(a.ids + m) * a.N + n) * a.rank;
+    float sum = 0.f;
+    for (int r = 0; r < a.rank; r += 4) {
+        float4 v[1];
+        lora_v(a, m, r, v);
+        const uint2 p = __ldg(reinterpret_cast<const uint2 *>(b + r));
+        const float2 lo = pair_to_float2<BF>(p.x), hi = pair_to_float2<BF>(p.y);
+        sum = fmaf(hi.y, v[0].w, fmaf(hi.x, v[0].z, fmaf(lo.y, v[0].y, fmaf(lo.x, v[0].x, sum))));
+    }
+    return sum;
+}
+template <bool BF>
+__global__ void __launch_bounds__(256, 2) lora_delta_runs_kernel(const __grid_constant__ LoraArgs a, __half *__restrict__ delta)
 {
     extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ float unscale[kDeltaRows];
     pdl_launch_dependents();
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
     const int n0 = 8 * kDeltaTiles * (8 * blockIdx.x + warp), m0 = kDeltaRows * blockIdx.y, count = min(kDeltaRows, a.M - m0);
@@ -238,16 +256,38 @@ __global__ void __launch_bounds__(256, 2) lora_delta_runs_kernel(const LoraArgs 
     uint4 p[kDeltaTiles] = {};
     if (leads) load_b(p, __shfl_sync(0xffffffffu, my_id, __ffs(leads) - 1), 8 * t4);      // on its way while v is prepared
     pdl_wait();
-    for (int i = threadIdx.x; i < kDeltaRows * width / 4; i += 256) {
-        const int row = i / (width / 4), r = 4 * (i - row * (width / 4));
-        float4 w[1] = {};
-        if (row < count && r < a.rank) lora_v(a, m0 + row, r, w);
-        const float4 v = w[0];
-        const uint2 h = make_uint2(pack16<BF>(v.x, v.y), pack16<BF>(v.z, v.w));
-        const float2 h0 = pair_to_float2<BF>(h.x), h1 = pair_to_float2<BF>(h.y);
-        uint8_t *at = smem + row * pitch + 2 * r;
-        *reinterpret_cast<uint2 *>(at) = h;
-        *reinterpret_cast<uint2 *>(at + 2 * width) = make_uint2(pack16<BF>(v.x - h0.x, v.y - h0.y), pack16<BF>(v.z - h1.x, v.w - h1.y));
+    {      // eight lanes prepare a row
+        const int row = threadIdx.x >> 3, r0 = 4 * (threadIdx.x & 7);
+        const bool named = __shfl_sync(0xffffffffu, my_id, row) >= 0;
+        float4 v[kLoraMaxRank / 32];
+        int top = 0;      // the largest finite magnitude's bits
+#pragma unroll
+        for (int i = 0; i < kLoraMaxRank / 32; ++i) {
+            if (32 * i >= width) break;
+            float4 w[1] = {};
+            if (named && r0 + 32 * i < a.rank) lora_v(a, m0 + row, r0 + 32 * i, w);
+            v[i] = w[0];
+            for (float f : {v[i].x, v[i].y, v[i].z, v[i].w}) {
+                const int bits = __float_as_int(f) & 0x7fffffff;
+                top = max(top, bits < 0x7f800000 ? bits : 0);
+            }
+        }
+#pragma unroll
+        for (int o = 1; o < 8; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const int e = top ? min(14 + 127 - (top >> 23), 126) : 0;      // -113 .. 126
+        const float scale = __int_as_float((127 + e) << 23);
+        if ((threadIdx.x & 7) == 0) unscale[row] = __int_as_float((127 - e) << 23);
+        auto rest = [](float f, float h) { return isfinite(h) ? f - h : 0.f; };
+#pragma unroll
+        for (int i = 0; i < kLoraMaxRank / 32; ++i) {
+            if (32 * i >= width) break;
+            const float4 f = make_float4(v[i].x * scale, v[i].y * scale, v[i].z * scale, v[i].w * scale);
+            const uint2 h = make_uint2(pack16<BF>(f.x, f.y), pack16<BF>(f.z, f.w));
+            const float2 h0 = pair_to_float2<BF>(h.x), h1 = pair_to_float2<BF>(h.y);
+            uint8_t *at = smem + row * pitch + 2 * (r0 + 32 * i);
+            *reinterpret_cast<uint2 *>(at) = h;
+            *reinterpret_cast<uint2 *>(at + 2 * width) = make_uint2(pack16<BF>(rest(f.x, h0.x), rest(f.y, h0.y)), pack16<BF>(rest(f.z, h1.x), rest(f.w, h1.y)));
+        }
     }
     __syncthreads();
     if (n0 >= a.N) return;
@@ -285,9 +325,15 @@ __global__ void __launch_bounds__(256, 2) lora_delta_runs_kernel(const LoraArgs 
         for (int half = 0; half < 2; ++half) {
             const int row = 16 * m + 8 * half + g;
             if (row >= count) continue;
+            const float by = unscale[row];
 #pragma unroll
-            for (int t = 0; t < kDeltaTiles; ++t)
-                *reinterpret_cast<uint32_t *>(delta + (size_t)(m0 + row) * a.N + n0 + 8 * t + 2 * t4) = pack16<BF>(out[m][t][2 * half], out[m][t][2 * half + 1]);
+            for (int t = 0; t < kDeltaTiles; ++t) {
+                const int n = n0 + 8 * t + 2 * t4;
+                float lo = out[m][t][2 * half] * by, hi = out[m][t][2 * half + 1] * by;
+                if (!isfinite(lo)) lo = long_expansion<BF>(a, m0 + row, n);
+                if (!isfinite(hi)) hi = long_expansion<BF>(a, m0 + row, n + 1);
+                *reinterpret_cast<uint32_t *>(delta + (size_t)(m0 + row) * a.N + n) = pack16<BF>(lo, hi);
+            }
         }
 }
 

@@ -609,3 +609,66 @@ def test_repeats_bit_for_bit(ws):
         ys = [H.moe_mlp(x, ids, w, moe.up, moe.down, r) for _ in range(4)]
         zs = [H.gemm_lora(xl, lora.D, lora.a, lora.b, il, lora.scales) for _ in range(4)]
         assert all(torch.equal(v, y) for v in ys) and all(torch.equal(v, z) for v in zs)
+
+
+# ------------------------------------------------------------------------------------- values at the ends of their types' ranges
+
+def zero_weights(lora):
+    """The shared layer's weights become zero (every nibble its zero point), so that y is the adapters' part alone.  Up to 8 rows it is formed
+    as sum q x - z sum x, off by 8 2^-23 (31 or 287) sum |x| s (the head of this file), where `sums` takes s from |w|, here 0: it is added."""
+    lora.L.qweight[:], lora.L.qzeros[:] = -0x77777778, -0x77777778
+    lora.w64.zero_()
+    bits = wl.make_scales_bf16(lora.L.G, lora.N, 5) if lora.dtype == torch.bfloat16 else None
+    lora.D = H.upload_and_repack(lora.L, scales_bf16_bits=bits)
+    scales = torch.from_numpy(lora.L.scales).cuda() if bits is None else H.bf16_from_bits(bits)
+    s64 = scales.double().repeat_interleave(lora.L.group_size, 0)
+    plain = lora.plain
+
+    def with_sums(x, ids, scales):
+        y, most, square = plain(x, ids, scales)
+        if x.shape[0] > 8:
+            return y, most, square
+        more = 8 * F32 * (287 if lora.dtype == torch.bfloat16 else 31) * (x.double().abs() @ s64)
+        return y, most + more, square + more * more
+
+    lora.plain = with_sums
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("M,rank", [(8, 16), (64, 16), (65, 16), (65, 40), (200, 256)])
+def test_lora_large_and_small_inner_sums(ws, M, rank, dtype):
+    """v = s x A^T far beyond and far below fp16's range, B the other way round: it is kept in fp32 (lora.plain's bounds; two 16-bit parts
+    of v, 2^-22 and 2^-16 of it, are within (K + rank) 2^-23 of the sum of absolute values).  Columns of A of sizes 2^-8 apart."""
+    lora = Lora(512, 256, rank, 3, dtype=dtype)
+    zero_weights(lora)
+    lora.scales = torch.tensor([2.0 ** 20, 1.0, 2.0 ** -20], device="cuda")
+    for a, e in enumerate((-10, 0, 8)):
+        lora.b[a] = (lora.b[a].float() * 2.0 ** e).to(dtype)
+    even = torch.arange(rank, device="cuda") % 2 == 0
+    lora.a[:, even] *= 2.0 ** -4
+    lora.b[:, :, even] *= 2.0 ** 4
+    lora.a[:, ~even] *= 2.0 ** 4
+    lora.b[:, :, ~even] *= 2.0 ** -4
+    x, ids = lora.inputs(M, "range")
+    lora.check(ws, x, ids, lora.scales)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("M", [6, 40, 100])
+def test_lora_infinities_in_the_adapter(ws, M, dtype):
+    """An infinity in B or in v gives what the sum over the rank gives."""
+    lora = Lora(512, 256, 16, 3, dtype=dtype)
+    x, ids = lora.inputs(M, "infb")
+    want = lora.check(ws, x, ids, lora.scales)
+    one, two, three = ids == 0, ids == 1, ids == 2
+    columns = torch.arange(256, device="cuda") % 5 == 2
+    lora.b[1, columns, 3] = math.inf                    # one infinity in some columns of B: that of v's sign
+    lora.a[2] = lora.a[2, :1].clone()                   # v infinite, of one sign for the whole rank, and B positive
+    lora.b[2] = lora.b[2].abs() + 0.125
+    lora.scales[2] = math.inf
+    y = H.gemm_lora(x, lora.D, lora.a, lora.b, ids, lora.scales).double()
+    assert torch.equal(y[one], want[one].double())
+    assert torch.equal(y[two][:, ~columns], want[two][:, ~columns].double())
+    v = x.double() @ lora.a[:, 3].double().t()          # [M, adapter]
+    assert torch.equal(y[two][:, columns], (math.inf * v[two, 1].sign())[:, None].expand(-1, int(columns.sum())))
+    assert torch.equal(y[three], (math.inf * v[three, 2].sign())[:, None].expand(-1, 256))
