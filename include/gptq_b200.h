@@ -309,7 +309,8 @@ int gptq_moe_route(const void *logits, int32_t *expert_ids, float *expert_weight
  * act_order = 1: gate_up_perm int32 [E, K] = the gate_up layers' perm_out, down_index int32 [E, F] = gptq_invert_perm of the down
  * layers' perm_out.  0: both ignored, may be NULL.  (GPTQ_ACT_ORDER_PRESORTED is refused: each expert has an order of its own.)
  * Arithmetic: sum q x and z sum x apart for each quantisation group, both in fp32 (their error: see gptq_gemm's one and two rows),
- * scales in fp32; the activation in fp32, up to 16 tokens kept as two 16-bit numbers (to 2^-22 of its size, bfloat16 2^-16), above rounded
+ * scales in fp32; the activation in fp32 (the fast exponential: 2^-18 of its size, for gates below -25 up to 2^-16), up to 16 tokens kept
+ * as two 16-bit numbers (to 2^-22 of its size, in fp16 2^-36 where that is more, in bfloat16 2^-16), above rounded
  * once to fp16 (a pass of up to 16 tokens behind full ones counts as such; a value beyond 65504 becomes an infinity); weights, sums over
  * experts and residual in fp32, one rounding of y.  The order of the sums is fixed: the same inputs give the same bits.  Sums that
  * infinities reach are formed as the formula has them.

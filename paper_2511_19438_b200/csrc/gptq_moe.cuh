@@ -338,14 +338,17 @@ __device__ __forceinline__ int build_slot_plan(const MoeArgs &a, int R, const Sl
     return s_segments;
 }
 
-// An activation's parts.  With two, 16 bits and the 16 of what they leave, h is good to 2^-22 (bfloat16 2^-16) and y's rounding is the
-// only one; an infinity leaves nothing.
+// An activation's parts.  With two, 16 bits and the 16 of what they leave, y's rounding is the only one that counts: h is good to 2^-22
+// (bfloat16 2^-16).  In fp16 the second part is kept times 2^11, as large as h at most, so that a small h (down to 2^-14; below, to 2^-36)
+// loses nothing to the subnormal numbers; the down kernel takes the power out of its sums.  An infinity leaves nothing.
+template <bool BF>
+__host__ __device__ constexpr float second_part_scale() { return BF ? 1.f : 2048.f; }
 template <bool BF>
 __device__ __forceinline__ void store_h(const MoeArgs &a, __half *at, float v)
 {
     store_out16<BF>(at, v);
     if (a.parts == 1) return;
-    const float left = v - out16_to_float<BF>(*at);
+    const float left = (v - out16_to_float<BF>(*at)) * second_part_scale<BF>();
     store_out16<BF>(at + (size_t)a.M * a.k * a.F, isfinite(left) ? left : 0.f);
 }
 
@@ -584,8 +587,10 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_down_kernel(co
 #pragma unroll
             for (int w = 0; w < kMoeWarps; ++w) sum += buf[(w * kValues + v) * 32 + lane];
             if (a.parts == 2) {      // column r + 4
+                float second = 0.f;
 #pragma unroll
-                for (int w = 0; w < kMoeWarps; ++w) sum += buf[(w * kValues + v) * 32 + lane + 2];
+                for (int w = 0; w < kMoeWarps; ++w) second += buf[(w * kValues + v) * 32 + lane + 2];
+                sum = fmaf(second, 1.f / second_part_scale<BF>(), sum);
             }
             const int s = plan.slot[first + r];
             float *cell = ysum + plan.token[s] * kCols + 16 * u + g + 8 * (i >> 1);

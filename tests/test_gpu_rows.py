@@ -672,3 +672,13 @@ def test_lora_infinities_in_the_adapter(ws, M, dtype):
     v = x.double() @ lora.a[:, 3].double().t()          # [M, adapter]
     assert torch.equal(y[two][:, columns], (math.inf * v[two, 1].sign())[:, None].expand(-1, int(columns.sum())))
     assert torch.equal(y[three], (math.inf * v[three, 2].sign())[:, None].expand(-1, 256))
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("M", [1, 5, 16])
+def test_moe_small_activations(ws, M, dtype):
+    """h of about 1e-6, below fp16's normal numbers, under weights that make y ordinary: its two parts still hold it to far less than
+    y's rounding (moe.check's mean square: u^2 + 2^-18 of h)."""
+    moe = Moe(256, 256, 4, dtype=dtype)
+    x, ids, w, _ = moe.inputs(M, 2, "small")
+    moe.check(ws, x * 2.0 ** -9, ids, w * 2.0 ** 15, None)
