@@ -313,7 +313,8 @@ int gptq_moe_route(const void *logits, int32_t *expert_ids, float *expert_weight
  * as two 16-bit numbers (to 2^-22 of its size, in fp16 2^-36 where that is more, in bfloat16 2^-16), above rounded
  * once to fp16 (a pass of up to 16 tokens behind full ones counts as such; a value beyond 65504 becomes an infinity); weights, sums over
  * experts and residual in fp32, one rounding of y.  The order of the sums is fixed: the same inputs give the same bits.  Sums that
- * infinities reach are formed as the formula has them.
+ * infinities or NaN reach, and bfloat16 ones that leave fp32's range in between, are formed again as the formula has them, a thread per
+ * output over the whole K: right but slow (a row of NaN with 8 experts of 2048 x 768: 0.8 ms instead of 15 us; padding rows belong under -1).
  * residual may be y; y may be x.  Scratch: gptq_moe_workspace_bytes of the registered workspace (GPTQ_ERR_WORKSPACE without it),
  * under the rules of gptq_set_workspace: calls, and graphs captured from calls, that may run at the same time must not share one.
  * Each expert in use is read once for every 8 of its tokens; M > 64 runs as passes of 64 tokens.  Two kernels per pass, three with
@@ -338,7 +339,8 @@ int gptq_moe_mlp_bf16(const void *x, const int32_t *expert_ids, const float *exp
  * to 256 (GPTQ_ERR_UNSUPPORTED).  W, x, y, g_idx, act_order, errors and accuracy of the product with W as for gptq_gemm; with
  * act_order = 1 x and lora_a are in the checkpoint's row order, with GPTQ_ACT_ORDER_PRESORTED both are in the sorted one.
  * x A^T, scaled, is summed and kept in fp32.  Up to 8 rows the expansion joins the fp32 sums before the one rounding of y (two
- * kernels, three with act_order = 1; the products are those of gptq_gemm's one and two rows: sum q x and z sum x apart); above, it
+ * kernels, three with act_order = 1; the products are those of gptq_gemm's one and two rows: sum q x and z sum x apart, and again the slow
+ * way where that gives infinities or NaN); above, it
  * is rounded to 16 bits on its way to them (a value beyond 65504 becomes an infinity; two kernels and gptq_gemm's).  A row's result does not depend on the other rows'
  * adapters, whatever these hold.  y must not be x (GPTQ_ERR_LAYOUT).  Scratch: gptq_lora_workspace_bytes of the registered workspace, always needed,
  * under the rules of gptq_set_workspace.  A layer tiled with GPTQ_FORMAT_GATE_UP or GPTQ_FORMAT_BF16 is refused as by gptq_gemm. */

@@ -15,7 +15,8 @@
 // by one more OR, and -(128 + z) sum x.  All in fp32: the error is that of sums of (q + z) |x| (bfloat16: (256 + q + z) |x|), far
 // below the rounding of the 16-bit results.  Against subtracting z from each weight this is 5 instead of 9 instructions per eight
 // weights; these kernels are bound by instruction issue as much as by memory.
-// An infinity in x makes such a difference NaN, whatever the product is; sums that end up NaN are formed again the long way, in the epilogues.
+// An infinity in x makes such a difference NaN, whatever the product is, and in bfloat16 sum (128 + q) x can leave fp32's range where the
+// product does not (x from 2^110 on): sums that end up so are formed again the long way, in the epilogues.
 #pragma once
 #include <mutex>
 
@@ -308,7 +309,14 @@ __device__ __forceinline__ void stream_items(uint32_t ring, int lane, uint32_t o
     }
 }
 
-// The sum over n items for one column (0 .. 15) of a unit and one token row, the formula as it stands, for sums that came out NaN.
+// whether a sum is formed again the long way (fp16 sums do not leave fp32's range: an infinity of x is NaN here)
+template <bool BF>
+__device__ __forceinline__ bool needs_long_sum(float v)
+{
+    if constexpr (BF) return !isfinite(v);
+    else return v != v;
+}
+// The sum over n items for one column (0 .. 15) of a unit and one token row, the formula as it stands, for sums that need it (see above).
 // w, s, z: the unit's addresses without a lane's share; in_order: the row lies in memory as direct_column has it.
 template <bool BF>
 __device__ __noinline__ float long_sum(const uint8_t *w, const uint8_t *s, const uint8_t *z, int sub, int col, uint32_t z_add,

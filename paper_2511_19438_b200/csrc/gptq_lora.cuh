@@ -421,7 +421,7 @@ lora_gemm_kernel(const LoraArgs a, const __half *x, const uint8_t *qweight, cons
             float sum = 0.f;
 #pragma unroll
             for (int w = 0; w < W; ++w) sum += buf[(w * kValues + v) * 32 + lane];
-            if (sum != sum) {      // the long way (see stream_items)
+            if (needs_long_sum<BF>(sum)) {
                 const UnitPtrs p = unit_ptrs<SUB>(qweight, scales, qzeros, n / kPanel, G, n % kPanel / 16);
                 sum = long_sum<BF>(p.w, p.s, p.z, SUB, n % 16, flags & kFormatZerosMinusOne, x + (size_t)m * a.K, G, false);
             }

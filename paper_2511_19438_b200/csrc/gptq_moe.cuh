@@ -426,7 +426,7 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_gate_up_kernel
     float acc[NU][4] = {};
     // the tile at hand, the one before it (its segment and column), how many came before
     int unit = t0, seg_at = t0 / per_seg, col_at = t0 - seg_at * per_seg, left = t0, left_seg = 0, left_col = 0, tiles = 0;
-    bool saw_nan = false;
+    bool again = false;
     auto add_up = [&]() {      // the sums of the tile at `left` over the warps, in their order
         const int done = tiles - 1;
         if (!mbar_wait(bars + 8 * (done & 1), (done >> 1) & 1)) return;
@@ -443,7 +443,7 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_gate_up_kernel
                 gate += buf[w * (kValues * 32) + at];
                 up += buf[w * (kValues * 32) + 128 + at];
             }
-            saw_nan |= gate != gate || up != up;
+            again |= needs_long_sum<BF>(gate) || needs_long_sum<BF>(up);
             int col = c0 + 16 * p + g + 8 * (i >> 1);
             if (a.down_index) col = __ldg(a.down_index + (size_t)plan.seg_expert[seg] * a.F + col);
             store_h<BF>(a, a.h + (size_t)plan.slot[first + r] * a.F + direct_column<BF>(col), silu_mul(gate, up));
@@ -472,8 +472,8 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_gate_up_kernel
     stream_items<NU, true, SUB, BF, false>(ring, lane, a.one, acc, next, [] {}, [&](int t) { while (unit < t) finish_tile(); });
     while (unit < t1) finish_tile();
     if (tiles) add_up();
-    if (!saw_nan) return;
-    // a thread goes over its outputs again and forms those that are NaN the long way (see stream_items)
+    if (!again) return;
+    // a thread goes over its outputs again and forms those that are not finite, as h is where gate or up was not, the long way
     for (unit = t0; unit < t1; unit += width(unit)) {
         const int seg = unit / per_seg, c0 = (unit - seg * per_seg) * 16, e = plan.seg_expert[seg];
         const int first = plan.seg_begin[seg], count = plan.seg_begin[seg + 1] - first;
@@ -485,7 +485,7 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_gate_up_kernel
             const int s = plan.slot[first + r], col = c0 + 16 * (v >> 2) + c;
             __half *at = a.h + (size_t)s * a.F + direct_column<BF>(a.down_index ? __ldg(a.down_index + (size_t)e * a.F + col) : col);
             const float now = out16_to_float<BF>(*at);
-            if (now == now) continue;
+            if (isfinite(now)) continue;
             float sum[2];
 #pragma unroll 1
             for (int half = 0; half < 2; ++half) {
@@ -634,7 +634,7 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_down_kernel(co
     auto place = [&](int o) { return (size_t)(o / kCols) * a.K + panel * kPanel + 16 * unit + o % kCols; };
     auto store = [&](int o, float v, float residual) {
         const int m = o / kCols, c = o % kCols;
-        if (v != v) {      // the long way (see stream_items)
+        if (needs_long_sum<BF>(v)) {
             v = 0.f;
 #pragma unroll 1
             for (int s = m * a.k; s < (m + 1) * a.k; ++s) {

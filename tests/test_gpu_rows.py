@@ -682,3 +682,45 @@ def test_moe_small_activations(ws, M, dtype):
     moe = Moe(256, 256, 4, dtype=dtype)
     x, ids, w, _ = moe.inputs(M, 2, "small")
     moe.check(ws, x * 2.0 ** -9, ids, w * 2.0 ** 15, None)
+
+
+def heavy(count, K, N, positive, group=128):
+    """bfloat16 layers whose weights (q - z) s are all positive or all negative: (QuantLinear list, scale bits, float64 weights)."""
+    out = []
+    for e in range(count):
+        q, z = np.full((K, N), 9 if positive else 4, np.uint8), np.full((K // group, N), 6 if positive else 12, np.uint8)
+        L = wl.make_linear_from_values(q, z, np.ones((K // group, N), np.float16), group_size=group)
+        bits = wl.make_scales_bf16(K // group, N, wl.seed_for("heavy", e, N))
+        out.append((L, bits, H.to_device(oracle.dequant_f32_bf16(L.qweight, L.qzeros, bits, L.g_idx, group, False)).double()))
+    return [o[0] for o in out], [o[1] for o in out], [o[2] for o in out]
+
+
+def test_lora_bf16_sums_whose_parts_overflow(ws):
+    """x of one sign and 2^114: sum (128 + q) x is beyond fp32's range, sum (q - z) x s is not."""
+    lora = Lora(512, 256, 16, 2, dtype=torch.bfloat16)
+    for positive in (False, True):
+        layers, bits, w64 = heavy(1, 512, 256, positive)
+        lora.D, lora.w64 = H.upload_and_repack(layers[0], scales_bf16_bits=bits[0]), w64[0]
+        for M in (1, 7):
+            x = torch.full((M, 512), 2.0 ** 114, dtype=torch.bfloat16, device="cuda")
+            lora.check(ws, x, torch.full((M,), -1, dtype=torch.int32, device="cuda"), None)
+
+
+def test_moe_bf16_sums_whose_parts_overflow(ws):
+    """The same for experts: gates far below zero, h = 0, y = residual; and h of 2^114 into the down layer."""
+    moe = Moe.__new__(Moe)
+    moe.K, moe.F, moe.E, moe.dtype = 256, 256, 2, torch.bfloat16
+    minus, plus = heavy(2, 256, 512, False), heavy(2, 256, 512, True)
+    down = heavy(2, 256, 256, True)
+    moe.down, moe.down64 = H.upload_experts(down[0], scales_bf16_bits=down[1]), down[2]
+    for M in (1, 9, 20):
+        ids = (torch.arange(M, device="cuda") % 2).to(torch.int32)[:, None].contiguous()
+        w = torch.ones((M, 1), device="cuda")
+        moe.up, moe.up64 = H.upload_experts(minus[0], gate_up=True, scales_bf16_bits=minus[1]), minus[2]
+        x = torch.full((M, 256), 2.0 ** 114, dtype=torch.bfloat16, device="cuda")
+        r = torch.randn((M, 256), generator=gen("overflow", M), device="cuda").to(torch.bfloat16)
+        H.ensure_for_moe(ws, M, moe.up, 1)
+        assert torch.equal(H.moe_mlp(x, ids, w, moe.up, moe.down, r), r)
+        moe.up, moe.up64 = H.upload_experts(plus[0], gate_up=True, scales_bf16_bits=plus[1]), plus[2]
+        x = torch.full((M, 256), 2.0 ** 55, dtype=torch.bfloat16, device="cuda")      # gate and up of 2^57 or so
+        moe.check(ws, x, ids, w, r)
