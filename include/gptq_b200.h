@@ -315,8 +315,8 @@ int gptq_moe_route(const void *logits, int32_t *expert_ids, float *expert_weight
  * experts and residual in fp32, one rounding of y.  The order of the sums is fixed: the same inputs give the same bits.  Sums that
  * infinities or NaN reach, and bfloat16 ones that leave fp32's range in between, are formed again as the formula has them, a thread per
  * output over the whole K: right but slow (a row of NaN with 8 experts of 2048 x 768: 0.8 ms instead of 15 us; padding rows belong under -1).
- * residual may be y; y may be x.  Scratch: gptq_moe_workspace_bytes of the registered workspace (GPTQ_ERR_WORKSPACE without it),
- * under the rules of gptq_set_workspace: calls, and graphs captured from calls, that may run at the same time must not share one.
+ * residual may be y; y may be x.  Scratch: gptq_moe_workspace_bytes of the registered workspace (GPTQ_ERR_WORKSPACE without it; what
+ * many tokens need does for fewer), under the rules of gptq_set_workspace: calls, and graphs captured from calls, that may run at the same time must not share one.
  * Each expert in use is read once for every 8 of its tokens; M > 64 runs as passes of 64 tokens.  Two kernels per pass, three with
  * act_order.  Layers of another tiling: nothing is stored, and gptq_check_status returns GPTQ_ERR_LAYOUT.
  * E <= 1024, top_k <= 32 (GPTQ_ERR_UNSUPPORTED).  Stream semantics and other errors as for gptq_gemm. */
@@ -342,8 +342,9 @@ int gptq_moe_mlp_bf16(const void *x, const int32_t *expert_ids, const float *exp
  * kernels, three with act_order = 1; the products are those of gptq_gemm's one and two rows: sum q x and z sum x apart, and again the slow
  * way where that gives infinities or NaN); above, it
  * is rounded to 16 bits on its way to them (a value beyond 65504 becomes an infinity; two kernels and gptq_gemm's).  A row's result does not depend on the other rows'
- * adapters, whatever these hold.  y must not be x (GPTQ_ERR_LAYOUT).  Scratch: gptq_lora_workspace_bytes of the registered workspace, always needed,
- * under the rules of gptq_set_workspace.  A layer tiled with GPTQ_FORMAT_GATE_UP or GPTQ_FORMAT_BF16 is refused as by gptq_gemm. */
+ * adapters, whatever these hold.  y must not be x (GPTQ_ERR_LAYOUT).  Scratch: gptq_lora_workspace_bytes of the registered workspace, always needed
+ * (GPTQ_ERR_WORKSPACE without it; what many rows need does for fewer, of the same N, K, rank and act_order), under the rules of
+ * gptq_set_workspace.  A layer tiled with GPTQ_FORMAT_GATE_UP or GPTQ_FORMAT_BF16 is refused as by gptq_gemm. */
 size_t gptq_lora_workspace_bytes(int M, int N, int K, int group_size, int act_order, int rank);
 int gptq_gemm_lora(const void *x, const void *qweight, const void *qzeros, const void *scales, const int32_t *g_idx,
                    const void *lora_a, const void *lora_b, const int32_t *adapter_ids, const float *adapter_scales, void *y,

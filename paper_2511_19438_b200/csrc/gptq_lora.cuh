@@ -465,13 +465,23 @@ lora_gemm_kernel(const LoraArgs a, const __half *x, const uint8_t *qweight, cons
 
 // The parts of K that the shrink kernel sums apart: so many that a warp has one batch of steps - a second one costs a round trip to
 // memory, 64 rows of 64 adapters of 5120 x 32: 17 us with five parts, 22 with four - as long as the CTAs are not too many anyway.
-constexpr int kLoraMaxParts = 12;
+constexpr int kLoraMaxParts = 12, kLoraMaxCtas = 1500;
 inline int lora_k_parts(int M, int K, int rank)
 {
     const long long ctas = (long long)((M + 7) / 8) * ((rank + 15) / 16) * (M < 8 ? M : M <= kLoraDecodeRows ? 8 : 1);
-    const int steps = kLoraWarps * kLoraSteps, most = 1500 / ctas < 1 ? 1 : 1500 / ctas > kLoraMaxParts ? kLoraMaxParts : (int)(1500 / ctas);
+    const int steps = kLoraWarps * kLoraSteps, most = kLoraMaxCtas / ctas < 1 ? 1 : kLoraMaxCtas / ctas > kLoraMaxParts ? kLoraMaxParts : (int)(kLoraMaxCtas / ctas);
     const int parts = (K / 32 + steps - 1) / steps;
     return parts < most ? parts : most;
+}
+
+// Rows of v over all parts that a call of M rows, or of fewer, writes at most: who has registered for the largest call has enough.  parts x
+// rows of m rows is m, or as many parts as K has x m and no more than 1500 / ctas x m, which is at most 1500 per 16 of the rank up to
+// kLoraDecodeRows rows and 8 times that above.
+inline size_t lora_v_rows(int M, int K, int rank)
+{
+    const long long ranks = (rank + 15) / 16, all = (long long)M * lora_k_parts(1, K, 16);      // (one row and rank 16: as many as K has)
+    const long long most = (M <= kLoraDecodeRows ? kLoraMaxCtas : 8 * kLoraMaxCtas) / ranks, rows = all < most ? all : most;
+    return (size_t)(rows > M ? rows : M);
 }
 
 // scratch: [x in the sorted order][v][expansion]
@@ -484,7 +494,7 @@ inline LoraScratch lora_scratch(int M, int N, int K, int rank, int act_order)
     LoraScratch l;
     l.x_perm = 0;
     l.v = act_order == 1 ? up((size_t)M * K * 2) : 0;
-    l.delta = l.v + up((size_t)lora_k_parts(M, K, rank) * M * rank * 4);
+    l.delta = l.v + up(lora_v_rows(M, K, rank) * rank * 4);
     l.total = l.delta + (M > kLoraDirectRows ? up((size_t)M * N * 2) : 0);
     return l;
 }

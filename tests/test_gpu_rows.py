@@ -724,3 +724,25 @@ def test_moe_bf16_sums_whose_parts_overflow(ws):
         moe.up, moe.up64 = H.upload_experts(plus[0], gate_up=True, scales_bf16_bits=plus[1]), plus[2]
         x = torch.full((M, 256), 2.0 ** 55, dtype=torch.bfloat16, device="cuda")      # gate and up of 2^57 or so
         moe.check(ws, x, ids, w, r)
+
+
+# ------------------------------------------------------------------------------------------------------------------------ scratch
+
+@pytest.mark.parametrize("K,rank,most", [(4096, 64, 256), (2048, 256, 33)])
+def test_lora_scratch_of_the_largest_call(ws, K, rank, most):
+    """Scratch of exactly the size that the largest call asks for: every smaller one runs in it, and nothing behind it is written."""
+    lora = Lora(K, 128, rank, 2)
+    need = B.gptq_lora_workspace_bytes(most, 128, K, 128, 0, rank)
+    buf = torch.full((need + 65536,), 0xa5, dtype=torch.uint8, device="cuda")
+    try:
+        B.check(B.gptq_set_workspace(buf, need), "gptq_set_workspace")
+        for M in (1, 8, 9, 32, 33, most - 9, most - 8, most - 1, most):
+            if M > most:
+                continue
+            x, ids = lora.inputs(M, "scratch")
+            want, bound, _ = lora.plain(x, ids, lora.scales)
+            y = H.gemm_lora(x, lora.D, lora.a, lora.b, ids, lora.scales)
+            assert ((y.double() - want).abs() <= bound).all()
+        assert (buf[need:] == 0xa5).all()
+    finally:
+        ws.ensure(1)

@@ -97,6 +97,18 @@ def test_workspace_sizes():
         assert B.gptq_lora_workspace_bytes(*bad) == 0
 
 
+@pytest.mark.parametrize("act", [0, 1, 2])
+@pytest.mark.parametrize("N,K,rank", [(128, 128, 8), (128, 11008, 256), (4096, 4096, 16), (4096, 4096, 64), (4096, 4096, 256), (4096, 11008, 64),
+                                      (12288, 4096, 64), (4096, 512 * 128, 40)])
+def test_adapter_scratch_for_many_rows_does_for_fewer(N, K, rank, act):
+    rows = list(range(1, 2200)) + list(range(2200, 40000, 37))
+    need = [B.gptq_lora_workspace_bytes(m, N, K, 128, act, rank) for m in rows]
+    falls = [(rows[i], rows[i + 1]) for i in range(len(need) - 1) if need[i] > need[i + 1]]
+    assert not falls, falls[:5]
+    # v at least once, with more than 8 rows the expansion, with act-order x
+    assert all(n >= m * rank * 4 + (2 * m * N if m > 8 else 0) + (2 * m * K if act == 1 else 0) for m, n in zip(rows, need))
+
+
 def test_a_ring_stage_is_refilled_behind_the_whole_warps_reads():
     """stream_items copies into the stage that was read last.  Scales and zero points in it are read by other lanes than those that copied
     them, so that between a product and the next copy the warp has to meet.  Followed through two turns of the loop in the source."""
