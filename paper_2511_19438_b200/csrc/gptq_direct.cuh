@@ -18,8 +18,6 @@
 // An infinity in x makes such a difference NaN, whatever the product is, and in bfloat16 sum (128 + q) x can leave fp32's range where the
 // product does not (x from 2^110 on): sums that end up so are formed again the long way, in the epilogues.
 #pragma once
-#include <mutex>
-
 #include "gptq_common.cuh"
 
 namespace gptq {
@@ -340,47 +338,43 @@ __device__ __noinline__ float long_sum(const uint8_t *w, const uint8_t *s, const
 // n things given out to `parts` in neighbouring ranges, the longer ranges spread evenly: the first of range i
 __device__ __forceinline__ int share_begin(int n, int parts, int i) { return (int)((unsigned long long)n * (unsigned)i / (unsigned)parts); }
 
-// Allows a kernel `smem_bytes` of dynamic shared memory and asks for room for `ctas` such CTAs per SM; what is left of the SM's
-// 256 KB is L1, in which these kernels keep the rows that they read again and again.
-static int ensure_direct_smem(const void *kernel, int *configured, int smem_bytes, int ctas)
-{
-    static std::mutex mu;
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return record_cuda_error(e);
-    if (dev < 0 || dev >= 64) return GPTQ_ERR_UNSUPPORTED;
-    std::lock_guard<std::mutex> lock(mu);
-    if (configured[dev] >= smem_bytes) return GPTQ_OK;
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes);
-    if (e != cudaSuccess) return record_cuda_error(e);
-    const int percent = (ctas * (smem_bytes + 2048) * 100 + 228 * 1024 - 1) / (228 * 1024);
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, percent < 100 ? percent : 100);
-    if (e != cudaSuccess) return record_cuda_error(e);
-    configured[dev] = smem_bytes;
-    return GPTQ_OK;
-}
-
-// a kernel launched as a programmatic dependent, in clusters of `cluster` CTAs
+// A kernel launched as a programmatic dependent, in clusters of `cluster` CTAs.  With per_sm it asks for shared memory for that many CTAs per
+// SM; what is left of the SM's 228 KB is L1, in which these kernels keep the rows that they read again and again.  That goes with the launch,
+// not with the kernel: other launches of it want another size or number (one token, 64 experts of 2048 x 768 behind a call of 512 x 512:
+// 22.0 us with the latter's share, 15.6 with its own).
 template <typename... Params, typename... Args>
-static int launch_dependent(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, int cluster, cudaStream_t s, Args... args)
+static int launch_sharing_sm(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, int cluster, int per_sm, cudaStream_t s, Args... args)
 {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = grid;
     cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
-    cudaLaunchAttribute attr[3];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)cluster;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
+    cudaLaunchAttribute attr[4];
+    int n = 0;
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n++].val.programmaticStreamSerializationAllowed = 1;
+    if (cluster > 1) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = (unsigned)cluster;
+        attr[n].val.clusterDim.y = 1;
+        attr[n++].val.clusterDim.z = 1;
+        attr[n].id = cudaLaunchAttributeClusterSchedulingPolicyPreference;      // clusters spread over the SMs
+        attr[n++].val.clusterSchedulingPolicyPreference = cudaClusterSchedulingPolicyLoadBalancing;
+    }
+    if (per_sm) {
+        const int percent = (int)((per_sm * (smem + 2048) * 100 + 228 * 1024 - 1) / (228 * 1024));      // (2 KB: static and the system's)
+        attr[n].id = cudaLaunchAttributePreferredSharedMemoryCarveout;
+        attr[n++].val.sharedMemCarveout = (unsigned)(percent < 100 ? percent : 100);
+    }
     cfg.attrs = attr;
-    attr[2].id = cudaLaunchAttributeClusterSchedulingPolicyPreference;      // clusters spread over the SMs
-    attr[2].val.clusterSchedulingPolicyPreference = cudaClusterSchedulingPolicyLoadBalancing;
-    cfg.numAttrs = cluster > 1 ? 3 : 1;
+    cfg.numAttrs = (unsigned)n;
     return record_cuda_error(cudaLaunchKernelEx(&cfg, kernel, Params(args)...));
+}
+template <typename... Params, typename... Args>
+static int launch_dependent(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, int cluster, cudaStream_t s, Args... args)
+{
+    return launch_sharing_sm(kernel, grid, threads, smem, cluster, 0, s, args...);
 }
 
 }  // namespace gptq

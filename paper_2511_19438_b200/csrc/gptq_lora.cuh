@@ -530,10 +530,10 @@ static int launch_lora_gemm_warps(const LoraArgs &a, const __half *x, const void
     const TiledTrailer *trailer = reinterpret_cast<const TiledTrailer *>((const uint8_t *)qzeros + tiled_zero_bytes(a.N, a.K, kGroup / SUB));
     const int smem = 8 * (a.rank + 4) * 4 + 2 * W * 4 * NU * 32 * 4 + direct_ring_bytes<NU, SUB>(W);
     static int configured[64] = {};
-    const int st = ensure_direct_smem((const void *)lora_gemm_kernel<W, NU, SUB, BF>, configured, smem, 16 / W);
+    const int st = ensure_dynamic_smem((const void *)lora_gemm_kernel<W, NU, SUB, BF>, configured, smem);
     if (st) return st;
     const int pairs = a.N / 32, slots = 16 / W * a.sms;
-    return launch_dependent(lora_gemm_kernel<W, NU, SUB, BF>, dim3((unsigned)(pairs < slots ? pairs : slots)), 32 * W, (size_t)smem, 1, s, a, x,
+    return launch_sharing_sm(lora_gemm_kernel<W, NU, SUB, BF>, dim3((unsigned)(pairs < slots ? pairs : slots)), 32 * W, (size_t)smem, 1, 16 / W, s, a, x,
                             (const uint8_t *)qweight, (const uint8_t *)scales, (const uint8_t *)qzeros, trailer, y);
 }
 template <int SUB, bool BF>

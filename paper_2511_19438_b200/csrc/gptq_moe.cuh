@@ -723,10 +723,11 @@ static int launch_gate_up(const MoeArgs &a, int most, cudaStream_t s)
 {
     static int configured[64] = {};
     const int smem = slot_plan_bytes(a.M * a.k, a.E) + moe_red_and_ring_bytes<NU, SUB>();
-    const int st = ensure_direct_smem((const void *)moe_gate_up_kernel<NU, SUB, BF>, configured, smem, kMoeCtasPerSm);
+    const int st = ensure_dynamic_smem((const void *)moe_gate_up_kernel<NU, SUB, BF>, configured, smem);
     if (st) return st;
     const long long units = (long long)most * (a.F / 16), slots = kMoeCtasPerSm * a.sms;
-    return launch_dependent(moe_gate_up_kernel<NU, SUB, BF>, dim3((unsigned)(units < slots ? units : slots)), kMoeThreads, (size_t)smem, 1, s, a);
+    return launch_sharing_sm(moe_gate_up_kernel<NU, SUB, BF>, dim3((unsigned)(units < slots ? units : slots)), kMoeThreads, (size_t)smem, 1,
+                             kMoeCtasPerSm, s, a);
 }
 template <int NU, int SUB>
 static int moe_down_smem(const MoeArgs &a, int S)
@@ -750,9 +751,9 @@ static int launch_down(const MoeArgs &a, cudaStream_t s)
     const int per_sm = tiles * S <= a.sms ? 1 : kMoeCtasPerSm;
     const int pad = 227 * 1024 / (per_sm + 1) + 512;
     if (smem < pad) smem = pad;
-    const int st = ensure_direct_smem((const void *)moe_down_kernel<NU, SUB, BF>, configured, smem, per_sm);
+    const int st = ensure_dynamic_smem((const void *)moe_down_kernel<NU, SUB, BF>, configured, smem);
     if (st) return st;
-    return launch_dependent(moe_down_kernel<NU, SUB, BF>, dim3((unsigned)(tiles * S)), kMoeThreads, (size_t)smem, S, s, a, S);
+    return launch_sharing_sm(moe_down_kernel<NU, SUB, BF>, dim3((unsigned)(tiles * S)), kMoeThreads, (size_t)smem, S, per_sm, s, a, S);
 }
 template <int SUB, bool BF>
 static int launch_moe_format(const MoeArgs &a, cudaStream_t s)

@@ -746,3 +746,56 @@ def test_lora_scratch_of_the_largest_call(ws, K, rank, most):
         assert (buf[need:] == 0xa5).all()
     finally:
         ws.ensure(1)
+
+
+def shared_memory_shares(call):
+    """(CTAs, dynamic shared memory, share of the SM asked for in percent) of each kernel with dynamic shared memory that `call(stream)` enqueues."""
+    from cuda.bindings import driver
+
+    def ok(result):
+        assert result[0] == driver.CUresult.CUDA_SUCCESS, result[0]
+        return result[1:] if len(result) > 2 else result[1] if len(result) == 2 else None
+
+    stream = torch.cuda.Stream()
+    ok(driver.cuStreamBeginCapture(stream.cuda_stream, driver.CUstreamCaptureMode.CU_STREAM_CAPTURE_MODE_RELAXED))
+    try:
+        call(stream)
+    finally:
+        graph = ok(driver.cuStreamEndCapture(stream.cuda_stream))
+    out = []
+    nodes, _ = ok(driver.cuGraphGetNodes(graph, 64))
+    for node in nodes:
+        if int(node) == 0 or ok(driver.cuGraphNodeGetType(node)) != driver.CUgraphNodeType.CU_GRAPH_NODE_TYPE_KERNEL:
+            continue
+        p = ok(driver.cuGraphKernelNodeGetParams(node))
+        share = ok(driver.cuGraphKernelNodeGetAttribute(node, driver.CUlaunchAttributeID.CU_LAUNCH_ATTRIBUTE_PREFERRED_SHARED_MEMORY_CARVEOUT))
+        if p.sharedMemBytes:
+            out.append((p.gridDimX, p.sharedMemBytes, share.sharedMemCarveout))
+    ok(driver.cuGraphDestroy(graph))
+    return sorted(out)
+
+
+def test_a_layers_share_of_the_sm_does_not_depend_on_other_layers(ws):
+    """Room for the CTAs that a launch puts on an SM, whatever the launches of the same kernel before it asked for: few columns take one CTA
+    per SM with most of its shared memory, more take two with less."""
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    few, more = Moe(512, 512, 4), Moe(2048, 768, 4)
+    lora = Lora(1024, 32 * 2 * sms // 128 * 128 + 256, 16, 2)
+    calls = []
+    for moe in (few, more):
+        x, ids, w, r = moe.inputs(1, 2, "share")
+        H.ensure_for_moe(ws, 1, moe.up, 2)
+        y = moe.check(ws, x, ids, w, r)
+        calls.append(lambda s, a=(x, ids, w, moe.up, moe.down, r, y): H.moe_mlp(*a, stream=s))
+    x, ids = lora.inputs(2, "share")
+    H.ensure_for_lora(ws, 2, lora.D, 16)
+    y = H.gemm_lora(x, lora.D, lora.a, lora.b, ids, None)
+    calls.append(lambda s: H.gemm_lora(x, lora.D, lora.a, lora.b, ids, None, y, stream=s))
+    seen = [shared_memory_shares(calls[i]) for i in (1, 0, 1, 0, 2)]
+    assert seen[0] == seen[2] and seen[1] == seen[3]
+    assert len(seen[0]) == len(seen[1]) == 2 and len(seen[4]) == 1
+    assert any(ctas <= sms for ctas, _, _ in seen[1])
+    for ctas, smem, share in seen[0] + seen[1] + seen[4]:
+        on_an_sm = 1 if ctas <= sms else 2
+        assert share / 100 * 228 * 1024 >= on_an_sm * (smem + 1024), (ctas, smem, share)
+    B.check(B.gptq_check_status(), "gptq_check_status")
