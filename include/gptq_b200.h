@@ -318,7 +318,8 @@ int gptq_moe_route(const void *logits, int32_t *expert_ids, float *expert_weight
  * residual may be y; y may be x.  Scratch: gptq_moe_workspace_bytes of the registered workspace (GPTQ_ERR_WORKSPACE without it; what
  * many tokens need does for fewer), under the rules of gptq_set_workspace: calls, and graphs captured from calls, that may run at the same time must not share one.
  * Each expert in use is read once for every 8 of its tokens; M > 64 runs as passes of 64 tokens.  Two kernels per pass, three with
- * act_order.  Layers of another tiling: nothing is stored, and gptq_check_status returns GPTQ_ERR_LAYOUT.
+ * act_order; one ahead of several passes.  Where any expert in use has layers of another tiling nothing is stored, and gptq_check_status
+ * returns GPTQ_ERR_LAYOUT.
  * E <= 1024, top_k <= 32 (GPTQ_ERR_UNSUPPORTED).  Stream semantics and other errors as for gptq_gemm. */
 size_t gptq_moe_workspace_bytes(int M, int K, int F, int top_k, int act_order);
 int gptq_moe_mlp(const void *x, const int32_t *expert_ids, const float *expert_weights, const void *gate_up_qweight,

@@ -1217,6 +1217,13 @@ static int moe_dispatch(const void *x, const int32_t *ids, const float *weights,
     a.sms = sms;
     a.one = 1;
     a.x_by_slot = act_order;
+    if (M > kMoeMaxRows) {
+        static std::atomic<unsigned long long> calls{0};
+        a.call = ++calls;
+        a.ids = ids;
+        st = launch_moe_check(a, (long long)M * top_k, bf16, (cudaStream_t)stream);
+        if (st) return st;
+    }
     for (int m0 = 0; m0 < M; m0 += kMoeMaxRows) {
         a.M = (M - m0) < kMoeMaxRows ? (M - m0) : kMoeMaxRows;
         a.parts = moe_parts(a.M);

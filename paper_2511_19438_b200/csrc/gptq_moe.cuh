@@ -115,7 +115,57 @@ struct MoeArgs {
     uint32_t one;             // 1 (see prepare_rows)
     int x_by_slot;            // rows of x: slots instead of tokens
     int parts;                // of h: rounded to 16 bits, and with 2 what that left, rounded too (see moe_parts)
+    unsigned long long call;  // of a call of several passes: its number, else 0 (see moe_check_kernel)
 };
+
+// whether the layers of an expert, by their trailers' flags, are the ones that the kernels are for
+template <bool BF>
+__device__ __forceinline__ bool moe_layers_fit(uint32_t up, uint32_t down)
+{
+    return (up & (kFormatGateUp | kFormatBf16)) == (kFormatGateUp | (BF ? kFormatBf16 : 0u)) &&
+           (down & (kFormatGateUp | kFormatBf16)) == (BF ? kFormatBf16 : 0u);
+}
+__device__ __forceinline__ uint32_t trailer_flags(const uint8_t *zeros, size_t bytes, int e)
+{
+    return __ldg(&reinterpret_cast<const TiledTrailer *>(zeros + (size_t)(e + 1) * bytes - kTrailerBytes)->flags);
+}
+
+// A call of several passes is refused as a whole: one block goes over the experts that any of its tokens names before the first pass.  Numbers
+// of refused calls stand in a table until the call runs again (a graph's replay) and fits; a call finds its own number or nothing.
+// (Two refused calls under way at once whose numbers are kRefusedCalls apart: the one loses its entry, and is refused pass by pass.)
+constexpr int kRefusedCalls = 256, kMoeCheckThreads = 1024;
+static_assert(kMoeMaxExperts <= kMoeCheckThreads, "a thread per expert");
+__device__ unsigned long long g_refused_calls[kRefusedCalls];
+template <bool BF>
+__global__ void __launch_bounds__(kMoeCheckThreads) moe_check_kernel(const MoeArgs a, long long slots)
+{
+    __shared__ uint32_t named[kMoeCheckThreads / 32];
+    if (threadIdx.x < kMoeCheckThreads / 32) named[threadIdx.x] = 0;
+    pdl_wait();
+    pdl_launch_dependents();
+    __syncthreads();
+    auto name = [&](int e) {
+        if ((unsigned)e < (unsigned)a.E && !(*(volatile uint32_t *)&named[e >> 5] >> (e & 31) & 1)) atomicOr(&named[e >> 5], 1u << (e & 31));
+    };
+    for (long long s = 4 * threadIdx.x; s < slots; s += 4 * kMoeCheckThreads) {
+        if (s + 4 <= slots) {
+            const int4 e = __ldg(reinterpret_cast<const int4 *>(a.ids + s));
+            name(e.x), name(e.y), name(e.z), name(e.w);
+        } else
+            for (long long i = s; i < slots; ++i) name(__ldg(a.ids + i));
+    }
+    __syncthreads();
+    const int e = threadIdx.x;
+    const bool bad = e < a.E && (named[e >> 5] >> (e & 31) & 1) &&
+                     !moe_layers_fit<BF>(trailer_flags(a.gu_z, a.gu_z_bytes, e), trailer_flags(a.dn_z, a.dn_z_bytes, e));
+    if (bad) atomicMax(&g_device_status, (int)kStatusLayoutMismatch);
+    const bool refused = __syncthreads_or(bad);
+    unsigned long long *entry = &g_refused_calls[a.call % kRefusedCalls];
+    if (threadIdx.x == 0) {
+        if (refused) *entry = a.call;
+        else if (*entry == a.call) *entry = 0;
+    }
+}
 
 // The slots (m, j) of a batch grouped by expert, in the order of experts and, within one, of slots.  An expert's slots are cut
 // into SEGMENTS of at most R, the rows that one sweep over the expert's weights serves.
@@ -391,9 +441,7 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_gate_up_kernel
     LanePtrs<SUB> ptrs{};
     const __half *row = nullptr;
     auto row_of = [&](int s) { return a.x + (size_t)(a.x_by_slot ? s : plan.token[s]) * a.K; };
-    auto up_flags = [&](int e) {
-        return __ldg(&reinterpret_cast<const TiledTrailer *>(a.gu_z + (size_t)(e + 1) * a.gu_z_bytes - kTrailerBytes)->flags);
-    };
+    auto up_flags = [&](int e) { return trailer_flags(a.gu_z, a.gu_z_bytes, e); };
     auto next = [&](DirectItem<SUB> &it) {
         l_item += kMoeWarps;
         while (l_item >= G) {
@@ -539,9 +587,6 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_down_kernel(co
     uint32_t l_flags = 0;
     LanePtrs<SUB> ptrs{};
     const __half *row = nullptr;
-    auto trailer_flags = [](const uint8_t *zeros, size_t bytes, int e) {
-        return __ldg(&reinterpret_cast<const TiledTrailer *>(zeros + (size_t)(e + 1) * bytes - kTrailerBytes)->flags);
-    };
     auto next = [&](DirectItem<SUB> &it) {
         l_item += kMoeWarps;
         while (l_item >= l_end) {
@@ -616,15 +661,12 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_down_kernel(co
     while (now < parts) finish_part();
     if (parts) add_up(parts - 1);
 
-    auto fits = [](uint32_t up, uint32_t down) {
-        return (up & (kFormatGateUp | kFormatBf16)) == (kFormatGateUp | (BF ? kFormatBf16 : 0u)) &&
-               (down & (kFormatGateUp | kFormatBf16)) == (BF ? kFormatBf16 : 0u);
-    };
-    bool bad = !fits(up_flags, down_flags);
+    bool bad = !moe_layers_fit<BF>(up_flags, down_flags);
     for (int i = threadIdx.x + kMoeThreads; i < segments; i += kMoeThreads) {
         const int e = plan.seg_expert[i];
-        bad |= !fits(trailer_flags(a.gu_z, a.gu_z_bytes, e), trailer_flags(a.dn_z, a.dn_z_bytes, e));
+        bad |= !moe_layers_fit<BF>(trailer_flags(a.gu_z, a.gu_z_bytes, e), trailer_flags(a.dn_z, a.dn_z_bytes, e));
     }
+    if (a.call && threadIdx.x == 0) bad |= *(volatile unsigned long long *)&g_refused_calls[a.call % kRefusedCalls] == a.call;
     if (bad) {
         s_bad = 1;
         atomicMax(&g_device_status, (int)kStatusLayoutMismatch);
@@ -690,6 +732,11 @@ __global__ void moe_gather_kernel(const __half *__restrict__ x, const int32_t *_
     *reinterpret_cast<uint2 *>(x_out + (size_t)s * K + i) = make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
 }
 
+int launch_moe_check(const MoeArgs &a, long long slots, int bf16, cudaStream_t s)
+{
+    return bf16 ? launch_dependent(moe_check_kernel<true>, dim3(1), kMoeCheckThreads, 0, 1, s, a, slots)
+                : launch_dependent(moe_check_kernel<false>, dim3(1), kMoeCheckThreads, 0, 1, s, a, slots);
+}
 int launch_moe_gather(const __half *x, const int32_t *ids, const int32_t *perm, __half *x_out, int P, int k, int E, int K, cudaStream_t s)
 {
     return launch_dependent(moe_gather_kernel, dim3((unsigned)((K / 4 + 255) / 256), (unsigned)P), 256, 0, 1, s, x, ids, perm, x_out, P, k, E, K);

@@ -799,3 +799,53 @@ def test_a_layers_share_of_the_sm_does_not_depend_on_other_layers(ws):
         on_an_sm = 1 if ctas <= sms else 2
         assert share / 100 * 228 * 1024 >= on_an_sm * (smem + 1024), (ctas, smem, share)
     B.check(B.gptq_check_status(), "gptq_check_status")
+
+
+# ------------------------------------------------------------------------------------------------------------ sizes, several passes
+
+def test_moe_refuses_other_layouts_before_the_first_pass(ws):
+    """A layer of another tiling that only a later pass of 64 tokens names: nothing is stored by the first one either."""
+    moe = Moe(256, 128, 4)
+    x, ids, w, r = moe.inputs(130, 2, "passes")
+    ids[:] = ids % 2
+    ids[ids[:, 0] == ids[:, 1], 1] = 1 - ids[ids[:, 0] == ids[:, 1], 0]
+    good = moe.check(ws, x, ids, w, r)
+    other = Moe(256, 128, 1, dtype=torch.bfloat16)
+    for kind in ("up", "down"):
+        for row, expert in ((64, 2), (129, 3)):
+            stack = getattr(moe, kind)
+            mixed = H.DeviceExperts(**{**stack.__dict__, "qzeros_t": stack.qzeros_t.clone()})
+            mixed.qzeros_t[expert] = getattr(other, kind).qzeros_t[0]
+            pair = (mixed, moe.down) if kind == "up" else (moe.up, mixed)
+            assert torch.equal(H.moe_mlp(x, ids, w, *pair, r), good)           # not named: no matter
+            assert B.gptq_check_status() == B.GPTQ_OK
+            named = ids.clone()
+            named[row, 1] = expert
+            for shared in (False, True):
+                y = x.clone() if shared else torch.full_like(x, 7.0)
+                before = y.clone()
+                H.moe_mlp(y if shared else x, named, w, *pair, r, y)
+                assert B.gptq_check_status() == B.GPTQ_ERR_LAYOUT
+                assert torch.equal(y, before)
+    assert torch.equal(H.moe_mlp(x, ids, w, moe.up, moe.down, r), good)
+    assert B.gptq_check_status() == B.GPTQ_OK
+
+
+def test_moe_refused_in_a_graph(ws):
+    """A captured call of several passes is refused or not as the layers and ids are when it is replayed."""
+    moe, other = Moe(256, 128, 3), Moe(256, 128, 1, dtype=torch.bfloat16)
+    x, ids, w, r = moe.inputs(70, 2, "replay")
+    ids[:] = torch.tensor([0, 1], dtype=torch.int32)
+    want = moe.check(ws, x, ids, w, r)
+    up = H.DeviceExperts(**{**moe.up.__dict__, "qzeros_t": moe.up.qzeros_t.clone()})
+    up.qzeros_t[2] = other.up.qzeros_t[0]
+    y = torch.empty_like(x)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        H.moe_mlp(x, ids, w, up, moe.down, r, y)
+    for bad in (False, True, True, False, True, False):
+        ids[69, 0] = 2 if bad else 0
+        y.fill_(7.0)
+        graph.replay()
+        assert B.gptq_check_status() == (B.GPTQ_ERR_LAYOUT if bad else B.GPTQ_OK)
+        assert torch.equal(y, torch.full_like(y, 7.0) if bad else want)
