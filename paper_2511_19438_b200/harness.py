@@ -239,12 +239,21 @@ def upload_experts(layers: list[QuantLinear], gate_up: bool = False, scales_bf16
                          torch.stack([invert_perm(d.perm) for d in D]) if act else None)
 
 
+def _expect(name: str, t: torch.Tensor | None, dtype: torch.dtype, shape: tuple) -> None:
+    """The kernels take addresses: a tensor of another type, shape or layout would be read as if it had these."""
+    if t is not None and (t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous()):
+        raise ValueError(f"{name}: contiguous {dtype} {list(shape)} expected, got {t.dtype} {list(t.shape)}, strides {list(t.stride())}")
+
+
 _LOGITS_TYPE = {torch.float32: B.GPTQ_LOGITS_F32, torch.float16: B.GPTQ_LOGITS_F16, torch.bfloat16: B.GPTQ_LOGITS_BF16}
 
 
 def moe_route(logits: torch.Tensor, top_k: int, renormalize: bool = True, stream=None) -> tuple[torch.Tensor, torch.Tensor]:
     """(expert ids int32 [M, top_k], weights fp32 [M, top_k]) of router logits [M, E] through gptq_moe_route."""
     M, E = logits.shape
+    if logits.dtype not in _LOGITS_TYPE:
+        raise ValueError(f"logits: float32, float16 or bfloat16 expected, got {logits.dtype}")
+    _expect("logits", logits, logits.dtype, (M, E))
     ids = torch.empty((M, top_k), dtype=torch.int32, device=logits.device)
     weights = torch.empty((M, top_k), dtype=torch.float32, device=logits.device)
     B.check(B.gptq_moe_route(logits, ids, weights, M, E, top_k, _LOGITS_TYPE[logits.dtype], renormalize, stream), "gptq_moe_route")
@@ -255,8 +264,18 @@ def moe_mlp(x: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor, gate_up: 
             residual: torch.Tensor | None = None, y: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """A mixture-of-experts MLP through gptq_moe_mlp or, for bfloat16 x, gptq_moe_mlp_bf16 (workspace: ensure_for_moe)."""
     M, K = x.shape
+    up, dn = gate_up, down
+    if (up.K, up.N, up.count, min(up.group_size, 128), bool(up.act_order)) != (dn.N, 2 * dn.K, dn.count, min(dn.group_size, 128), bool(dn.act_order)):
+        raise ValueError(f"gate_up [{up.K}, {up.N}] x {up.count}, groups of {up.group_size}, act-order {up.act_order} and down [{dn.K}, {dn.N}] x "
+                         f"{dn.count}, groups of {dn.group_size}, act-order {dn.act_order} are not one layer's experts")
     if y is None:
-        y = torch.empty_like(x)
+        y = torch.empty_like(x, memory_format=torch.contiguous_format)
+    act = torch.bfloat16 if x.dtype == torch.bfloat16 else torch.float16
+    _expect("x", x, act, (M, gate_up.K))
+    _expect("ids", ids, torch.int32, (M, ids.shape[-1]))
+    _expect("weights", weights, torch.float32, tuple(ids.shape))
+    _expect("residual", residual, act, (M, K))
+    _expect("y", y, act, (M, K))
     fn = B.gptq_moe_mlp_bf16 if x.dtype == torch.bfloat16 else B.gptq_moe_mlp
     B.check(fn(x, ids, weights, gate_up.qweight_t, gate_up.qzeros_t, gate_up.scales_t, gate_up.perm, down.qweight_t, down.qzeros_t,
                down.scales_t, down.index, residual, y, M, K, down.K, gate_up.count, ids.shape[1], min(gate_up.group_size, 128),
@@ -275,6 +294,14 @@ def gemm_lora(x: torch.Tensor, D: DeviceLinear, lora_a: torch.Tensor, lora_b: to
     M = x.shape[0]
     if y is None:
         y = torch.empty((M, D.N), dtype=x.dtype, device=x.device)
+    act = torch.bfloat16 if x.dtype == torch.bfloat16 else torch.float16
+    adapters, rank = lora_a.shape[0], lora_a.shape[1]
+    _expect("x", x, act, (M, D.K))
+    _expect("lora_a", lora_a, act, (adapters, rank, D.K))
+    _expect("lora_b", lora_b, act, (adapters, D.N, rank))
+    _expect("adapter_ids", adapter_ids, torch.int32, (M,))
+    _expect("adapter_scales", adapter_scales, torch.float32, (adapters,))
+    _expect("y", y, act, (M, D.N))
     fn = B.gptq_gemm_lora_bf16 if x.dtype == torch.bfloat16 else B.gptq_gemm_lora
     B.check(fn(x, D.qweight_t, D.qzeros_t, D.scales_t, D.perm, lora_a, lora_b, adapter_ids, adapter_scales, y, M, D.N, D.K,
                D.group_size, D.act_order, lora_a.shape[1], lora_a.shape[0], stream), fn.__name__)

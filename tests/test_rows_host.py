@@ -4,6 +4,7 @@ import os
 import re
 
 import pytest
+import torch
 
 from paper_2511_19438_b200 import build as libbuild
 
@@ -126,3 +127,64 @@ def test_a_ring_stage_is_refilled_behind_the_whole_warps_reads():
             read = False
         else:
             assert not read, "a copy stands behind a product without a barrier of the warp between them"
+
+
+# ---- the harness: what does not fit together is refused before an address goes anywhere
+
+def experts(K, N, group, act=False, count=4):
+    from paper_2511_19438_b200 import harness as H
+    t = torch.zeros((count, 16), dtype=torch.uint8)
+    return H.DeviceExperts(K, N, group, act, count, t, t, t, None, None)
+
+
+@pytest.fixture
+def no_calls(monkeypatch):
+    """The binding's functions count instead of launching."""
+    calls = []
+    for fn in ("gptq_moe_route", "gptq_moe_mlp", "gptq_moe_mlp_bf16", "gptq_gemm_lora", "gptq_gemm_lora_bf16"):
+        stand_in = lambda *a, **k: calls.append(a) or B.GPTQ_OK
+        stand_in.__name__ = fn
+        monkeypatch.setattr(B, fn, stand_in)
+    return calls
+
+
+def test_harness_experts_that_do_not_fit(no_calls):
+    from paper_2511_19438_b200 import harness as H
+    M, K, F, k = 3, 256, 128, 2
+    good = dict(x=torch.zeros((M, K), dtype=torch.float16), ids=torch.zeros((M, k), dtype=torch.int32), weights=torch.zeros((M, k)),
+                gate_up=experts(K, 2 * F, 128), down=experts(F, K, 128), residual=torch.zeros((M, K), dtype=torch.float16))
+    H.moe_mlp(**good)
+    H.moe_mlp(**{**good, "gate_up": experts(K, 2 * F, 256)})      # (tiled as groups of 128)
+    assert len(no_calls) == 2
+    for bad in (dict(down=experts(F, K, 64)), dict(gate_up=experts(K, 2 * F, 32)), dict(down=experts(2 * F, K, 128)), dict(down=experts(F, 2 * K, 128)),
+                dict(down=experts(F, K, 128, count=3)), dict(down=experts(F, K, 128, act=True)), dict(x=torch.zeros((M, 2 * K), dtype=torch.float16)),
+                dict(x=torch.zeros((M, K))), dict(x=torch.zeros((K, M), dtype=torch.float16).t()), dict(ids=torch.zeros((M, k), dtype=torch.int64)),
+                dict(ids=torch.zeros((k, M), dtype=torch.int32).t()), dict(ids=torch.zeros((M - 1, k), dtype=torch.int32)),
+                dict(weights=torch.zeros((M, k), dtype=torch.float16)), dict(weights=torch.zeros((M, k + 1))),
+                dict(residual=torch.zeros((M, K), dtype=torch.bfloat16)), dict(y=torch.zeros((M, K))), dict(y=torch.zeros((M, 2 * K), dtype=torch.float16)[:, :K])):
+        with pytest.raises(ValueError):
+            H.moe_mlp(**{**good, **bad})
+    assert len(no_calls) == 2
+
+
+def test_harness_adapters_and_logits_that_do_not_fit(no_calls):
+    from paper_2511_19438_b200 import harness as H
+    M, K, N, r, n = 3, 256, 128, 8, 2
+    t = torch.zeros(16, dtype=torch.uint8)
+    D = H.DeviceLinear(K, N, 128, False, t, t, t, None, None)
+    half = lambda *shape: torch.zeros(shape, dtype=torch.float16)
+    good = dict(x=half(M, K), D=D, lora_a=half(n, r, K), lora_b=half(n, N, r), adapter_ids=torch.zeros(M, dtype=torch.int32), adapter_scales=torch.ones(n))
+    H.gemm_lora(**good)
+    H.gemm_lora(**{**good, "adapter_scales": None, "y": half(M, N)})
+    H.moe_route(torch.zeros((M, 8)), 2)
+    assert len(no_calls) == 3
+    for bad in (dict(lora_a=half(n, r, N)), dict(lora_a=torch.zeros((n, r, K))), dict(lora_b=half(n - 1, N, r)), dict(lora_b=half(n, r, N)),
+                dict(adapter_ids=torch.zeros(M, dtype=torch.int64)), dict(adapter_ids=torch.zeros(M + 1, dtype=torch.int32)),
+                dict(adapter_scales=torch.ones(n, dtype=torch.float16)), dict(adapter_scales=torch.ones(n + 1)), dict(x=half(M, 2 * K)),
+                dict(x=half(K, M).t()), dict(x=torch.zeros((M, K), dtype=torch.bfloat16)), dict(y=half(M, N + 8)), dict(y=torch.zeros((M, N)))):
+        with pytest.raises(ValueError):
+            H.gemm_lora(**{**good, **bad})
+    for logits in (torch.zeros((M, 8), dtype=torch.float64), torch.zeros((8, M)).t()):
+        with pytest.raises(ValueError):
+            H.moe_route(logits, 2)
+    assert len(no_calls) == 3
