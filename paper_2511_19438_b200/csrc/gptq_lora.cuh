@@ -242,7 +242,9 @@ __global__ void __launch_bounds__(256, 2) lora_delta_runs_kernel(const __grid_co
     __shared__ float unscale[kDeltaRows];
     pdl_launch_dependents();
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
-    const int n0 = 8 * kDeltaTiles * (8 * blockIdx.x + warp), m0 = kDeltaRows * blockIdx.y, count = min(kDeltaRows, a.M - m0);
+    const int n0 = 8 * kDeltaTiles * (8 * blockIdx.x + warp), m0 = kDeltaRows * (blockIdx.z * gridDim.y + blockIdx.y);
+    if (m0 >= a.M) return;      // (the last of several layers of the grid)
+    const int count = min(kDeltaRows, a.M - m0);
     const int width = (a.rank + 31) & ~31, pitch = 2 * width * 2 + 16;      // a row: hi, lo, 16 bytes against bank conflicts
     int my_id = lane < count ? __ldg(a.ids + m0 + lane) : -1;               // (a row per lane)
     if ((unsigned)my_id >= (unsigned)a.adapters) my_id = -1;
@@ -517,7 +519,9 @@ int launch_lora_delta(const LoraArgs &a, __half *delta, int bf16, cudaStream_t s
         return bf16 ? launch_dependent(lora_delta_rows_kernel<true>, grid, 256, 0, 1, s, a, delta)
                     : launch_dependent(lora_delta_rows_kernel<false>, grid, 256, 0, 1, s, a, delta);
     }
-    const dim3 grid((unsigned)((a.N + 255) / 256), (unsigned)((a.M + kDeltaRows - 1) / kDeltaRows));
+    // a grid is 65535 blocks high: more blocks of rows lie in layers
+    const int blocks = (a.M - 1) / kDeltaRows + 1, layers = (blocks - 1) / 32768 + 1;
+    const dim3 grid((unsigned)((a.N + 255) / 256), (unsigned)((blocks - 1) / layers + 1), (unsigned)layers);
     const size_t smem = (size_t)kDeltaRows * (2 * ((a.rank + 31) & ~31) * 2 + 16);      // at most 33 KB
     return bf16 ? launch_dependent(lora_delta_runs_kernel<true>, grid, 256, smem, 1, s, a, delta)
                 : launch_dependent(lora_delta_runs_kernel<false>, grid, 256, smem, 1, s, a, delta);

@@ -849,3 +849,18 @@ def test_moe_refused_in_a_graph(ws):
         graph.replay()
         assert B.gptq_check_status() == (B.GPTQ_ERR_LAYOUT if bad else B.GPTQ_OK)
         assert torch.equal(y, torch.full_like(y, 7.0) if bad else want)
+
+
+def test_lora_more_rows_than_a_grid_is_high(ws):
+    """65536 blocks of 32 rows and some: the last rows are computed like the first."""
+    lora = Lora(128, 128, 8, 2)
+    M = 32 * 65536 + 40
+    x, ids = lora.inputs(100, "far")
+    far_x, far_ids = torch.zeros((M, 128), dtype=torch.float16, device="cuda"), torch.full((M,), -1, dtype=torch.int32, device="cuda")
+    far_x[-100:], far_ids[-100:] = x, ids
+    H.ensure_for_lora(ws, M, lora.D, 8)
+    y = H.gemm_lora(far_x, lora.D, lora.a, lora.b, far_ids, lora.scales)
+    assert B.gptq_check_status() == B.GPTQ_OK
+    want, most, _ = lora.plain(x, ids, lora.scales)
+    assert ((y[-100:].double() - want).abs() <= most).all()
+    assert not y[:-100].any()
