@@ -9,7 +9,8 @@ namespace gptq {
 // ------------------------------------------------------------------------------ routing
 // One warp per token; lane l holds the logits of experts l, l + 32, ... as keys whose unsigned order is the order of the
 // logits (0: an expert that cannot be chosen).  A pick is two warp-wide reductions: the largest key, then the lowest expert
-// that has it.  The weights are exp(l - max) over their sum, or over the sum of all experts, in fp32.
+// that has it.  The weights are exp(l - max) over their sum, or over the sum of all experts, in fp32, to some steps of 2^-24 (a lane forms the
+// exponential of its own pick, behind the picks).
 // Bound by the chain of 2 k reductions: 4096 tokens, 128 experts in bfloat16, top 8: 4.0 us, 0.2 would be its memory's.
 constexpr int kRouteMaxExperts = 1024, kRouteMaxTopK = 32, kRouteWarps = 4;
 
@@ -27,6 +28,19 @@ __device__ __forceinline__ uint32_t logit_key(uint32_t b)
     return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k); }
+// exp(l - top) to a few steps of 2^-24 for every l: of x = l - top and of t = x log2(e) the fast exponential takes only the rounded values, whose
+// errors grow with x (100 steps at l = top - 80).  Both errors are known exactly - x's by the two-term sum of two floats, t's by an
+// fma and the rest of log2(e) - and enter as the factor 2^r = 1 + r ln 2.
+__device__ __forceinline__ float exp_below(float l, float top)
+{
+    constexpr float kLog2e = 1.44269504f, kLog2eRest = 1.92596299e-8f, kLn2 = 0.693147181f;
+    const float x = __fsub_rn(l, top), back = __fadd_rn(x, top);
+    const float x_rest = __fsub_rn(__fsub_rn(l, back), __fsub_rn(top, __fsub_rn(back, x)));
+    const float t = __fmul_rn(x, kLog2e), r = __fmaf_rn(x_rest, kLog2e, __fmaf_rn(x, kLog2eRest, __fmaf_rn(x, kLog2e, -t)));
+    float p;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(p) : "f"(t));
+    return t > -126.f ? __fmaf_rn(p, r * kLn2, p) : p;
+}
 
 template <int NV>
 __global__ void __launch_bounds__(32 * kRouteWarps)
@@ -57,7 +71,7 @@ route_kernel(const void *__restrict__ logits, int type, int32_t *__restrict__ id
                 float sum = 0.f;
 #pragma unroll
                 for (int i = 0; i < NV; ++i)
-                    if (key[i]) sum += __expf(key_logit(key[i]) - top);
+                    if (key[i]) sum += exp_below(key_logit(key[i]), top);
 #pragma unroll
                 for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
                 total = sum;
@@ -71,13 +85,18 @@ route_kernel(const void *__restrict__ logits, int type, int32_t *__restrict__ id
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if (e == (uint32_t)(lane + 32 * i)) key[i] = 0;
-        const float p = __expf(key_logit(all) - top);
-        if (renormalize) total += p;
-        if (lane == j) { mine = p; my_id = (int)e; }
+        if (lane == j) { mine = key_logit(all); my_id = (int)e; }
+    }
+    // a lane's pick: its exponential, and the picks' sum
+    const float p = my_id >= 0 ? exp_below(mine, top) : 0.f;
+    if (renormalize) {
+        total = p;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
     }
     if (lane < k) {
         ids[(size_t)m * k + lane] = my_id;
-        weights[(size_t)m * k + lane] = my_id >= 0 ? mine / total : 0.f;
+        weights[(size_t)m * k + lane] = my_id >= 0 ? p / total : 0.f;
     }
 }
 

@@ -864,3 +864,18 @@ def test_lora_more_rows_than_a_grid_is_high(ws):
     want, most, _ = lora.plain(x, ids, lora.scales)
     assert ((y[-100:].double() - want).abs() <= most).all()
     assert not y[:-100].any()
+
+
+def test_route_weights_of_spread_logits():
+    """p = exp(l - max): 2^-22 for the exponential (two steps, as CUDA gives for ex2.approx) and 2^-23 for what goes into it, in numerator
+    and sum alike, 2^-22 for the division (two steps), 2^-24 for each addition."""
+    g = gen("route-spread")
+    for E, k in ((8, 8), (64, 32), (1000, 32)):
+        logits = (85 * torch.rand((200, E), generator=g, device="cuda") - 40).float()
+        for renormalize in (True, False):
+            ids, w = H.moe_route(logits, k, renormalize)
+            want_ids, want = plain_route(logits, k, renormalize)
+            assert np.array_equal(ids.cpu().numpy(), want_ids)
+            err = np.abs(w.cpu().double().numpy() - want) / want
+            # the sum over all experts: E / 32 additions in a lane and five between lanes
+            assert err.max() <= 2 * (2.0 ** -22 + 2.0 ** -23) + 2.0 ** -22 + (k if renormalize else E / 32 + 5) * 2.0 ** -24, (E, renormalize, err.max() * 2 ** 24)
