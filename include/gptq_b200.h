@@ -288,8 +288,8 @@ int gptq_gemm_w8(const void *x, const void *qweight, const void *qzeros, const v
  * order, equal logits by ascending expert: expert_ids int32[M, top_k], and their weights fp32[M, top_k] = softmax over all E
  * logits (renormalize = 0), or over the chosen ones (renormalize != 0: they sum to one).  logits: [M, E] of logits_type.
  * A logit of -inf or NaN is an expert that cannot be chosen and has no share in the softmax; +inf counts as the largest finite
- * number.  Where fewer than top_k can be chosen, the rest of the row is expert -1 with weight 0.  A weight is good to about ten steps of 2^-24
- * of itself, and one for each expert of the sum, however far its logit is below the largest (86 and more below: 0).
+ * number.  Where fewer than top_k can be chosen, the rest of the row is expert -1 with weight 0.  A weight is good to 16 steps of 2^-24 of
+ * itself, and one for each expert of the sum, however far its logit is below the largest (87 and more below: 0).
  * E <= 1024, top_k <= 32 (GPTQ_ERR_UNSUPPORTED), top_k <= E (GPTQ_ERR_SHAPE); pointers 16-byte aligned; an unknown
  * logits_type: GPTQ_ERR_LAYOUT. */
 #define GPTQ_LOGITS_F32 0

@@ -17,7 +17,12 @@ namespace gptq {
 constexpr int kLoraMaxRank = 256;
 constexpr int kLoraDirectRows = 8;       // rows of the fused kernel
 constexpr int kLoraWarps = 8, kLoraThreads = 32 * kLoraWarps;
-constexpr int kLoraDecodeRows = 64;      // up to here rows are taken to have adapters of their own, above to come in runs
+// Up to here rows are taken to have adapters of their own (a CTA of the shrink kernel per adapter of eight rows, lora_delta_rows_kernel), above
+// to come in runs of one (a CTA takes eight rows' adapters in turn, lora_delta_runs_kernel).  The ids would tell, but they are on the device.
+// Whole calls in us, own adapters / one adapter, 5120 x 5120, rank 32: 16 rows 17.0 / 14.9 this way and 35.6 / 13.7 the other; 64 rows
+// 32.8 / 26.4 and 67.8 / 18.5; 128 rows 47.0 / 35.2 and 72.0 / 22.4; 256 rows 71.6 / 50.0 and 124 / 28.0.  So a short prompt of one adapter and
+// a decode batch of more than 64 rows get the slower way: by up to 2.1 (rank 64, 64 rows: 50.7 for 23.7) and 2.7 times (rank 16, 256: 108 for 39.3).
+constexpr int kLoraDecodeRows = 64;
 constexpr int kLoraSteps = 4;            // 32-column steps of K that a warp of the shrink kernel requests at once
 
 template <int N>
@@ -174,8 +179,8 @@ __device__ __forceinline__ uint32_t pack16(float a, float b)
 //
 // Decode batches, every row with an adapter of its own: a column of B has rank / 8 pieces of 16 bytes; neighbouring lanes read
 // neighbouring pieces, multiply them with their 8 values of v, which they keep, and add up.  A warp takes a row and kDeltaSteps times the
-// columns that its lanes read at once, all requested before the first is used.  Bound by those reads: every row has its own B.  64 rows of 5120 x 5120, rank 32: 33 us with the
-// shrink kernel and the matmul, which alone takes 13.4.
+// columns that its lanes read at once, all requested before the first is used.  Every row has its own B; 60 % of the issue slots, 19 % of
+// the DRAM rate, the stalls waits for loads.  64 rows of 5120 x 5120, rank 32: 33 us with the shrink kernel and the matmul, which alone takes 13.4.
 constexpr int kDeltaSteps = 4;
 template <bool BF>
 __global__ void __launch_bounds__(256, 4) lora_delta_rows_kernel(const LoraArgs a, __half *__restrict__ delta)
@@ -344,7 +349,8 @@ __global__ void __launch_bounds__(256, 2) lora_delta_runs_kernel(const __grid_co
 // tile's items along K, leave their sums and go on, and add up at the next tile's end.  W: 8 warps, two CTAs per SM; where there is no
 // more than a pair of units for each SM, 16 warps and one (4096 x 4096, rank 16, one row, with the shrink kernel: 0.3 us
 // less, now 6.3).
-// 8 rows of 8 adapters, 4096 x 12288: 13.0 us, bound by instruction issue; the shared matmul alone takes 8.5 in the decode kernel.
+// 8 rows of 8 adapters, 4096 x 12288: 13.0 us with the shrink kernel, the shared matmul alone 8.5 in the decode kernel.  Neither issue (43 % of
+// the slots) nor DRAM (22 %) is full: most of the stalls are waits for loads.
 template <int W, int NU, int SUB, bool BF>
 __global__ void __launch_bounds__(32 * W, 16 / W)
 lora_gemm_kernel(const LoraArgs a, const __half *x, const uint8_t *qweight, const uint8_t *scales, const uint8_t *qzeros,
@@ -466,7 +472,9 @@ lora_gemm_kernel(const LoraArgs a, const __half *x, const uint8_t *qweight, cons
 }
 
 // The parts of K that the shrink kernel sums apart: so many that a warp has one batch of steps - a second one costs a round trip to
-// memory, 64 rows of 64 adapters of 5120 x 32: 17 us with five parts, 22 with four - as long as the CTAs are not too many anyway.
+// memory - as long as the CTAs are not too many anyway.  Whole calls: 64 rows of 64 adapters of 5120 x 5120 x 32 32.8 us with five parts, 33.9
+// with four; 13 rows of 11008 x 4096 x 64 21.8 with eleven, 22.2 with eight, 23.9 with four; one row of 11008 x 4096 x 16, where adding the parts up
+// counts for more, 10.4, 10.1 and 9.9.  750 or 4000 CTAs at most make no difference to these.
 constexpr int kLoraMaxParts = 12, kLoraMaxCtas = 1500;
 inline int lora_k_parts(int M, int K, int rank)
 {

@@ -784,6 +784,7 @@ constexpr int kHalfSmBytes = 227 * 1024 / 2 - 1024;      // of a CTA that shares
 template <int NU, int SUB>
 static int moe_red_and_ring_bytes() { return 2 * kMoeWarps * 4 * NU * 32 * 4 + direct_ring_bytes<NU, SUB>(kMoeWarps); }
 
+// (From about 1024 slots in a pass on - 64 tokens, top 16 - the slot plan leaves room for one CTA on an SM; the other half of the grid follows it.)
 template <int NU, int SUB, bool BF>
 static int launch_gate_up(const MoeArgs &a, int most, cudaStream_t s)
 {
