@@ -702,8 +702,11 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_down_kernel(co
                 const int e = plan.key[s];
                 if (e < 0) continue;
                 const UnitPtrs p = unit_ptrs<SUB>(a.dn_w + e * a.dn_w_bytes, a.dn_s + e * a.dn_s_bytes, a.dn_z + e * a.dn_z_bytes, panel, G, unit + c / 16);
-                v = fmaf(plan.weight[s], long_sum<BF>(p.w, p.s, p.z, SUB, c % 16, trailer_flags(a.dn_z, a.dn_z_bytes, e) & kFormatZerosMinusOne,
-                                                      a.h + (size_t)s * a.F, G, true), v);
+                const uint32_t z_add = trailer_flags(a.dn_z, a.dn_z_bytes, e) & kFormatZerosMinusOne;
+                const __half *h = a.h + (size_t)s * a.F;
+                v = fmaf(plan.weight[s], long_sum<BF>(p.w, p.s, p.z, SUB, c % 16, z_add, h, G, true), v);
+                // (h's second part: in fp16 an infinity brought us here, which has none that counts)
+                if (BF && a.parts == 2) v = fmaf(plan.weight[s], long_sum<BF>(p.w, p.s, p.z, SUB, c % 16, z_add, h + (size_t)a.M * a.k * a.F, G, true), v);
             }
         }
         store_out16<BF>(a.y + place(o), v + residual);

@@ -879,3 +879,29 @@ def test_route_weights_of_spread_logits():
             err = np.abs(w.cpu().double().numpy() - want) / want
             # the sum over all experts: E / 32 additions in a lane and five between lanes
             assert err.max() <= 2 * (2.0 ** -22 + 2.0 ** -23) + 2.0 ** -22 + (k if renormalize else E / 32 + 5) * 2.0 ** -24, (E, renormalize, err.max() * 2 ** 24)
+
+
+def test_moe_bf16_overflowing_parts_keep_both_parts_of_h(ws):
+    """One h of 2^122 in a row: (128 + q) h is beyond fp32's range, and the second of its two 16-bit parts still counts (moe.check's bound
+    allows one rounding of y)."""
+    moe = Moe.__new__(Moe)
+    moe.K, moe.F, moe.E, moe.dtype = 256, 128, 1, torch.bfloat16
+    up, bits, _ = heavy(1, 256, 256, True)
+    bits[0][:] = 0
+    bits[0][:, [5, 128 + 5]] = wl.bf16_bits(np.float32([3 * 2.0 ** -8]))[0]
+    moe.up = H.upload_experts(up, gate_up=True, scales_bf16_bits=bits)
+    moe.up64 = [H.to_device(oracle.dequant_f32_bf16(up[0].qweight, up[0].qzeros, bits[0], up[0].g_idx, 128, False)).double()]
+    down = heavy(1, 128, 256, True)
+    moe.down, moe.down64 = H.upload_experts(down[0], scales_bf16_bits=down[1]), down[2]
+    for M in (3, 16):
+        x = (2.0 ** 58 * (1 + torch.randint(0, 128, (M, 1), generator=gen("parts", M), device="cuda") / 128)).expand(M, 256).to(torch.bfloat16).contiguous()
+        moe.check(ws, x, torch.zeros((M, 1), dtype=torch.int32, device="cuda"), torch.ones((M, 1), device="cuda"), None)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("M", [65, 144])
+def test_moe_several_passes_of_act_order_layers(ws, M, dtype):
+    moe = Moe(256, 128, 5, 64, True, True, dtype)
+    x, ids, w, r = moe.inputs(M, 3, "passes-act")
+    ids[M // 2] = -1
+    moe.check(ws, x, ids, w, r)
