@@ -340,11 +340,10 @@ int gptq_moe_mlp_bf16(const void *x, const int32_t *expert_ids, const float *exp
  * adapter_scales fp32 [adapters] or NULL (1).  An id outside 0 .. adapters-1: the row has no adapter.  rank: a multiple of 8 up
  * to 256 (GPTQ_ERR_UNSUPPORTED).  W, x, y, g_idx, act_order, errors and accuracy of the product with W as for gptq_gemm; with
  * act_order = 1 x and lora_a are in the checkpoint's row order, with GPTQ_ACT_ORDER_PRESORTED both are in the sorted one.
- * x A^T, scaled, is summed and kept in fp32.  Up to 8 rows the expansion joins the fp32 sums before the one rounding of y (two
+ * x A^T, scaled, is summed and kept in fp32 (above 64 rows multiplied as two 16-bit numbers, good to 2^-22 of it, in bfloat16 2^-16).  Up to 8 rows the expansion joins the fp32 sums before the one rounding of y (two
  * kernels, three with act_order = 1; the products are those of gptq_gemm's one and two rows: sum q x and z sum x apart, and again the slow
- * way where that gives infinities or NaN); above, it
- * is rounded to 16 bits on its way to them (a value beyond 65504 becomes an infinity; two kernels and gptq_gemm's).  A row's result does not depend on the other rows'
- * adapters, whatever these hold.  y must not be x (GPTQ_ERR_LAYOUT).  Scratch: gptq_lora_workspace_bytes of the registered workspace, always needed
+ * way where that gives infinities or NaN); above, it is rounded to 16 bits on its way to them (a value beyond 65504 becomes an infinity; two
+ * kernels and gptq_gemm's).  A row's result does not depend on the other rows' adapters, whatever these hold.  y must not be x (GPTQ_ERR_LAYOUT).  Scratch: gptq_lora_workspace_bytes of the registered workspace, always needed
  * (GPTQ_ERR_WORKSPACE without it; what many rows need does for fewer, of the same N, K, rank and act_order), under the rules of
  * gptq_set_workspace.  A layer tiled with GPTQ_FORMAT_GATE_UP or GPTQ_FORMAT_BF16 is refused as by gptq_gemm. */
 size_t gptq_lora_workspace_bytes(int M, int N, int K, int group_size, int act_order, int rank);

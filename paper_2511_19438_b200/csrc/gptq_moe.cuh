@@ -427,7 +427,7 @@ __device__ __forceinline__ void store_h(const MoeArgs &a, __half *at, float v)
 // the next tile's end, when all have long arrived.
 //
 // Bound by instruction issue: 64 rows, 32 experts of 4096 x 2048, top 4: 2.4 instructions per clock and SM at 51 % of the DRAM rate and
-// 34 % of the tensor pipe's.  Two CTAs of 8 warps per SM with rings; the whole layer of 64 rows takes 155 us (65 would be its memory's),
+// 34 % of the tensor pipe's.  Two CTAs of 8 warps per SM with rings; the whole layer of 64 rows takes 156 us (65 would be its memory's),
 // 167 with one CTA of 16 warps per SM.
 template <int NU, int SUB, bool BF>
 __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_gate_up_kernel(const MoeArgs a)
@@ -569,7 +569,7 @@ __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_gate_up_kernel
 // kernel 1; what its warps leave of it is added up, weighted, in a [token][column] tile in shared memory, part after part, and
 // the CTAs' tiles in the order of ranks: the order of all sums is fixed.
 // Clusters, because a few tokens leave too few columns for the machine: as many CTAs as fill two per SM, up to 8 to a cluster.  One row,
-// 8 experts of 4096 x 11008, top 2: both kernels 39 us, 22 would be their memory's.
+// 8 experts of 4096 x 11008, top 2: both kernels 40 us, 22 would be their memory's.
 template <int NU, int SUB, bool BF>
 __global__ void __launch_bounds__(kMoeThreads, kMoeCtasPerSm) moe_down_kernel(const MoeArgs a, int S)
 {
