@@ -355,6 +355,48 @@ int gptq_gemm_lora_bf16(const void *x, const void *qweight, const void *qzeros, 
                         const void *lora_a, const void *lora_b, const int32_t *adapter_ids, const float *adapter_scales, void *y,
                         int M, int N, int K, int group_size, int act_order, int rank, int adapters, void *stream);
 
+/* ---- 8-bit floating point with a scale for each block of 128 (no counterpart in the paper, whose layers are GPTQ - Section 1) ----
+ * Layers as checkpoints hold them, nothing is repacked: weight e4m3 [N, K] (a byte each, output features first), weight_scales fp32
+ * [ceil(N / 128), ceil(K / 128)], w[n, k] = weight[n, k] * weight_scales[n / 128, k / 128].  Rows of activations or gradients: e4m3
+ * [M, K] and x_scales fp32 [M, ceil(K / 128)].  e4m3: 1 sign, 4 exponent (bias 7), 3 fraction bits, largest number 448, no infinities.
+ * `format`: 0 (16-bit inputs and results are fp16) or GPTQ_FORMAT_BF16 (bfloat16); anything else: GPTQ_ERR_LAYOUT.
+ * K is a multiple of 16, N of 8 (GPTQ_ERR_SHAPE); a last block may have fewer than 128.  Pointers, NULL or not, are 16-byte aligned.
+ * Stream semantics as for gptq_gemm: launches overlap the end of earlier kernels on the stream, and weights (not their scales, nor anything
+ * else) are read before these have ended, which matters only if the kernel in front writes weights and lets later kernels start early. */
+
+/* Rows to e4m3: for each 128 columns of a row s = max(max|x| / 448, 2^-126) and q = x / s, both quotients and q rounded to the nearest
+ * (ties to even).  Numbers below 2^-126 count as zero; a block that holds an infinity or a NaN has s infinite or NaN, and every product with it is NaN. */
+int gptq_fp8_quantize(const void *x, void *x_fp8, float *x_scales, int M, int K, int format, void *stream);
+
+/* The layer the other way round, for products with its transpose: weight_out e4m3 [K, N], scales_out [ceil(K / 128), ceil(N / 128)]; it
+ * dequantises to the same numbers.  N is a multiple of 16.  Once per layer, like a repack. */
+int gptq_fp8_transpose(const void *weight, const float *weight_scales, void *weight_out, float *scales_out, int N, int K, void *stream);
+
+/* y 16-bit [M, N] = x w^T + bias[N] + residual[M, N] (either NULL: none; 16-bit, of y's type; residual may be y).  x_scales != NULL: x is e4m3.
+ * NULL: x is 16-bit [M, K] and becomes e4m3 as by gptq_fp8_quantize, in the registered workspace: gptq_fp8_workspace_bytes(M, K)
+ * (GPTQ_ERR_WORKSPACE without it), under the rules of gptq_set_workspace.  Sums over a block of 128 in the tensor core's fp32, times the two
+ * scales (their product in fp32: below 2^-126 it counts as zero), over blocks, bias and residual in fp32, one rounding of y.  The order of the sums is fixed.
+ * y must not be x (GPTQ_ERR_LAYOUT).  The gradient of x is the same call with the gradient of y in the place of x and the layer of
+ * gptq_fp8_transpose (rounding to e4m3 counts as the identity). */
+size_t gptq_fp8_workspace_bytes(int M, int K);
+int gptq_gemm_fp8(const void *x, const float *x_scales, const void *weight, const float *weight_scales, const void *bias,
+                  const void *residual, void *y, int M, int N, int K, int format, void *stream);
+
+/* The first half of a gated feed-forward block: out[M, F] = silu(x Wg^T) * (x Wu^T), weight [2 F, K] = gate rows, then up rows; F is a multiple of
+ * 128.  out_scales != NULL: out is e4m3 [M, F] with out_scales [M, F / 128], formed from the fp32 result as by gptq_fp8_quantize: what
+ * gptq_gemm_fp8 takes for the down projection.  NULL: out is 16-bit.  Otherwise as gptq_gemm_fp8; the exponential is the fast one (2^-20 of the
+ * result for gates above -10). */
+int gptq_gemm_fp8_silu_mul(const void *x, const float *x_scales, const void *weight, const float *weight_scales, void *out,
+                           float *out_scales, int M, int F, int K, int format, void *stream);
+
+/* The way back: from d_out 16-bit [M, F], the gradient of that result, the gradients of the two projections' outputs
+ *     d_gate = d_out * up * p * (1 + gate * (1 - p)),  d_up = d_out * gate * p,  p = 1 / (1 + exp(-gate))
+ * with gate and up formed again from x and weight.  d_gate_up [M, 2 F] = gate's columns, then up's: e4m3 with d_gate_up_scales [M, 2 F / 128],
+ * or (NULL) 16-bit.  The gradient of x is gptq_gemm_fp8(d_gate_up, d_gate_up_scales, the layer of gptq_fp8_transpose, ..., M, K, 2 F).
+ * d_gate_up must not be x or d_out.  Otherwise as gptq_gemm_fp8_silu_mul. */
+int gptq_gemm_fp8_silu_mul_backward(const void *x, const float *x_scales, const void *weight, const float *weight_scales, const void *d_out,
+                                    void *d_gate_up, float *d_gate_up_scales, int M, int F, int K, int format, void *stream);
+
 /* Process-wide switch: with enable != 0, gptq_gemm runs problems with M >= 256 and an even number
  * of 128-column panels on CTA pairs (tcgen05.mma.cta_group::2: two SMs share one 256 x 256 x 16 MMA and
  * each loads half of the x tile).  Same arithmetic and tolerance as the default kernel; it halves the

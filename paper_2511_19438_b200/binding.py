@@ -93,6 +93,12 @@ _SIGNATURES = {
     "gptq_lora_workspace_bytes": (_sz, [_i] * 6),
     "gptq_gemm_lora": (_i, [_vp] * 10 + [_i] * 7 + [_vp]),
     "gptq_gemm_lora_bf16": (_i, [_vp] * 10 + [_i] * 7 + [_vp]),
+    "gptq_fp8_quantize": (_i, [_vp] * 3 + [_i] * 3 + [_vp]),
+    "gptq_fp8_transpose": (_i, [_vp] * 4 + [_i] * 2 + [_vp]),
+    "gptq_fp8_workspace_bytes": (_sz, [_i] * 2),
+    "gptq_gemm_fp8": (_i, [_vp] * 7 + [_i] * 4 + [_vp]),
+    "gptq_gemm_fp8_silu_mul": (_i, [_vp] * 6 + [_i] * 4 + [_vp]),
+    "gptq_gemm_fp8_silu_mul_backward": (_i, [_vp] * 7 + [_i] * 4 + [_vp]),
     "gptq_set_cta_pairs": (_i, [_i]),
     "gptq_gemm_host": (_i, [_vp] * 8 + [_i, _i, _i, _i, _i, _vp]),
     "gptq_gemm_noalloc": (_i, [_vp] * 6 + [_i, _i, _i, _i, _i, _vp]),
@@ -313,6 +319,34 @@ def gptq_gemm_lora_bf16(x, qweight, qzeros, scales, g_idx, lora_a, lora_b, adapt
     return _lib.gptq_gemm_lora_bf16(_ptr(x), _ptr(qweight), _ptr(qzeros), _ptr(scales), _ptr(g_idx), _ptr(lora_a), _ptr(lora_b),
                                     _ptr(adapter_ids), _ptr(adapter_scales), _ptr(y), M, N, K, group_size, int(act_order), rank,
                                     adapters, _stream(stream))
+
+
+def gptq_fp8_quantize(x, x_fp8, x_scales, M, K, fmt, stream=None) -> int:
+    return _lib.gptq_fp8_quantize(_ptr(x), _ptr(x_fp8), _ptr(x_scales), M, K, int(fmt), _stream(stream))
+
+
+def gptq_fp8_transpose(weight, weight_scales, weight_out, scales_out, N, K, stream=None) -> int:
+    return _lib.gptq_fp8_transpose(_ptr(weight), _ptr(weight_scales), _ptr(weight_out), _ptr(scales_out), N, K, _stream(stream))
+
+
+def gptq_fp8_workspace_bytes(M, K) -> int:
+    return _lib.gptq_fp8_workspace_bytes(M, K)
+
+
+def gptq_gemm_fp8(x, x_scales, weight, weight_scales, bias, residual, y, M, N, K, fmt, stream=None) -> int:
+    return _lib.gptq_gemm_fp8(_ptr(x), _ptr(x_scales), _ptr(weight), _ptr(weight_scales), _ptr(bias), _ptr(residual), _ptr(y), M, N, K,
+                              int(fmt), _stream(stream))
+
+
+def gptq_gemm_fp8_silu_mul(x, x_scales, weight, weight_scales, out, out_scales, M, F, K, fmt, stream=None) -> int:
+    return _lib.gptq_gemm_fp8_silu_mul(_ptr(x), _ptr(x_scales), _ptr(weight), _ptr(weight_scales), _ptr(out), _ptr(out_scales), M, F, K,
+                                       int(fmt), _stream(stream))
+
+
+def gptq_gemm_fp8_silu_mul_backward(x, x_scales, weight, weight_scales, d_out, d_gate_up, d_gate_up_scales, M, F, K, fmt,
+                                    stream=None) -> int:
+    return _lib.gptq_gemm_fp8_silu_mul_backward(_ptr(x), _ptr(x_scales), _ptr(weight), _ptr(weight_scales), _ptr(d_out), _ptr(d_gate_up),
+                                                _ptr(d_gate_up_scales), M, F, K, int(fmt), _stream(stream))
 
 
 def gptq_set_cta_pairs(enable) -> int:

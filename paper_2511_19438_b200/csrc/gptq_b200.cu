@@ -13,6 +13,7 @@
 #include "gptq_direct.cuh"
 #include "gptq_moe.cuh"
 #include "gptq_lora.cuh"
+#include "gptq_fp8.cuh"
 
 #include <atomic>
 #include <cstdio>
@@ -1334,6 +1335,110 @@ int gptq_gemm_lora_bf16(const void *x, const void *qweight, const void *qzeros, 
 {
     return lora_dispatch(x, qweight, qzeros, scales, g_idx, lora_a, lora_b, adapter_ids, adapter_scales, y, M, N, K, group_size,
                          act_order, rank, adapters, stream, 1);
+}
+
+}  // extern "C"
+
+// ---- layers in 8-bit floating point (gptq_fp8.cuh) -------------------------------------------------------------------------
+
+// e4m3 x and its scales in the registered workspace, for calls that bring x in 16 bits
+static size_t fp8_x_bytes(int M, int K) { return ((size_t)M * K + 255) & ~(size_t)255; }
+static size_t fp8_workspace_need(int M, int K) { return fp8_x_bytes(M, K) + (size_t)M * fp8_blocks(K) * sizeof(float); }
+
+static int check_fp8(int M, int N, int K, int format)
+{
+    if (format & ~GPTQ_FORMAT_BF16) return GPTQ_ERR_LAYOUT;
+    if (M < 1 || N < 8 || K < 16 || N % 8 || K % 16) return GPTQ_ERR_SHAPE;
+    return GPTQ_OK;
+}
+
+static int fp8_dispatch(Fp8Call c, int format, void *stream)
+{
+    int st = check_fp8(c.M, c.N, c.K, format);
+    if (st) return st;
+    if (c.kind != kFp8Plain && c.N % (2 * kFp8Block)) return GPTQ_ERR_SHAPE;
+    if (!c.x || !c.w || !c.w_scales || !c.out || (c.kind == kFp8Backward && !c.in)) return GPTQ_ERR_NULL;
+    const void *ptrs[] = {c.x, c.x_scales, c.w, c.w_scales, c.bias, c.in, c.out, c.out_scales};
+    for (const void *p : ptrs)
+        if (!aligned16(p)) return GPTQ_ERR_ALIGN;
+    if (c.out == c.x || (c.kind == kFp8Backward && c.out == c.in)) return GPTQ_ERR_LAYOUT;      // rows of them are read while others of the result are written
+    int dev;
+    st = current_device_sms(&dev, &c.sms);
+    if (st) return st;
+    c.bf16 = format & GPTQ_FORMAT_BF16 ? 1 : 0;
+    cudaStream_t s = (cudaStream_t)stream;
+    if (c.x_scales == nullptr) {
+        uint8_t *ws;
+        st = registered_workspace(dev, fp8_workspace_need(c.M, c.K), &ws);
+        if (st) return st;
+        float *scales = (float *)(ws + fp8_x_bytes(c.M, c.K));
+        st = launch_fp8_quantize(c.x, ws, scales, c.M, c.K, c.bf16, c.sms, s);
+        if (st) return st;
+        c.x = ws, c.x_scales = scales;
+    }
+    return launch_fp8(c, s);
+}
+
+extern "C" {
+
+int gptq_fp8_quantize(const void *x, void *x_fp8, float *x_scales, int M, int K, int format, void *stream)
+{
+    int st = check_fp8(M, 8, K, format);
+    if (st) return st;
+    if (!x || !x_fp8 || !x_scales) return GPTQ_ERR_NULL;
+    if (!aligned16(x) || !aligned16(x_fp8) || !aligned16(x_scales)) return GPTQ_ERR_ALIGN;
+    if (x == x_fp8) return GPTQ_ERR_LAYOUT;
+    int dev, sms;
+    st = current_device_sms(&dev, &sms);
+    if (st) return st;
+    return launch_fp8_quantize(x, x_fp8, x_scales, M, K, format & GPTQ_FORMAT_BF16 ? 1 : 0, sms, (cudaStream_t)stream);
+}
+
+int gptq_fp8_transpose(const void *weight, const float *weight_scales, void *weight_out, float *scales_out, int N, int K, void *stream)
+{
+    if (N < 16 || K < 16 || N % 16 || K % 16) return GPTQ_ERR_SHAPE;
+    if (!weight || !weight_scales || !weight_out || !scales_out) return GPTQ_ERR_NULL;
+    if (!aligned16(weight) || !aligned16(weight_scales) || !aligned16(weight_out) || !aligned16(scales_out)) return GPTQ_ERR_ALIGN;
+    if (weight == weight_out || weight_scales == scales_out) return GPTQ_ERR_LAYOUT;
+    return launch_fp8_transpose(weight, weight_scales, weight_out, scales_out, N, K, (cudaStream_t)stream);
+}
+
+size_t gptq_fp8_workspace_bytes(int M, int K)
+{
+    if (check_fp8(M, 8, K, 0) != GPTQ_OK) return 0;
+    return fp8_workspace_need(M, K);
+}
+
+int gptq_gemm_fp8(const void *x, const float *x_scales, const void *weight, const float *weight_scales, const void *bias,
+                  const void *residual, void *y, int M, int N, int K, int format, void *stream)
+{
+    Fp8Call c{};
+    c.kind = kFp8Plain;
+    c.x = x, c.x_scales = x_scales, c.w = weight, c.w_scales = weight_scales, c.bias = bias, c.in = residual, c.out = y;
+    c.M = M, c.N = N, c.K = K;
+    return fp8_dispatch(c, format, stream);
+}
+
+int gptq_gemm_fp8_silu_mul(const void *x, const float *x_scales, const void *weight, const float *weight_scales, void *out,
+                           float *out_scales, int M, int F, int K, int format, void *stream)
+{
+    if (F < 1 || F > (1 << 29)) return GPTQ_ERR_SHAPE;
+    Fp8Call c{};
+    c.kind = kFp8Gated;
+    c.x = x, c.x_scales = x_scales, c.w = weight, c.w_scales = weight_scales, c.out = out, c.out_scales = out_scales;
+    c.M = M, c.N = 2 * F, c.K = K;
+    return fp8_dispatch(c, format, stream);
+}
+
+int gptq_gemm_fp8_silu_mul_backward(const void *x, const float *x_scales, const void *weight, const float *weight_scales, const void *d_out,
+                                    void *d_gate_up, float *d_gate_up_scales, int M, int F, int K, int format, void *stream)
+{
+    if (F < 1 || F > (1 << 29)) return GPTQ_ERR_SHAPE;
+    Fp8Call c{};
+    c.kind = kFp8Backward;
+    c.x = x, c.x_scales = x_scales, c.w = weight, c.w_scales = weight_scales, c.in = d_out, c.out = d_gate_up, c.out_scales = d_gate_up_scales;
+    c.M = M, c.N = 2 * F, c.K = K;
+    return fp8_dispatch(c, format, stream);
 }
 
 }  // extern "C"

@@ -1,0 +1,589 @@
+// Layers in 8-bit floating point (e4m3 with a scale for each block of 128): rows to e4m3, products, the gated block and its gradients.
+//
+//     y[m, n] = sum_kb sx[m, kb] sw[n / 128, kb] sum_{k in block kb} qx[m, k] qw[n, k]
+//
+// The inner sum is an MMA of e4m3 operands with fp32 accumulators; a scale that changes every 128 of K cannot stay outside the whole
+// sum, so each block of K gets an accumulator of its own in tensor memory and the warps that drain it add it, times its scale, to
+// sums in registers.
+#pragma once
+#include "gptq_prefill.cuh"      // tcgen05, cluster and stage helpers
+
+namespace gptq {
+
+constexpr int kFp8Block = 128;                        // columns (and weight rows) per scale
+constexpr float kFp8Max = 448.0f, kFp8ScaleMin = 1.17549435e-38f;      // largest e4m3 number; 2^-126
+__host__ __device__ inline int fp8_blocks(int n) { return (n + kFp8Block - 1) / kFp8Block; }
+
+// ---- rows of numbers to e4m3 -------------------------------------------------------------------------------------------
+// s = max(max|v| / 448, 2^-126), q = e4m3(v / s): both divisions to the nearest, since with 16-bit v the quotient lies exactly in the
+// middle of two e4m3 numbers often (1 of 128 elements where v / max|v| has few digits), and a last bit would decide.
+// `top`: the bits of max|v|, by integer maximum, so that a NaN wins over an infinity and both over numbers.
+__device__ __forceinline__ float fp8_scale(uint32_t top)
+{
+    const float s = __fdiv_rn(__uint_as_float(top), kFp8Max);      // (an infinity or NaN stays one: the whole block becomes NaN)
+    return s < kFp8ScaleMin ? kFp8ScaleMin : s;
+}
+// two numbers to e4m3, nearest even; a in the low byte; NaN becomes NaN, what rounds beyond 448 becomes 448
+__device__ __forceinline__ uint32_t fp8_pair(float a, float b)
+{
+    unsigned short v;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(v) : "f"(b), "f"(a));
+    return v;
+}
+__device__ __forceinline__ uint32_t fp8_four(float a, float b, float c, float d) { return fp8_pair(a, b) | fp8_pair(c, d) << 16; }
+__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+// Half a warp per block of 128: 16 bytes of x and 8 of the result per lane.  kFp8QuantUnroll blocks per half warp are requested
+// together.
+constexpr int kFp8QuantThreads = 256, kFp8QuantUnroll = 4;
+template <bool BF>
+__global__ void __launch_bounds__(kFp8QuantThreads) fp8_quantize_kernel(const uint4 *x, uint2 *q, float *scales, int K, int KB, long long blocks)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    const int lane16 = threadIdx.x & 15;
+    const long long halves = (long long)gridDim.x * (kFp8QuantThreads / 16);
+    const long long first = (long long)blockIdx.x * (kFp8QuantThreads / 16) + threadIdx.x / 16;
+    for (long long b0 = first; b0 < blocks; b0 += halves * kFp8QuantUnroll) {
+        uint4 v[kFp8QuantUnroll];
+        size_t at[kFp8QuantUnroll];
+        bool in[kFp8QuantUnroll];
+#pragma unroll
+        for (int i = 0; i < kFp8QuantUnroll; ++i) {
+            const long long b = b0 + i * halves;
+            const long long row = b / KB;
+            const int k = (int)(b - row * KB) * kFp8Block + lane16 * 8;
+            in[i] = b < blocks && k < K;
+            at[i] = ((size_t)row * K + k) / 8;
+            v[i] = in[i] ? x[at[i]] : make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < kFp8QuantUnroll; ++i) {
+            const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+            float2 f[4];
+            uint32_t top = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                f[j] = pair_to_float2<BF>(w[j]);
+                top = max(top, max(abs_bits(f[j].x), abs_bits(f[j].y)));
+            }
+#pragma unroll
+            for (int o = 8; o; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+            const float s = fp8_scale(top);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f[j] = make_float2(__fdiv_rn(f[j].x, s), __fdiv_rn(f[j].y, s));
+            if (in[i]) q[at[i]] = make_uint2(fp8_four(f[0].x, f[0].y, f[1].x, f[1].y), fp8_four(f[2].x, f[2].y, f[3].x, f[3].y));
+            if (lane16 == 0 && b0 + i * halves < blocks) scales[b0 + i * halves] = s;
+        }
+    }
+}
+
+// ---- a layer the other way round ---------------------------------------------------------------------------------------
+// [N, K] -> [K, N], scales likewise; a tile of 64 x 64 bytes per CTA.  Runs once per layer.
+__global__ void __launch_bounds__(256) fp8_transpose_kernel(const uint8_t *w, const float *scales, uint8_t *w_out, float *scales_out, int N, int K)
+{
+    __shared__ uint8_t tile[64][68];
+    const int tiles_k = (K + 63) / 64;
+    const int n0 = (int)(blockIdx.x / tiles_k) * 64, k0 = (int)(blockIdx.x % tiles_k) * 64;
+    const int r = threadIdx.x / 4, c = threadIdx.x % 4 * 16;
+    if (n0 + r < N && k0 + c < K) {
+        const uint4 v = *reinterpret_cast<const uint4 *>(w + (size_t)(n0 + r) * K + k0 + c);
+        uint32_t *t = reinterpret_cast<uint32_t *>(&tile[r][c]);
+        t[0] = v.x, t[1] = v.y, t[2] = v.z, t[3] = v.w;
+    }
+    __syncthreads();
+    if (k0 + r < K && n0 + c < N) {
+        uint32_t v[4];
+        for (int j = 0; j < 4; ++j)
+            v[j] = tile[c + 4 * j][r] | tile[c + 4 * j + 1][r] << 8 | tile[c + 4 * j + 2][r] << 16 | (uint32_t)tile[c + 4 * j + 3][r] << 24;
+        *reinterpret_cast<uint4 *>(w_out + (size_t)(k0 + r) * N + n0 + c) = make_uint4(v[0], v[1], v[2], v[3]);
+    }
+    if (threadIdx.x == 0 && n0 % kFp8Block == 0 && k0 % kFp8Block == 0)
+        scales_out[(size_t)(k0 / kFp8Block) * fp8_blocks(N) + n0 / kFp8Block] = scales[(size_t)(n0 / kFp8Block) * fp8_blocks(K) + k0 / kFp8Block];
+}
+
+// ---- many rows: tiles of 128 token rows x 256 weight rows ---------------------------------------------------------------
+// One persistent CTA per SM: a TMA warp, an MMA warp, eight warps that drain.  A stage of the ring is one block of K of both operands
+// (48 KB); the MMA's accumulator alternates between two halves of tensor memory, one block of K each, so that a block is drained
+// while the next is multiplied.  Token rows are the MMA's rows (lanes of tensor memory): a thread that drains holds one token
+// row, hence one scale per block of K.  A drain warp has 2 x 64 of the tile's columns; in the gated kinds these are gate and up of the
+// same 64 columns, so that the activation needs no exchange but the maximum over two warps.
+constexpr int kFp8TileM = 128, kFp8TileN = 256, kFp8Stages = 4;
+constexpr int kFp8DrainWarps = 8, kFp8Threads = 32 * (2 + kFp8DrainWarps);
+constexpr int kFp8XBytes = kFp8TileM * kFp8Block, kFp8WBytes = kFp8TileN * kFp8Block, kFp8StageBytes = kFp8XBytes + kFp8WBytes;
+constexpr int kFp8OutBytes = 32 * 128;      // per drain warp: 32 rows of 64 16-bit columns, in and out
+constexpr int kFp8SmemBytes = 2048 + kFp8Stages * kFp8StageBytes + kFp8DrainWarps * kFp8OutBytes;
+static_assert(kFp8SmemBytes <= 227 * 1024, "the ring does not fit");
+
+enum Fp8Kind : int { kFp8Plain = 0, kFp8Gated = 1, kFp8Backward = 2 };
+
+struct Fp8Args {
+    const float *x_scales, *w_scales;      // [M, KB], [blocks of N, KB]
+    const __half *bias;                    // [N] or nullptr
+    float *out_scales;                     // gated kinds: the result is e4m3 with these scales; nullptr: 16 bits
+    int M, N, K, KB;                       // gated kinds: N = 2 F
+    int tiles_m, tiles_n;
+    int has_in;                            // a residual, or the gradient of the result
+};
+
+__device__ __forceinline__ void umma_f8_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t src, int c0, int c1)
+{
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(c0), "r"(c1), "r"(src)
+                 : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+__device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void tma_store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+// two fp32 multiply-adds in one instruction
+__device__ __forceinline__ void fma2(uint64_t &acc, uint32_t lo, uint32_t hi, uint64_t s)
+{
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(lo), "r"(hi));
+    asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(v), "l"(s));
+}
+__device__ __forceinline__ uint64_t both(float s)
+{
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %1};" : "=l"(v) : "r"(__float_as_uint(s)));
+    return v;
+}
+__device__ __forceinline__ float2 unpack2(uint64_t v)
+{
+    uint32_t lo, hi;
+    asm("mov.b64 {%0, %1}, %2;" : "=r"(lo), "=r"(hi) : "l"(v));
+    return make_float2(__uint_as_float(lo), __uint_as_float(hi));
+}
+__device__ __forceinline__ uint64_t pack2(float2 f)
+{
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(__float_as_uint(f.x)), "r"(__float_as_uint(f.y)));
+    return v;
+}
+// silu(g) * u; p is the logistic function (0 where it is below 2^-126)
+__device__ __forceinline__ float logistic(float g) { return __frcp_rn(1.0f + __expf(-g)); }
+
+// tile number -> (row of tiles, column of tiles): columns outermost within groups of 8 rows of tiles, so that what runs at the same time shares
+// both operands in L2
+__device__ __forceinline__ void fp8_tile(int t, int tiles_m, int tiles_n, int &tm, int &tn)
+{
+    constexpr int kRows = 8;
+    const int group = t / (kRows * tiles_n), first = group * kRows;
+    const int rows = min(kRows, tiles_m - first);
+    const int in = t - group * kRows * tiles_n;
+    tm = first + in % rows;
+    tn = in / rows;
+}
+
+template <int KIND, bool BF, bool OUT8>
+__global__ void __launch_bounds__(kFp8Threads, 1)
+fp8_tiles_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map,
+                 const __grid_constant__ CUtensorMap in_map, const __grid_constant__ CUtensorMap out_map)
+{
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    // full / empty: stages; dfull / dempty: accumulators; in: a drain warp's input tile
+    const uint32_t bar_full = base, bar_empty = base + 64, bar_dfull = base + 128, bar_dempty = base + 144, bar_in = base + 192, tmem_slot = base + 256;
+    const uint32_t ring = base + 1024, out_stage = ring + kFp8Stages * kFp8StageBytes;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    const int tiles = a.tiles_m * a.tiles_n, KB = a.KB, F = a.N / 2;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kFp8Stages; ++s) {
+            mbar_init(bar_full + 8 * s, 1);
+            mbar_init(bar_empty + 8 * s, 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(bar_dfull + 8 * s, 1);
+            mbar_init(bar_dempty + 8 * s, kFp8DrainWarps);
+        }
+        for (int s = 0; s < kFp8DrainWarps; ++s) mbar_init(bar_in + 8 * s, 1);
+        fence_barrier_init();
+        fence_proxy_async();
+    }
+    if (warp == 1) {
+        tmem_alloc(tmem_slot, 512);
+        tmem_relinquish();
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = lds32(tmem_slot);
+    pdl_launch_dependents();
+
+    if (warp == 0) {
+        // ------------------------------------------------------------------------------------------ TMA (one thread)
+        if (elect_one()) {
+            tma_prefetch_descriptor(&x_map);
+            tma_prefetch_descriptor(&w_map);
+            auto issue_w = [&](int s, int tn, int kb) {
+                const uint32_t st = ring + s * kFp8StageBytes + kFp8XBytes;
+                const int n0 = KIND == kFp8Plain ? tn * kFp8TileN : tn * kFp8Block;
+                tma_load_2d(st, &w_map, kb * kFp8Block, n0, bar_full + 8 * s);
+                tma_load_2d(st + kFp8WBytes / 2, &w_map, kb * kFp8Block, KIND == kFp8Plain ? n0 + kFp8Block : F + n0, bar_full + 8 * s);
+            };
+            // weights do not depend on earlier kernels: the first ones are requested before these have ended
+            int tm, tn, early = 0;
+            fp8_tile(blockIdx.x, a.tiles_m, a.tiles_n, tm, tn);
+            for (; early < kFp8Stages && early < KB; ++early) {
+                mbar_expect_tx(bar_full + 8 * early, kFp8WBytes);
+                issue_w(early, tn, early);
+            }
+            pdl_wait();
+            int i = 0;      // blocks requested
+            bool ok = true;
+            for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
+                fp8_tile(t, a.tiles_m, a.tiles_n, tm, tn);
+                for (int kb = 0; kb < KB; ++kb, ++i) {
+                    const int s = i % kFp8Stages;
+                    if (i >= kFp8Stages && !(ok = mbar_wait(bar_empty + 8 * s, (uint32_t)(i / kFp8Stages - 1) & 1))) break;
+                    if (i < early) {
+                        mbar_arrive_expect_tx(bar_full + 8 * s, kFp8XBytes);
+                    } else {
+                        mbar_arrive_expect_tx(bar_full + 8 * s, kFp8XBytes + kFp8WBytes);
+                        issue_w(s, tn, kb);
+                    }
+                    tma_load_2d(ring + s * kFp8StageBytes, &x_map, kb * kFp8Block, tm * kFp8TileM, bar_full + 8 * s);
+                }
+            }
+            // nothing may be on its way into this shared memory when the CTA ends
+            for (int j = i < kFp8Stages ? 0 : i - kFp8Stages; j < i; ++j) mbar_wait(bar_full + 8 * (j % kFp8Stages), (uint32_t)(j / kFp8Stages) & 1);
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------------------------------ MMA (one thread)
+        if (elect_one()) {
+            constexpr uint32_t idesc = umma_idesc_f16(kFp8TileM, kFp8TileN);      // (both operands e4m3: format fields 0)
+            int i = 0;
+            bool ok = true;
+            for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x)
+                for (int kb = 0; kb < KB; ++kb, ++i) {
+                    const int s = i % kFp8Stages, d = i & 1;
+                    if (!(ok = mbar_wait(bar_full + 8 * s, (uint32_t)(i / kFp8Stages) & 1))) break;
+                    if (i >= 2 && !(ok = mbar_wait(bar_dempty + 8 * d, (uint32_t)(i / 2 - 1) & 1))) break;
+                    tc_fence_after_sync();
+                    const uint64_t xd = umma_desc_k_major_sw128(ring + s * kFp8StageBytes);
+                    const uint64_t wd = umma_desc_k_major_sw128(ring + s * kFp8StageBytes + kFp8XBytes);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) umma_f8_ss(tmem + d * kFp8TileN, xd + 2 * j, wd + 2 * j, idesc, j);
+                    umma_commit(bar_empty + 8 * s);
+                    umma_commit(bar_dfull + 8 * d);
+                }
+        }
+    } else {
+        // ------------------------------------------------------------------------------------------ drain
+        pdl_wait();
+        const int q = warp & 3, half = (warp - 2) >> 2;                  // lanes 32 q .. of tensor memory; which columns
+        const uint32_t stage = out_stage + (warp - 2) * kFp8OutBytes, my_in = bar_in + 8 * (warp - 2);
+        const int col0 = KIND == kFp8Plain ? 128 * half : 64 * half, col1 = KIND == kFp8Plain ? col0 + 64 : 128 + col0;
+        const int nb_last = fp8_blocks(a.N) - 1;
+        int i = 0, ins = 0;
+        bool ok = true;      // false once a wait has given up: from then on nothing is waited for or stored, but every barrier met
+        for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
+            int tm, tn;
+            fp8_tile(t, a.tiles_m, a.tiles_n, tm, tn);
+            const int row0 = tm * kFp8TileM + 32 * q, row = row0 + lane;
+            const bool live = row0 < a.M;
+            // first columns of this warp's two groups of 64, in y or (gated kinds) in the F columns of the result
+            const int out0 = KIND == kFp8Plain ? tn * kFp8TileN + col0 : tn * kFp8Block + col0;
+            if (KIND != kFp8Plain || a.has_in) {      // the input of the first group (gated: the only one)
+                if (live && out0 < (KIND == kFp8Plain ? a.N : F) && elect_one()) {
+                    tma_store_wait_read();
+                    if (KIND == kFp8Backward || KIND == kFp8Plain) {
+                        mbar_arrive_expect_tx(my_in, kFp8OutBytes);
+                        tma_load_2d(stage, &in_map, out0, row0, my_in);
+                    }
+                }
+            }
+            const int nb0 = KIND == kFp8Plain ? min(tn * 2 + half, nb_last) : tn, nb1 = KIND == kFp8Plain ? nb0 : F / kFp8Block + tn;
+            const float *ws0 = a.w_scales + (size_t)nb0 * KB, *ws1 = a.w_scales + (size_t)nb1 * KB;
+            const float *xs = a.x_scales + (size_t)min(row, a.M - 1) * KB;
+            uint64_t acc[2][32];
+#pragma unroll
+            for (int j = 0; j < 64; ++j) acc[j / 32][j % 32] = 0;
+            float x_next = __ldg(xs), w0_next = __ldg(ws0), w1_next = __ldg(ws1);
+            for (int kb = 0; kb < KB; ++kb, ++i) {
+                const uint64_t s0 = both(x_next * w0_next), s1 = KIND == kFp8Plain ? s0 : both(x_next * w1_next);
+                const int nx = min(kb + 1, KB - 1);
+                x_next = __ldg(xs + nx), w0_next = __ldg(ws0 + nx);
+                if (KIND != kFp8Plain) w1_next = __ldg(ws1 + nx);
+                const int d = i & 1;
+                if (ok) ok = mbar_wait_warp(bar_dfull + 8 * d, (uint32_t)(i / 2) & 1);
+                tc_fence_after_sync();
+                if (live) {
+                    const uint32_t from = tmem + d * kFp8TileN + ((uint32_t)(32 * q) << 16);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t v[32];
+                        tmem_ld_32x32(from + (c < 2 ? col0 : col1) + 32 * (c & 1), v);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) fma2(acc[c / 2][16 * (c & 1) + j], v[2 * j], v[2 * j + 1], c < 2 ? s0 : s1);
+                    }
+                }
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar_dempty + 8 * d);
+            }
+            if (!live) continue;
+
+            // row `lane` of the stage, 16-byte piece c: 128-byte rows, 128-byte swizzle (the tensor maps')
+            auto piece = [&](int c) { return stage + lane * 128 + ((c ^ (lane & 7)) << 4); };
+            auto send16 = [&](int col) {
+                fence_proxy_async();
+                __syncwarp();
+                if (ok && elect_one()) tma_store_2d(&out_map, stage, col, row0);
+            };
+            auto stage_free = [&]() {
+                if (elect_one()) tma_store_wait_read();      // (the lane that issued: one and the same)
+                __syncwarp();
+            };
+            if constexpr (KIND == kFp8Plain) {
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    const int col = out0 + 64 * g;
+                    if (col >= a.N) break;
+                    if (a.has_in) {
+                        if (g == 1) {
+                            stage_free();
+                            if (elect_one()) {
+                                mbar_arrive_expect_tx(my_in, kFp8OutBytes);
+                                tma_load_2d(stage, &in_map, col, row0, my_in);
+                            }
+                        }
+                        if (ok) ok = mbar_wait_warp(my_in, (uint32_t)ins & 1);
+                        ++ins;
+                    } else {
+                        stage_free();
+                    }
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        float2 f[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) f[j] = unpack2(acc[g][4 * c + j]);
+                        if (a.bias != nullptr && col + 8 * c < a.N) {      // (N % 8 == 0)
+                            const uint4 b = __ldg(reinterpret_cast<const uint4 *>(a.bias + col + 8 * c));
+                            const uint32_t bw[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const float2 e = pair_to_float2<BF>(bw[j]);
+                                f[j].x += e.x, f[j].y += e.y;
+                            }
+                        }
+                        if (a.has_in) {
+                            const uint4 b = lds128(piece(c));
+                            const uint32_t bw[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const float2 e = pair_to_float2<BF>(bw[j]);
+                                f[j].x += e.x, f[j].y += e.y;
+                            }
+                        }
+                        sts128(piece(c), make_uint4(pack_out16<BF>(f[0]), pack_out16<BF>(f[1]), pack_out16<BF>(f[2]), pack_out16<BF>(f[3])));
+                    }
+                    send16(col);
+                }
+            } else {
+                // h = silu(gate) up in the place of gate's sums; backward: the gradients in the places of both
+                uint32_t top0 = 0, top1 = 0;
+                if constexpr (KIND == kFp8Backward) {
+                    if (ok) ok = mbar_wait_warp(my_in, (uint32_t)ins & 1);
+                    ++ins;
+                }
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    uint32_t dw[4];
+                    if constexpr (KIND == kFp8Backward) {
+                        const uint4 b = lds128(piece(c));
+                        dw[0] = b.x, dw[1] = b.y, dw[2] = b.z, dw[3] = b.w;
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float2 g = unpack2(acc[0][4 * c + j]), u = unpack2(acc[1][4 * c + j]);
+                        const float2 p = make_float2(logistic(g.x), logistic(g.y));
+                        float2 r;
+                        if constexpr (KIND == kFp8Gated) {
+                            r = make_float2(g.x * p.x * u.x, g.y * p.y * u.y);
+                        } else {
+                            const float2 e = pair_to_float2<BF>(dw[j]);
+                            r = make_float2(e.x * u.x * p.x * (1.0f + g.x * (1.0f - p.x)), e.y * u.y * p.y * (1.0f + g.y * (1.0f - p.y)));
+                            const float2 v = make_float2(e.x * g.x * p.x, e.y * g.y * p.y);
+                            acc[1][4 * c + j] = pack2(v);
+                            top1 = max(top1, max(abs_bits(v.x), abs_bits(v.y)));
+                        }
+                        acc[0][4 * c + j] = pack2(r);
+                        top0 = max(top0, max(abs_bits(r.x), abs_bits(r.y)));
+                    }
+                }
+                constexpr int kOuts = KIND == kFp8Backward ? 2 : 1;
+                if constexpr (OUT8) {
+                    // the two warps that hold a row's 128 columns exchange their maxima (in the stages, which are free)
+                    stage_free();
+                    asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(stage + 8 * lane), "r"(top0), "r"(top1) : "memory");
+                    named_bar_sync(1 + q, 64);
+                    const uint2 other = lds64(out_stage + ((warp - 2) ^ 4) * kFp8OutBytes + 8 * lane);
+                    named_bar_sync(1 + q, 64);
+                    const float s0 = fp8_scale(max(top0, other.x)), s1 = fp8_scale(max(top1, other.y));
+                    const int FB = F / kFp8Block;
+                    if (half == 0 && row < a.M && ok) {
+                        a.out_scales[(size_t)row * kOuts * FB + tn] = s0;
+                        if (kOuts == 2) a.out_scales[(size_t)row * 2 * FB + FB + tn] = s1;
+                    }
+                    // 64-byte rows, 64-byte swizzle
+#pragma unroll
+                    for (int o = 0; o < kOuts; ++o) {
+                        const float s = o ? s1 : s0;
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const float2 f0 = unpack2(acc[o][8 * c + 2 * j]), f1 = unpack2(acc[o][8 * c + 2 * j + 1]);
+                                w[j] = fp8_four(__fdiv_rn(f0.x, s), __fdiv_rn(f0.y, s), __fdiv_rn(f1.x, s), __fdiv_rn(f1.y, s));
+                            }
+                            sts128(stage + o * 2048 + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
+                        }
+                    }
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (ok && elect_one())
+                        for (int o = 0; o < kOuts; ++o) tma_store_2d(&out_map, stage + o * 2048, o * F + out0, row0);
+                } else {
+#pragma unroll
+                    for (int o = 0; o < kOuts; ++o) {
+                        stage_free();
+#pragma unroll
+                        for (int c = 0; c < 8; ++c)
+                            sts128(piece(c), make_uint4(pack_out16<BF>(unpack2(acc[o][4 * c])), pack_out16<BF>(unpack2(acc[o][4 * c + 1])),
+                                                        pack_out16<BF>(unpack2(acc[o][4 * c + 2])), pack_out16<BF>(unpack2(acc[o][4 * c + 3]))));
+                        send16(o * F + out0);
+                    }
+                }
+            }
+        }
+        if (elect_one()) tma_store_wait();
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    if (warp == 1) tmem_dealloc(tmem, 512);
+}
+
+// ---- launches -----------------------------------------------------------------------------------------------------------
+
+inline cudaError_t fp8_launch(void *kernel, int grid, int threads, int smem, int cluster, cudaStream_t s, void **args)
+{
+    cudaLaunchAttribute attr[3] = {};
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = s;
+    cfg.attrs = attr;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.numAttrs = 1;
+    if (cluster > 1) {
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = (unsigned)cluster;
+        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        attr[2].id = cudaLaunchAttributeClusterSchedulingPolicyPreference;
+        attr[2].val.clusterSchedulingPolicyPreference = cudaClusterSchedulingPolicyLoadBalancing;
+        cfg.numAttrs = 3;
+    }
+    return cudaLaunchKernelExC(&cfg, kernel, args);
+}
+
+inline int launch_fp8_quantize(const void *x, void *q, float *scales, int M, int K, int bf16, int sms, cudaStream_t s)
+{
+    int KB = fp8_blocks(K);
+    long long blocks = (long long)M * KB;
+    const long long per_cta = kFp8QuantThreads / 16, want = (blocks + per_cta - 1) / per_cta;
+    const int grid = (int)(want < 8ll * sms ? want : 8ll * sms);
+    const uint4 *xp = (const uint4 *)x;
+    uint2 *qp = (uint2 *)q;
+    void *args[] = {&xp, &qp, &scales, &K, &KB, &blocks};
+    return record_cuda_error(fp8_launch(bf16 ? (void *)fp8_quantize_kernel<true> : (void *)fp8_quantize_kernel<false>, grid, kFp8QuantThreads, 0, 1, s, args));
+}
+
+inline int launch_fp8_transpose(const void *w, const float *scales, void *w_out, float *scales_out, int N, int K, cudaStream_t s)
+{
+    const long long tiles = (long long)((N + 63) / 64) * ((K + 63) / 64);
+    if (tiles > 0x7fffffffll) return GPTQ_ERR_UNSUPPORTED;
+    fp8_transpose_kernel<<<(unsigned)tiles, 256, 0, s>>>((const uint8_t *)w, scales, (uint8_t *)w_out, scales_out, N, K);
+    return record_cuda_error(cudaGetLastError());
+}
+
+struct Fp8Call {
+    int kind;                    // Fp8Kind
+    const void *x;               // e4m3 [M, K]
+    const float *x_scales;
+    const void *w;               // e4m3 [N, K]
+    const float *w_scales;
+    const void *bias, *in;       // in: residual [M, N], or the gradient of the result [M, N / 2]
+    void *out;
+    float *out_scales;
+    int M, N, K, bf16, sms;
+};
+
+template <int KIND, bool BF, bool OUT8>
+int launch_fp8_tiles(const Fp8Call &c, cudaStream_t s)
+{
+    static int configured[64];
+    auto kernel = fp8_tiles_kernel<KIND, BF, OUT8>;
+    int st = ensure_dynamic_smem((const void *)kernel, configured, kFp8SmemBytes);
+    if (st) return st;
+    const int F = c.N / 2;
+    Fp8Args a{};
+    a.x_scales = c.x_scales, a.w_scales = c.w_scales, a.bias = (const __half *)c.bias, a.out_scales = c.out_scales;
+    a.M = c.M, a.N = c.N, a.K = c.K, a.KB = fp8_blocks(c.K);
+    a.tiles_m = (c.M - 1) / kFp8TileM + 1;
+    a.tiles_n = KIND == kFp8Plain ? (c.N - 1) / kFp8TileN + 1 : F / kFp8Block;
+    a.has_in = c.in != nullptr;
+    const long long tiles = (long long)a.tiles_m * a.tiles_n;
+    if (tiles > 0x3fffffffll) return GPTQ_ERR_UNSUPPORTED;
+    CUtensorMap xm, wm, im, om;
+    const auto u8 = CU_TENSOR_MAP_DATA_TYPE_UINT8;
+    const auto b16 = CU_TENSOR_MAP_DATA_TYPE_UINT16;
+    const auto sw128 = CU_TENSOR_MAP_SWIZZLE_128B;
+    st = make_tensor_map_2d(&xm, u8, c.x, c.K, c.M, c.K, kFp8Block, kFp8TileM, sw128);
+    if (!st) st = make_tensor_map_2d(&wm, u8, c.w, c.K, c.N, c.K, kFp8Block, kFp8Block, sw128);
+    const uint64_t in_cols = KIND == kFp8Plain ? c.N : F, out_cols = KIND == kFp8Gated ? F : c.N;
+    if (!st) {
+        if (OUT8) st = make_tensor_map_2d(&om, u8, c.out, out_cols, c.M, out_cols, 64, 32, CU_TENSOR_MAP_SWIZZLE_64B);
+        else st = make_tensor_map_2d(&om, b16, c.out, out_cols, c.M, out_cols * 2, 64, 32, sw128);
+    }
+    if (!st) {
+        if (c.in) st = make_tensor_map_2d(&im, b16, c.in, in_cols, c.M, in_cols * 2, 64, 32, sw128);
+        else im = om;
+    }
+    if (st) return st;
+    void *args[] = {&a, &xm, &wm, &im, &om};
+    return record_cuda_error(fp8_launch((void *)kernel, (int)(tiles < c.sms ? tiles : c.sms), kFp8Threads, kFp8SmemBytes, 1, s, args));
+}
+
+inline int launch_fp8(const Fp8Call &c, cudaStream_t s)
+{
+    const bool out8 = c.out_scales != nullptr;
+    switch (c.kind * 4 + (out8 ? 2 : 0) + (c.bf16 ? 1 : 0)) {
+    case 0: return launch_fp8_tiles<kFp8Plain, false, false>(c, s);
+    case 1: return launch_fp8_tiles<kFp8Plain, true, false>(c, s);
+    case 4: return launch_fp8_tiles<kFp8Gated, false, false>(c, s);
+    case 5: return launch_fp8_tiles<kFp8Gated, true, false>(c, s);
+    case 6: case 7: return launch_fp8_tiles<kFp8Gated, false, true>(c, s);      // (the type of the result is not the type of anything else)
+    case 8: return launch_fp8_tiles<kFp8Backward, false, false>(c, s);
+    case 9: return launch_fp8_tiles<kFp8Backward, true, false>(c, s);
+    case 10: return launch_fp8_tiles<kFp8Backward, false, true>(c, s);
+    case 11: return launch_fp8_tiles<kFp8Backward, true, true>(c, s);
+    default: return GPTQ_ERR_UNSUPPORTED;
+    }
+}
+
+}  // namespace gptq

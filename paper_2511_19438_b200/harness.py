@@ -310,3 +310,123 @@ def gemm_lora(x: torch.Tensor, D: DeviceLinear, lora_a: torch.Tensor, lora_b: to
 
 def ensure_for_lora(ws: "WorkspaceHolder", M: int, D: DeviceLinear, rank: int) -> None:
     ws.ensure(B.gptq_lora_workspace_bytes(M, D.N, D.K, D.group_size, D.act_order, rank))
+
+
+# ---- layers in 8-bit floating point -------------------------------------------------------------------------------------
+
+@dataclass
+class DeviceFp8Linear:
+    """An e4m3 layer as checkpoints hold it, and its transpose where gradients are wanted."""
+    K: int
+    N: int
+    weight: torch.Tensor         # float8_e4m3fn [N, K]
+    scales: torch.Tensor         # float32 [ceil(N / 128), ceil(K / 128)]
+    transposed: "DeviceFp8Linear | None" = None
+
+
+def _blocks(n: int) -> int:
+    return -(-n // 128)
+
+
+def fp8_linear(weight: torch.Tensor, scales: torch.Tensor, transpose: bool = False) -> DeviceFp8Linear:
+    """A layer whose tensors are on the GPU; ``transpose``: laid out the other way round too (gptq_fp8_transpose)."""
+    N, K = weight.shape
+    _expect("weight", weight, torch.float8_e4m3fn, (N, K))
+    _expect("scales", scales, torch.float32, (_blocks(N), _blocks(K)))
+    D = DeviceFp8Linear(K, N, weight, scales)
+    if transpose:
+        T = DeviceFp8Linear(N, K, torch.empty((K, N), dtype=weight.dtype, device=weight.device),
+                            torch.empty((_blocks(K), _blocks(N)), dtype=scales.dtype, device=scales.device))
+        B.check(B.gptq_fp8_transpose(weight, scales, T.weight, T.scales, N, K), "gptq_fp8_transpose")
+        D.transposed = T
+    return D
+
+
+def ensure_for_fp8(ws: "WorkspaceHolder", M: int, K: int) -> None:
+    """Scratch for calls that bring [M, K] in 16 bits."""
+    ws.ensure(B.gptq_fp8_workspace_bytes(M, K))
+
+
+def _format_of(dtype: torch.dtype) -> int:
+    if dtype not in (torch.float16, torch.bfloat16):
+        raise ValueError(f"float16 or bfloat16 expected, got {dtype}")
+    return B.GPTQ_FORMAT_BF16 if dtype == torch.bfloat16 else 0
+
+
+def _expect_rows(x: torch.Tensor, x_scales: torch.Tensor | None, dtype: torch.dtype, K: int) -> int:
+    M = x.shape[0]
+    _expect("x", x, dtype if x_scales is None else torch.float8_e4m3fn, (M, K))
+    _expect("x_scales", x_scales, torch.float32, (M, _blocks(K)))
+    return M
+
+
+def _rows_fp8(M: int, N: int, device) -> tuple[torch.Tensor, torch.Tensor]:
+    return (torch.empty((M, N), dtype=torch.float8_e4m3fn, device=device), torch.empty((M, _blocks(N)), dtype=torch.float32, device=device))
+
+
+def fp8_quantize(x: torch.Tensor, stream=None) -> tuple[torch.Tensor, torch.Tensor]:
+    """(e4m3 [M, K], fp32 scales [M, ceil(K / 128)]) of 16-bit rows through gptq_fp8_quantize."""
+    M, K = x.shape
+    _expect("x", x, x.dtype, (M, K))
+    q, s = _rows_fp8(M, K, x.device)
+    B.check(B.gptq_fp8_quantize(x, q, s, M, K, _format_of(x.dtype), stream), "gptq_fp8_quantize")
+    return q, s
+
+
+def gemm_fp8(x: torch.Tensor, D: DeviceFp8Linear, bias: torch.Tensor | None = None, residual: torch.Tensor | None = None,
+             y: torch.Tensor | None = None, x_scales: torch.Tensor | None = None, dtype: torch.dtype | None = None,
+             stream=None) -> torch.Tensor:
+    """y = x w^T + bias + residual through gptq_gemm_fp8: x 16-bit (workspace: ensure_for_fp8), or e4m3 with ``x_scales`` and the
+    ``dtype`` of the result."""
+    dtype = x.dtype if x_scales is None else dtype or torch.float16
+    fmt = _format_of(dtype)
+    M = _expect_rows(x, x_scales, dtype, D.K)
+    if y is None:
+        y = torch.empty((M, D.N), dtype=dtype, device=x.device)
+    _expect("bias", bias, dtype, (D.N,))
+    _expect("residual", residual, dtype, (M, D.N))
+    _expect("y", y, dtype, (M, D.N))
+    B.check(B.gptq_gemm_fp8(x, x_scales, D.weight, D.scales, bias, residual, y, M, D.N, D.K, fmt, stream), "gptq_gemm_fp8")
+    return y
+
+
+def gemm_fp8_silu_mul(x: torch.Tensor, D: DeviceFp8Linear, x_scales: torch.Tensor | None = None, quantized: bool = False,
+                      dtype: torch.dtype | None = None, stream=None):
+    """silu(gate) * up [M, N / 2] through gptq_gemm_fp8_silu_mul, D's rows = gate's, then up's: 16-bit, or (``quantized``) e4m3 and
+    its scales."""
+    dtype = x.dtype if x_scales is None else dtype or torch.float16
+    fmt = _format_of(dtype)
+    M, F = _expect_rows(x, x_scales, dtype, D.K), D.N // 2
+    out, s = _rows_fp8(M, F, x.device) if quantized else (torch.empty((M, F), dtype=dtype, device=x.device), None)
+    B.check(B.gptq_gemm_fp8_silu_mul(x, x_scales, D.weight, D.scales, out, s, M, F, D.K, fmt, stream), "gptq_gemm_fp8_silu_mul")
+    return (out, s) if quantized else out
+
+
+def gemm_fp8_silu_mul_backward(x: torch.Tensor, D: DeviceFp8Linear, d_out: torch.Tensor, x_scales: torch.Tensor | None = None,
+                               quantized: bool = True, stream=None):
+    """The gradients [M, N] of gate's and up's columns through gptq_gemm_fp8_silu_mul_backward: e4m3 and scales, or 16-bit."""
+    fmt = _format_of(d_out.dtype)
+    M, F = _expect_rows(x, x_scales, d_out.dtype, D.K), D.N // 2
+    _expect("d_out", d_out, d_out.dtype, (M, F))
+    out, s = _rows_fp8(M, D.N, x.device) if quantized else (torch.empty((M, D.N), dtype=d_out.dtype, device=x.device), None)
+    B.check(B.gptq_gemm_fp8_silu_mul_backward(x, x_scales, D.weight, D.scales, d_out, out, s, M, F, D.K, fmt, stream),
+            "gptq_gemm_fp8_silu_mul_backward")
+    return (out, s) if quantized else out
+
+
+def mlp_fp8(x: torch.Tensor, gate_up: DeviceFp8Linear, down: DeviceFp8Linear, residual: torch.Tensor | None = None,
+            y: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """A gated feed-forward block, y = down(silu(gate) * up) + residual, the activation in 8 bits between the layers
+    (workspace: ensure_for_fp8 of x)."""
+    h, s = gemm_fp8_silu_mul(x, gate_up, quantized=True, stream=stream)
+    return gemm_fp8(h, down, residual=residual, y=y, x_scales=s, dtype=x.dtype, stream=stream)
+
+
+def mlp_fp8_backward(x: torch.Tensor, gate_up: DeviceFp8Linear, down: DeviceFp8Linear, d_y: torch.Tensor, stream=None) -> torch.Tensor:
+    """The gradient of mlp_fp8's x without the residual's share (layers with their transposes; workspace: ensure_for_fp8 of d_y
+    and of x)."""
+    if gate_up.transposed is None or down.transposed is None:
+        raise ValueError("gate_up and down are needed the other way round too: fp8_linear(..., transpose=True)")
+    d_h = gemm_fp8(d_y, down.transposed, stream=stream)
+    d_gate_up, s = gemm_fp8_silu_mul_backward(x, gate_up, d_h, stream=stream)
+    return gemm_fp8(d_gate_up, gate_up.transposed, x_scales=s, dtype=x.dtype, stream=stream)
