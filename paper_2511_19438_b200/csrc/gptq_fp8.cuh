@@ -7,6 +7,7 @@
 // sums in registers.
 #pragma once
 #include "gptq_prefill.cuh"      // tcgen05, cluster and stage helpers
+#include "gptq_umma2.cuh"        // CTA pairs
 
 namespace gptq {
 
@@ -102,18 +103,25 @@ __global__ void __launch_bounds__(256) fp8_transpose_kernel(const uint8_t *w, co
         scales_out[(size_t)(k0 / kFp8Block) * fp8_blocks(N) + n0 / kFp8Block] = scales[(size_t)(n0 / kFp8Block) * fp8_blocks(K) + k0 / kFp8Block];
 }
 
-// ---- many rows: tiles of 128 token rows x 256 weight rows ---------------------------------------------------------------
-// One persistent CTA per SM: a TMA warp, an MMA warp, eight warps that drain.  A stage of the ring is one block of K of both operands
-// (48 KB); the MMA's accumulator alternates between two halves of tensor memory, one block of K each, so that a block is drained
-// while the next is multiplied.  Token rows are the MMA's rows (lanes of tensor memory): a thread that drains holds one token
-// row, hence one scale per block of K.  A drain warp has 2 x 64 of the tile's columns; in the gated kinds these are gate and up of the
-// same 64 columns, so that the activation needs no exchange but the maximum over two warps.
-constexpr int kFp8TileM = 128, kFp8TileN = 256, kFp8Stages = 4;
-constexpr int kFp8DrainWarps = 8, kFp8Threads = 32 * (2 + kFp8DrainWarps);
-constexpr int kFp8XBytes = kFp8TileM * kFp8Block, kFp8WBytes = kFp8TileN * kFp8Block, kFp8StageBytes = kFp8XBytes + kFp8WBytes;
-constexpr int kFp8OutBytes = 32 * 128;      // per drain warp: 32 rows of 64 16-bit columns, in and out
-constexpr int kFp8SmemBytes = 2048 + kFp8Stages * kFp8StageBytes + kFp8DrainWarps * kFp8OutBytes;
-static_assert(kFp8SmemBytes <= 227 * 1024, "the ring does not fit");
+// ---- many rows: CTA pairs, tiles of 256 token rows x 256 weight rows ------------------------------------------------------
+// A persistent pair of CTAs (two SMs) multiplies a tile with tcgen05.mma.cta_group::2: each CTA loads 128 token rows (its lanes of the
+// accumulator) and 128 of the 256 weight rows, a block of K (32 KB) per stage.  The accumulator alternates between two halves of tensor
+// memory, one block of K each, so that a block is drained while the next is multiplied.  Token rows are the MMA's rows: a thread that
+// drains holds one token row, hence one scale per block of K and weight block.  A drain warp has 2 x 64 of the tile's columns; in the gated
+// kinds these are gate and up of the same 64 columns, so that the activation needs no exchange but the maximum over two warps.
+//   warp 0  TMA of this CTA's halves; both CTAs' copies complete on the leader's barrier
+//   warp 1  the MMAs (the leader's)
+//   warps 2, 3  products of scales, two blocks ahead: 128 rows x 2 weight blocks per block of K into a ring of four
+//   warps 4 to 11 drain.  The first four give registers to them: 128 sums and 32 columns on their way.
+constexpr int kFp8TileM = 256, kFp8TileN = 256, kFp8HalfM = 128, kFp8Stages = 4;
+constexpr int kFp8FirstDrain = 4, kFp8DrainWarps = 8, kFp8Threads = 32 * (kFp8FirstDrain + kFp8DrainWarps);
+constexpr int kFp8LaunchRegs = 168, kFp8FewRegs = 72, kFp8ManyRegs = 216;
+static_assert(kFp8FewRegs + 2 * kFp8ManyRegs <= 3 * kFp8LaunchRegs, "three warpgroups share what the CTA was launched with");
+constexpr int kFp8HalfBytes = kFp8HalfM * kFp8Block, kFp8StageBytes = 2 * kFp8HalfBytes;
+constexpr int kFp8OutBytes = 32 * 128;      // 32 rows of 64 16-bit columns, in and out: two per drain warp
+constexpr int kFp8ScaleSlots = 4, kFp8ScaleBytes = 2 * kFp8HalfM * 4;
+constexpr int kFp8SmemBytes = 2048 + kFp8Stages * kFp8StageBytes + 2 * kFp8DrainWarps * kFp8OutBytes + kFp8ScaleSlots * kFp8ScaleBytes;
+static_assert(kFp8SmemBytes <= 227 * 1024 && 2 * kFp8SmemBytes > 227 * 1024, "one CTA per SM: it takes all tensor memory");
 
 enum Fp8Kind : int { kFp8Plain = 0, kFp8Gated = 1, kFp8Backward = 2 };
 
@@ -126,13 +134,21 @@ struct Fp8Args {
     int has_in;                            // a residual, or the gradient of the result
 };
 
-__device__ __forceinline__ void umma_f8_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+__device__ __forceinline__ void umma_f8_ss_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
 {
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
         "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
         ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// tiled load into this CTA's shared memory that completes on a barrier of either CTA of the pair
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap *map, int c0, int c1, uint32_t cluster_bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+        ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(cluster_bar)
         : "memory");
 }
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t src, int c0, int c1)
@@ -143,12 +159,35 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t sr
 }
 __device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 __device__ __forceinline__ void tma_store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
-// two fp32 multiply-adds in one instruction
+// A converged warp's wait in few instructions and without a call: what is live in the drain warps fills the registers, and a call
+// would have it stored.
+__device__ __forceinline__ bool mbar_wait_warp_inline(uint32_t bar, uint32_t parity)
+{
+    uint64_t start = 0;
+    for (;;) {
+        uint32_t done;
+        asm volatile(
+            "{\n\t.reg .pred p, more;\n\t.reg .u32 n;\n\tmov.u32 n, 0;\n"
+            "TRY:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t@p bra.uni END;\n\t"
+            "add.u32 n, n, 1;\n\tsetp.lt.u32 more, n, 4096;\n\t@more bra.uni TRY;\n"
+            "END:\n\tselp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(done)
+            : "r"(bar), "r"(parity)
+            : "memory");
+        if (__any_sync(0xffffffffu, done)) return true;
+        const uint64_t now = global_timer_ns();
+        if (start == 0) start = now;
+        if (__any_sync(0xffffffffu, now - start > kWaitLimitNs)) break;
+    }
+    atomicMax(&g_device_status, (int)kStatusWaitTimeout);
+    return false;
+}
+template <int REGS> __device__ __forceinline__ void setmaxnreg_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS)); }
+template <int REGS> __device__ __forceinline__ void setmaxnreg_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS)); }
+// Two fp32 multiply-adds in one instruction.  (volatile: lo and hi come from tensor memory and are not there before the wait in front.)
 __device__ __forceinline__ void fma2(uint64_t &acc, uint32_t lo, uint32_t hi, uint64_t s)
 {
-    uint64_t v;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(lo), "r"(hi));
-    asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(v), "l"(s));
+    asm volatile("{\n\t.reg .b64 v;\n\tmov.b64 v, {%1, %2};\n\tfma.rn.f32x2 %0, v, %3, %0;\n\t}" : "+l"(acc) : "r"(lo), "r"(hi), "l"(s));
 }
 __device__ __forceinline__ uint64_t both(float s)
 {
@@ -190,10 +229,13 @@ fp8_tiles_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap x_map, con
 {
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    // full / empty: stages; dfull / dempty: accumulators; in: a drain warp's input tile
-    const uint32_t bar_full = base, bar_empty = base + 64, bar_dfull = base + 128, bar_dempty = base + 144, bar_in = base + 192, tmem_slot = base + 256;
-    const uint32_t ring = base + 1024, out_stage = ring + kFp8Stages * kFp8StageBytes;
+    // full (the leader's): both CTAs' copies into a stage have landed; empty (in both): the MMAs that read it have completed; dfull (in
+    // both): an accumulator is complete and its scales are written; dempty (the leader's): both CTAs have drained it; in: a drain warp's input
+    const uint32_t bar_full = base, bar_empty = base + 64, bar_dfull = base + 128, bar_dempty = base + 160, bar_in = base + 192, tmem_slot = base + 448,
+                   bell = base + 512;
+    const uint32_t ring = base + 1024, out_stage = ring + kFp8Stages * kFp8StageBytes, scale_ring = out_stage + 2 * kFp8DrainWarps * kFp8OutBytes;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    const int rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     const int tiles = a.tiles_m * a.tiles_n, KB = a.KB, F = a.N / 2;
 
     if (threadIdx.x == 0) {
@@ -202,206 +244,239 @@ fp8_tiles_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap x_map, con
             mbar_init(bar_empty + 8 * s, 1);
         }
         for (int s = 0; s < 2; ++s) {
-            mbar_init(bar_dfull + 8 * s, 1);
-            mbar_init(bar_dempty + 8 * s, kFp8DrainWarps);
+            mbar_init(bar_dfull + 8 * s, 3);      // the MMAs, two warps' scales
+            mbar_init(bar_dempty + 8 * s, 1);
         }
-        for (int s = 0; s < kFp8DrainWarps; ++s) mbar_init(bar_in + 8 * s, 1);
+        for (int s = 0; s < 2 * kFp8DrainWarps; ++s) mbar_init(bar_in + 8 * s, 1);
         fence_barrier_init();
         fence_proxy_async();
     }
     if (warp == 1) {
-        tmem_alloc(tmem_slot, 512);
-        tmem_relinquish();
+        tmem_alloc_pair(tmem_slot, 512);
+        tmem_relinquish_pair();
     }
     tc_fence_before_sync();
     __syncthreads();
+    cluster_arrive_release();      // both CTAs' barriers exist before anything arrives from the other
+    cluster_wait_acquire();
     tc_fence_after_sync();
     const uint32_t tmem = lds32(tmem_slot);
     pdl_launch_dependents();
 
-    if (warp == 0) {
+    if (warp < kFp8FirstDrain) {
+      setmaxnreg_dec<kFp8FewRegs>();
+      if (warp == 0) {
         // ------------------------------------------------------------------------------------------ TMA (one thread)
         if (elect_one()) {
             tma_prefetch_descriptor(&x_map);
             tma_prefetch_descriptor(&w_map);
+            const uint32_t full = map_to_cluster_rank(bar_full, 0);
             auto issue_w = [&](int s, int tn, int kb) {
-                const uint32_t st = ring + s * kFp8StageBytes + kFp8XBytes;
-                const int n0 = KIND == kFp8Plain ? tn * kFp8TileN : tn * kFp8Block;
-                tma_load_2d(st, &w_map, kb * kFp8Block, n0, bar_full + 8 * s);
-                tma_load_2d(st + kFp8WBytes / 2, &w_map, kb * kFp8Block, KIND == kFp8Plain ? n0 + kFp8Block : F + n0, bar_full + 8 * s);
+                const int n0 = KIND == kFp8Plain ? tn * kFp8TileN + rank * kFp8Block : rank * F + tn * kFp8Block;
+                tma_load_2d_pair(ring + s * kFp8StageBytes + kFp8HalfBytes, &w_map, kb * kFp8Block, n0, full + 8 * s);
             };
-            // weights do not depend on earlier kernels: the first ones are requested before these have ended
+            // weights do not depend on earlier kernels: the first ones are requested before these have ended (the bytes are counted
+            // before they are expected: the barrier's phase cannot end without the leader's arrival)
             int tm, tn, early = 0;
-            fp8_tile(blockIdx.x, a.tiles_m, a.tiles_n, tm, tn);
-            for (; early < kFp8Stages && early < KB; ++early) {
-                mbar_expect_tx(bar_full + 8 * early, kFp8WBytes);
-                issue_w(early, tn, early);
-            }
+            fp8_tile(pair, a.tiles_m, a.tiles_n, tm, tn);
+            for (; early < kFp8Stages && early < KB; ++early) issue_w(early, tn, early);
             pdl_wait();
             int i = 0;      // blocks requested
             bool ok = true;
-            for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
+            for (int t = pair; t < tiles && ok; t += pairs) {
                 fp8_tile(t, a.tiles_m, a.tiles_n, tm, tn);
                 for (int kb = 0; kb < KB; ++kb, ++i) {
                     const int s = i % kFp8Stages;
                     if (i >= kFp8Stages && !(ok = mbar_wait(bar_empty + 8 * s, (uint32_t)(i / kFp8Stages - 1) & 1))) break;
-                    if (i < early) {
-                        mbar_arrive_expect_tx(bar_full + 8 * s, kFp8XBytes);
-                    } else {
-                        mbar_arrive_expect_tx(bar_full + 8 * s, kFp8XBytes + kFp8WBytes);
-                        issue_w(s, tn, kb);
-                    }
-                    tma_load_2d(ring + s * kFp8StageBytes, &x_map, kb * kFp8Block, tm * kFp8TileM, bar_full + 8 * s);
+                    if (rank == 0) mbar_arrive_expect_tx(bar_full + 8 * s, 2 * kFp8StageBytes);
+                    if (i >= early) issue_w(s, tn, kb);
+                    tma_load_2d_pair(ring + s * kFp8StageBytes, &x_map, kb * kFp8Block, tm * kFp8TileM + rank * kFp8HalfM, full + 8 * s);
                 }
             }
-            // nothing may be on its way into this shared memory when the CTA ends
-            for (int j = i < kFp8Stages ? 0 : i - kFp8Stages; j < i; ++j) mbar_wait(bar_full + 8 * (j % kFp8Stages), (uint32_t)(j / kFp8Stages) & 1);
+            // nothing may be on its way into either shared memory when the CTAs end
+            if (rank == 0)
+                for (int j = i < kFp8Stages ? 0 : i - kFp8Stages; j < i; ++j) mbar_wait(bar_full + 8 * (j % kFp8Stages), (uint32_t)(j / kFp8Stages) & 1);
         }
-    } else if (warp == 1) {
-        // ------------------------------------------------------------------------------------------ MMA (one thread)
-        if (elect_one()) {
+      } else if (warp == 1) {
+        // ------------------------------------------------------------------------------------------ MMA (one thread of the leader)
+        if (rank == 0 && elect_one()) {
             constexpr uint32_t idesc = umma_idesc_f16(kFp8TileM, kFp8TileN);      // (both operands e4m3: format fields 0)
-            int i = 0;
-            bool ok = true;
-            for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x)
-                for (int kb = 0; kb < KB; ++kb, ++i) {
-                    const int s = i % kFp8Stages, d = i & 1;
-                    if (!(ok = mbar_wait(bar_full + 8 * s, (uint32_t)(i / kFp8Stages) & 1))) break;
-                    if (i >= 2 && !(ok = mbar_wait(bar_dempty + 8 * d, (uint32_t)(i / 2 - 1) & 1))) break;
-                    tc_fence_after_sync();
-                    const uint64_t xd = umma_desc_k_major_sw128(ring + s * kFp8StageBytes);
-                    const uint64_t wd = umma_desc_k_major_sw128(ring + s * kFp8StageBytes + kFp8XBytes);
+            auto wait = [](uint32_t bar, uint32_t parity) { return mbar_try_wait_cluster(bar, parity) || mbar_wait_cluster(bar, parity); };
+            const int blocks = ((tiles - 1 - pair) / pairs + 1) * KB;
+            int s = 0;
+            uint32_t ph = 0;
+            for (int i = 0; i < blocks; ++i) {
+                const int d = i & 1;
+                if (!wait(bar_full + 8 * s, ph)) break;
+                if (i >= 2 && !wait(bar_dempty + 8 * d, (uint32_t)(i / 2 - 1) & 1)) break;
+                tc_fence_after_sync();
+                const uint64_t xd = umma_desc_k_major_sw128(ring + s * kFp8StageBytes);
+                const uint64_t wd = umma_desc_k_major_sw128(ring + s * kFp8StageBytes + kFp8HalfBytes);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) umma_f8_ss(tmem + d * kFp8TileN, xd + 2 * j, wd + 2 * j, idesc, j);
-                    umma_commit(bar_empty + 8 * s);
-                    umma_commit(bar_dfull + 8 * d);
-                }
+                for (int j = 0; j < 4; ++j) umma_f8_ss_pair(tmem + d * kFp8TileN, xd + 2 * j, wd + 2 * j, idesc, j);
+                umma_commit_pair(bar_dfull + 8 * d, 3);
+                umma_commit_pair(bar_empty + 8 * s, 3);
+                mbar_arrive_expect_tx(bar_dempty + 8 * d, 2 * 4 * kFp8DrainWarps);
+                if (++s == kFp8Stages) s = 0, ph ^= 1;
+            }
         }
-    } else {
-        // ------------------------------------------------------------------------------------------ drain
+      } else {
+        // ------------------------------------------------------------------------------------------ scales
+        // Lane l of the two warps' 64 has rows 2 l and 2 l + 1.  Block i's go into slot i % 4 once block i - 2 is complete: its MMA
+        // waited until block i - 4, which had the slot, was drained.  They count as an arrival for block i's accumulator.
         pdl_wait();
-        const int q = warp & 3, half = (warp - 2) >> 2;                  // lanes 32 q .. of tensor memory; which columns
-        const uint32_t stage = out_stage + (warp - 2) * kFp8OutBytes, my_in = bar_in + 8 * (warp - 2);
-        const int col0 = KIND == kFp8Plain ? 128 * half : 64 * half, col1 = KIND == kFp8Plain ? col0 + 64 : 128 + col0;
-        const int nb_last = fp8_blocks(a.N) - 1;
-        int i = 0, ins = 0;
-        bool ok = true;      // false once a wait has given up: from then on nothing is waited for or stored, but every barrier met
-        for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
+        const int nb_last = fp8_blocks(a.N) - 1, l2 = 2 * (threadIdx.x - 64);
+        const bool by_four = (KB & 3) == 0;
+        auto four = [&](const float *p, int kb) {
+            if (by_four) return __ldg(reinterpret_cast<const float4 *>(p + kb));
+            return make_float4(__ldg(p + kb), __ldg(p + min(kb + 1, KB - 1)), __ldg(p + min(kb + 2, KB - 1)), __ldg(p + min(kb + 3, KB - 1)));
+        };
+        float4 x[2], w[2];      // [row], [weight block]: four blocks of K
+        auto fetch = [&](int t, int kb) {
             int tm, tn;
             fp8_tile(t, a.tiles_m, a.tiles_n, tm, tn);
-            const int row0 = tm * kFp8TileM + 32 * q, row = row0 + lane;
-            const bool live = row0 < a.M;
-            // first columns of this warp's two groups of 64, in y or (gated kinds) in the F columns of the result
-            const int out0 = KIND == kFp8Plain ? tn * kFp8TileN + col0 : tn * kFp8Block + col0;
-            if (KIND != kFp8Plain || a.has_in) {      // the input of the first group (gated: the only one)
-                if (live && out0 < (KIND == kFp8Plain ? a.N : F) && elect_one()) {
-                    tma_store_wait_read();
-                    if (KIND == kFp8Backward || KIND == kFp8Plain) {
-                        mbar_arrive_expect_tx(my_in, kFp8OutBytes);
-                        tma_load_2d(stage, &in_map, out0, row0, my_in);
-                    }
+            const int row = tm * kFp8TileM + rank * kFp8HalfM + l2;
+#pragma unroll
+            for (int r = 0; r < 2; ++r) x[r] = four(a.x_scales + (size_t)min(row + r, a.M - 1) * KB, kb);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                w[h] = four(a.w_scales + (size_t)(KIND == kFp8Plain ? min(2 * tn + h, nb_last) : h * (F / kFp8Block) + tn) * KB, kb);
+        };
+        int i = 0;
+        bool ok = true;
+        fetch(pair, 0);
+        for (int t = pair; t < tiles && ok; t += pairs)
+            for (int kb0 = 0; kb0 < KB && ok; kb0 += 4) {
+                float2 p[2][4];      // [weight block][block of K]: the lane's rows
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    p[h][0] = make_float2(x[0].x * w[h].x, x[1].x * w[h].x);
+                    p[h][1] = make_float2(x[0].y * w[h].y, x[1].y * w[h].y);
+                    p[h][2] = make_float2(x[0].z * w[h].z, x[1].z * w[h].z);
+                    p[h][3] = make_float2(x[0].w * w[h].w, x[1].w * w[h].w);
+                }
+                if (kb0 + 4 < KB) fetch(t, kb0 + 4);
+                else if (t + pairs < tiles) fetch(t + pairs, 0);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (kb0 + j >= KB || !ok) break;
+                    if (i >= 2) ok = mbar_wait_warp(bar_dfull + 8 * (i & 1), (uint32_t)(i / 2 - 1) & 1);
+                    const uint32_t slot = scale_ring + (i & 3) * kFp8ScaleBytes + 4 * l2;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) sts64(slot + h * kFp8HalfM * 4, __float_as_uint(p[h][j].x), __float_as_uint(p[h][j].y));
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar_dfull + 8 * (i & 1));
+                    ++i;
                 }
             }
-            const int nb0 = KIND == kFp8Plain ? min(tn * 2 + half, nb_last) : tn, nb1 = KIND == kFp8Plain ? nb0 : F / kFp8Block + tn;
-            const float *ws0 = a.w_scales + (size_t)nb0 * KB, *ws1 = a.w_scales + (size_t)nb1 * KB;
-            const float *xs = a.x_scales + (size_t)min(row, a.M - 1) * KB;
+      }
+    } else {
+        // ------------------------------------------------------------------------------------------ drain
+        setmaxnreg_inc<kFp8ManyRegs>();
+        pdl_wait();
+        const int q = warp & 3, cols = 64 * ((warp - kFp8FirstDrain) >> 2);      // lanes 32 q .. of tensor memory; first column of a half
+        const uint32_t stage = out_stage + (warp - kFp8FirstDrain) * 2 * kFp8OutBytes, my_in = bar_in + 16 * (warp - kFp8FirstDrain);
+        const uint32_t lanes = tmem + ((uint32_t)(32 * q) << 16);
+        const uint32_t my_scale = scale_ring + (32 * q + lane) * 4;
+        // "drained" to the leader: a store of four bytes that counts on its barrier (a remote arrival would hold the warp up)
+        const uint32_t leader_dempty = map_to_cluster_rank(bar_dempty, 0), leader_bell = map_to_cluster_rank(bell + 4 * warp, 0);
+        auto drained = [&](uint32_t offset) {
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) st_async_f32(leader_bell, 0.0f, leader_dempty + offset);
+        };
+        uint32_t at = 0, parity = 0, slot = 0;      // of this block of K: its barriers' offset (0 or 8), their parity, its scales
+        int ins = 0;
+        bool ok = true;      // false once a wait has given up: from then on nothing is waited for or stored, but every barrier met
+        for (int t = pair; t < tiles; t += pairs) {
+            int tm, tn;
+            fp8_tile(t, a.tiles_m, a.tiles_n, tm, tn);
+            const int row0 = tm * kFp8TileM + rank * kFp8HalfM + 32 * q, row = row0 + lane;
+            const bool live = row0 < a.M;
+            // first column of this warp's 64 of half h, in y or (gated kinds) among the F columns of the result
+            auto out_col = [&](int h) { return KIND == kFp8Plain ? tn * kFp8TileN + h * 128 + cols : tn * kFp8Block + cols; };
+            if (live && elect_one()) {
+                tma_store_wait_read();      // the last tile's results have left the stages
+                if (KIND == kFp8Backward || (KIND == kFp8Plain && a.has_in))
+#pragma unroll
+                    for (int h = 0; h < (KIND == kFp8Plain ? 2 : 1); ++h)
+                        if (KIND != kFp8Plain || out_col(h) < a.N) {
+                            mbar_arrive_expect_tx(my_in + 8 * h, kFp8OutBytes);
+                            tma_load_2d(stage + h * kFp8OutBytes, &in_map, out_col(h), row0, my_in + 8 * h);
+                        }
+            }
+            __syncwarp();
             uint64_t acc[2][32];
 #pragma unroll
             for (int j = 0; j < 64; ++j) acc[j / 32][j % 32] = 0;
-            float x_next = __ldg(xs), w0_next = __ldg(ws0), w1_next = __ldg(ws1);
-            for (int kb = 0; kb < KB; ++kb, ++i) {
-                const uint64_t s0 = both(x_next * w0_next), s1 = KIND == kFp8Plain ? s0 : both(x_next * w1_next);
-                const int nx = min(kb + 1, KB - 1);
-                x_next = __ldg(xs + nx), w0_next = __ldg(ws0 + nx);
-                if (KIND != kFp8Plain) w1_next = __ldg(ws1 + nx);
-                const int d = i & 1;
-                if (ok) ok = mbar_wait_warp(bar_dfull + 8 * d, (uint32_t)(i / 2) & 1);
+            for (int kb = 0; kb < KB; ++kb) {
+                const uint32_t from = lanes + 32 * at + cols;
+                if (ok) ok = mbar_wait_warp_inline(bar_dfull + at, parity);
                 tc_fence_after_sync();
                 if (live) {
-                    const uint32_t from = tmem + d * kFp8TileN + ((uint32_t)(32 * q) << 16);
+                    uint32_t v[2][16];
+                    tmem_ld_32x16(from, v[0]);
+                    const uint64_t s0 = both(__uint_as_float(lds32(my_scale + slot)));
+                    const uint64_t s1 = both(__uint_as_float(lds32(my_scale + slot + kFp8HalfM * 4)));
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t v[32];
-                        tmem_ld_32x32(from + (c < 2 ? col0 : col1) + 32 * (c & 1), v);
+                    for (int c = 0; c < 8; ++c) {      // the next 16 columns are on their way while these are added
                         tmem_wait_ld();
+                        if (c < 7) tmem_ld_32x16(from + (c < 3 ? 0 : 128) + 16 * ((c + 1) & 3), v[(c + 1) & 1]);
+                        else drained(at);
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) fma2(acc[c / 2][16 * (c & 1) + j], v[2 * j], v[2 * j + 1], c < 2 ? s0 : s1);
+                        for (int j = 0; j < 8; ++j) fma2(acc[c / 4][8 * (c & 3) + j], v[c & 1][2 * j], v[c & 1][2 * j + 1], c < 4 ? s0 : s1);
                     }
+                } else {
+                    drained(at);
                 }
-                tc_fence_before_sync();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar_dempty + 8 * d);
+                parity ^= at >> 3;
+                at ^= 8;
+                slot = (slot + kFp8ScaleBytes) & (kFp8ScaleSlots * kFp8ScaleBytes - 1);
             }
             if (!live) continue;
 
-            // row `lane` of the stage, 16-byte piece c: 128-byte rows, 128-byte swizzle (the tensor maps')
-            auto piece = [&](int c) { return stage + lane * 128 + ((c ^ (lane & 7)) << 4); };
-            auto send16 = [&](int col) {
-                fence_proxy_async();
-                __syncwarp();
-                if (ok && elect_one()) tma_store_2d(&out_map, stage, col, row0);
-            };
-            auto stage_free = [&]() {
-                if (elect_one()) tma_store_wait_read();      // (the lane that issued: one and the same)
-                __syncwarp();
-            };
+            // row `lane` of a stage, 16-byte piece c: 128-byte rows, 128-byte swizzle (the tensor maps')
+            auto piece = [&](int h, int c) { return stage + h * kFp8OutBytes + lane * 128 + ((c ^ (lane & 7)) << 4); };
             if constexpr (KIND == kFp8Plain) {
 #pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    const int col = out0 + 64 * g;
+                for (int h = 0; h < 2; ++h) {
+                    const int col = out_col(h);
                     if (col >= a.N) break;
-                    if (a.has_in) {
-                        if (g == 1) {
-                            stage_free();
-                            if (elect_one()) {
-                                mbar_arrive_expect_tx(my_in, kFp8OutBytes);
-                                tma_load_2d(stage, &in_map, col, row0, my_in);
-                            }
-                        }
-                        if (ok) ok = mbar_wait_warp(my_in, (uint32_t)ins & 1);
-                        ++ins;
-                    } else {
-                        stage_free();
-                    }
+                    if (a.has_in && ok) ok = mbar_wait_warp_inline(my_in + 8 * h, (uint32_t)ins >> h & 1);
+                    if (a.has_in) ins ^= 1 << h;
 #pragma unroll
                     for (int c = 0; c < 8; ++c) {
                         float2 f[4];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) f[j] = unpack2(acc[g][4 * c + j]);
-                        if (a.bias != nullptr && col + 8 * c < a.N) {      // (N % 8 == 0)
-                            const uint4 b = __ldg(reinterpret_cast<const uint4 *>(a.bias + col + 8 * c));
+                        for (int j = 0; j < 4; ++j) f[j] = unpack2(acc[h][4 * c + j]);
+                        auto add = [&](const uint4 b) {
                             const uint32_t bw[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
                                 const float2 e = pair_to_float2<BF>(bw[j]);
                                 f[j].x += e.x, f[j].y += e.y;
                             }
-                        }
-                        if (a.has_in) {
-                            const uint4 b = lds128(piece(c));
-                            const uint32_t bw[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const float2 e = pair_to_float2<BF>(bw[j]);
-                                f[j].x += e.x, f[j].y += e.y;
-                            }
-                        }
-                        sts128(piece(c), make_uint4(pack_out16<BF>(f[0]), pack_out16<BF>(f[1]), pack_out16<BF>(f[2]), pack_out16<BF>(f[3])));
+                        };
+                        if (a.bias != nullptr && col + 8 * c < a.N) add(__ldg(reinterpret_cast<const uint4 *>(a.bias + col + 8 * c)));      // (N % 8 == 0)
+                        if (a.has_in) add(lds128(piece(h, c)));
+                        sts128(piece(h, c), make_uint4(pack_out16<BF>(f[0]), pack_out16<BF>(f[1]), pack_out16<BF>(f[2]), pack_out16<BF>(f[3])));
                     }
-                    send16(col);
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (ok && elect_one()) tma_store_2d(&out_map, stage + h * kFp8OutBytes, col, row0);
                 }
             } else {
                 // h = silu(gate) up in the place of gate's sums; backward: the gradients in the places of both
-                uint32_t top0 = 0, top1 = 0;
+                uint32_t top[2] = {0, 0};
                 if constexpr (KIND == kFp8Backward) {
-                    if (ok) ok = mbar_wait_warp(my_in, (uint32_t)ins & 1);
-                    ++ins;
+                    if (ok) ok = mbar_wait_warp_inline(my_in, (uint32_t)ins & 1);
+                    ins ^= 1;
                 }
 #pragma unroll
                 for (int c = 0; c < 8; ++c) {
                     uint32_t dw[4];
                     if constexpr (KIND == kFp8Backward) {
-                        const uint4 b = lds128(piece(c));
+                        const uint4 b = lds128(piece(0, c));
                         dw[0] = b.x, dw[1] = b.y, dw[2] = b.z, dw[3] = b.w;
                     }
 #pragma unroll
@@ -416,30 +491,27 @@ fp8_tiles_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap x_map, con
                             r = make_float2(e.x * u.x * p.x * (1.0f + g.x * (1.0f - p.x)), e.y * u.y * p.y * (1.0f + g.y * (1.0f - p.y)));
                             const float2 v = make_float2(e.x * g.x * p.x, e.y * g.y * p.y);
                             acc[1][4 * c + j] = pack2(v);
-                            top1 = max(top1, max(abs_bits(v.x), abs_bits(v.y)));
+                            top[1] = max(top[1], max(abs_bits(v.x), abs_bits(v.y)));
                         }
                         acc[0][4 * c + j] = pack2(r);
-                        top0 = max(top0, max(abs_bits(r.x), abs_bits(r.y)));
+                        top[0] = max(top[0], max(abs_bits(r.x), abs_bits(r.y)));
                     }
                 }
                 constexpr int kOuts = KIND == kFp8Backward ? 2 : 1;
+                __syncwarp();      // every lane has read its input: the stages are free
                 if constexpr (OUT8) {
-                    // the two warps that hold a row's 128 columns exchange their maxima (in the stages, which are free)
-                    stage_free();
-                    asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(stage + 8 * lane), "r"(top0), "r"(top1) : "memory");
+                    // the two warps that hold a row's 128 columns exchange their maxima (in their stages)
+                    asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(stage + 8 * lane), "r"(top[0]), "r"(top[1]) : "memory");
                     named_bar_sync(1 + q, 64);
-                    const uint2 other = lds64(out_stage + ((warp - 2) ^ 4) * kFp8OutBytes + 8 * lane);
+                    const uint2 other = lds64(out_stage + ((warp - kFp8FirstDrain) ^ 4) * 2 * kFp8OutBytes + 8 * lane);
                     named_bar_sync(1 + q, 64);
-                    const float s0 = fp8_scale(max(top0, other.x)), s1 = fp8_scale(max(top1, other.y));
+                    top[0] = max(top[0], other.x), top[1] = max(top[1], other.y);
                     const int FB = F / kFp8Block;
-                    if (half == 0 && row < a.M && ok) {
-                        a.out_scales[(size_t)row * kOuts * FB + tn] = s0;
-                        if (kOuts == 2) a.out_scales[(size_t)row * 2 * FB + FB + tn] = s1;
-                    }
-                    // 64-byte rows, 64-byte swizzle
 #pragma unroll
                     for (int o = 0; o < kOuts; ++o) {
-                        const float s = o ? s1 : s0;
+                        const float s = fp8_scale(top[o]);
+                        if (cols == 0 && row < a.M && ok) a.out_scales[(size_t)row * kOuts * FB + o * FB + tn] = s;
+                        // 64-byte rows, 64-byte swizzle
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
                             uint32_t w[4];
@@ -448,32 +520,35 @@ fp8_tiles_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap x_map, con
                                 const float2 f0 = unpack2(acc[o][8 * c + 2 * j]), f1 = unpack2(acc[o][8 * c + 2 * j + 1]);
                                 w[j] = fp8_four(__fdiv_rn(f0.x, s), __fdiv_rn(f0.y, s), __fdiv_rn(f1.x, s), __fdiv_rn(f1.y, s));
                             }
-                            sts128(stage + o * 2048 + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
+                            sts128(stage + o * kFp8OutBytes + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
                         }
                     }
-                    fence_proxy_async();
-                    __syncwarp();
-                    if (ok && elect_one())
-                        for (int o = 0; o < kOuts; ++o) tma_store_2d(&out_map, stage + o * 2048, o * F + out0, row0);
                 } else {
 #pragma unroll
-                    for (int o = 0; o < kOuts; ++o) {
-                        stage_free();
+                    for (int o = 0; o < kOuts; ++o)
 #pragma unroll
                         for (int c = 0; c < 8; ++c)
-                            sts128(piece(c), make_uint4(pack_out16<BF>(unpack2(acc[o][4 * c])), pack_out16<BF>(unpack2(acc[o][4 * c + 1])),
-                                                        pack_out16<BF>(unpack2(acc[o][4 * c + 2])), pack_out16<BF>(unpack2(acc[o][4 * c + 3]))));
-                        send16(o * F + out0);
-                    }
+                            sts128(piece(o, c), make_uint4(pack_out16<BF>(unpack2(acc[o][4 * c])), pack_out16<BF>(unpack2(acc[o][4 * c + 1])),
+                                                           pack_out16<BF>(unpack2(acc[o][4 * c + 2])), pack_out16<BF>(unpack2(acc[o][4 * c + 3]))));
                 }
+                fence_proxy_async();
+                __syncwarp();
+                if (ok && elect_one())
+#pragma unroll
+                    for (int o = 0; o < kOuts; ++o) tma_store_2d(&out_map, stage + o * kFp8OutBytes, o * F + out_col(0), row0);
             }
         }
         if (elect_one()) tma_store_wait();
     }
+    // neither CTA may free tensor memory or end while the pair's MMAs, or the other's copies and arrivals, can still touch it
     tc_fence_before_sync();
     __syncthreads();
-    tc_fence_after_sync();
-    if (warp == 1) tmem_dealloc(tmem, 512);
+    cluster_arrive_release();
+    cluster_wait_acquire();
+    if (warp == 1) {
+        tc_fence_after_sync();
+        tmem_dealloc_pair(tmem, 512);
+    }
 }
 
 // ---- launches -----------------------------------------------------------------------------------------------------------
@@ -537,9 +612,17 @@ template <int KIND, bool BF, bool OUT8>
 int launch_fp8_tiles(const Fp8Call &c, cudaStream_t s)
 {
     static int configured[64];
+    static std::atomic<int> registers{0};
     auto kernel = fp8_tiles_kernel<KIND, BF, OUT8>;
     int st = ensure_dynamic_smem((const void *)kernel, configured, kFp8SmemBytes);
     if (st) return st;
+    if (registers.load() == 0) {      // the warps that take registers would wait for ever for what the launch did not bring
+        cudaFuncAttributes fa;
+        const cudaError_t e = cudaFuncGetAttributes(&fa, (const void *)kernel);
+        if (e != cudaSuccess) return record_cuda_error(e);
+        registers.store(fa.numRegs);
+    }
+    if (registers.load() < kFp8LaunchRegs) return GPTQ_ERR_UNSUPPORTED;
     const int F = c.N / 2;
     Fp8Args a{};
     a.x_scales = c.x_scales, a.w_scales = c.w_scales, a.bias = (const __half *)c.bias, a.out_scales = c.out_scales;
@@ -553,7 +636,7 @@ int launch_fp8_tiles(const Fp8Call &c, cudaStream_t s)
     const auto u8 = CU_TENSOR_MAP_DATA_TYPE_UINT8;
     const auto b16 = CU_TENSOR_MAP_DATA_TYPE_UINT16;
     const auto sw128 = CU_TENSOR_MAP_SWIZZLE_128B;
-    st = make_tensor_map_2d(&xm, u8, c.x, c.K, c.M, c.K, kFp8Block, kFp8TileM, sw128);
+    st = make_tensor_map_2d(&xm, u8, c.x, c.K, c.M, c.K, kFp8Block, kFp8HalfM, sw128);
     if (!st) st = make_tensor_map_2d(&wm, u8, c.w, c.K, c.N, c.K, kFp8Block, kFp8Block, sw128);
     const uint64_t in_cols = KIND == kFp8Plain ? c.N : F, out_cols = KIND == kFp8Gated ? F : c.N;
     if (!st) {
@@ -566,7 +649,7 @@ int launch_fp8_tiles(const Fp8Call &c, cudaStream_t s)
     }
     if (st) return st;
     void *args[] = {&a, &xm, &wm, &im, &om};
-    return record_cuda_error(fp8_launch((void *)kernel, (int)(tiles < c.sms ? tiles : c.sms), kFp8Threads, kFp8SmemBytes, 1, s, args));
+    return record_cuda_error(fp8_launch((void *)kernel, 2 * (int)(tiles < c.sms / 2 ? tiles : c.sms / 2), kFp8Threads, kFp8SmemBytes, 2, s, args));
 }
 
 inline int launch_fp8(const Fp8Call &c, cudaStream_t s)
