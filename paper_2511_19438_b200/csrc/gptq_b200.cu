@@ -14,6 +14,7 @@
 #include "gptq_moe.cuh"
 #include "gptq_lora.cuh"
 #include "gptq_fp8.cuh"
+#include "gptq_fp8_few.cuh"
 
 #include <atomic>
 #include <cstdio>
@@ -1371,12 +1372,13 @@ static int fp8_dispatch(Fp8Call c, int format, void *stream)
         uint8_t *ws;
         st = registered_workspace(dev, fp8_workspace_need(c.M, c.K), &ws);
         if (st) return st;
+        if (c.M <= kFp8FewInline) return launch_fp8_any(c, s);      // (needs no scratch, but who has 4 rows may have 5 next)
         float *scales = (float *)(ws + fp8_x_bytes(c.M, c.K));
         st = launch_fp8_quantize(c.x, ws, scales, c.M, c.K, c.bf16, c.sms, s);
         if (st) return st;
         c.x = ws, c.x_scales = scales;
     }
-    return launch_fp8(c, s);
+    return launch_fp8_any(c, s);
 }
 
 extern "C" {

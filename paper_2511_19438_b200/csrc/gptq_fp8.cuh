@@ -24,6 +24,23 @@ __device__ __forceinline__ float fp8_scale(uint32_t top)
     const float s = __fdiv_rn(__uint_as_float(top), kFp8Max);      // (an infinity or NaN stays one: the whole block becomes NaN)
     return s < kFp8ScaleMin ? kFp8ScaleMin : s;
 }
+// v / s, rounded to the nearest, for many v of one s: Markstein's theorem (IBM J. Res. Dev. 34, 1990) - with y the nearest number to
+// 1 / s and q = v y, the remainder v - q s is exact and q + (v - q s) y rounds to the nearest quotient.  Small blocks are scaled first, so that the
+// remainder does not underflow.  (The operator's own division leaves its fast way for zeros: padding rows made a gated call of 1000 rows 26 us instead of 17.)
+struct Fp8Quotient {
+    float f, s, y;
+    __device__ __forceinline__ explicit Fp8Quotient(float scale)
+    {
+        f = scale < 0x1p-60f ? 0x1p64f : 1.0f;
+        s = scale * f;
+        y = __frcp_rn(s);
+    }
+    __device__ __forceinline__ float operator()(float v) const
+    {
+        const float a = v * f, q = a * y;
+        return fmaf(fmaf(-q, s, a), y, q);
+    }
+};
 // two numbers to e4m3, nearest even; a in the low byte; NaN becomes NaN, what rounds beyond 448 becomes 448
 __device__ __forceinline__ uint32_t fp8_pair(float a, float b)
 {
@@ -34,6 +51,25 @@ __device__ __forceinline__ uint32_t fp8_pair(float a, float b)
 __device__ __forceinline__ uint32_t fp8_four(float a, float b, float c, float d) { return fp8_pair(a, b) | fp8_pair(c, d) << 16; }
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
+// loads that stay behind the wait for earlier kernels
+__device__ __forceinline__ uint4 ldg_behind(const void *p)
+{
+    uint4 v;
+    asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ uint2 ldg64_behind(const void *p)
+{
+    uint2 v;
+    asm volatile("ld.global.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ float ldgf_behind(const float *p)
+{
+    float v;
+    asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(p));
+    return v;
+}
 // Half a warp per block of 128: 16 bytes of x and 8 of the result per lane.  kFp8QuantUnroll blocks per half warp are requested
 // together.
 constexpr int kFp8QuantThreads = 256, kFp8QuantUnroll = 4;
@@ -43,20 +79,24 @@ __global__ void __launch_bounds__(kFp8QuantThreads) fp8_quantize_kernel(const ui
     pdl_launch_dependents();
     pdl_wait();
     const int lane16 = threadIdx.x & 15;
-    const long long halves = (long long)gridDim.x * (kFp8QuantThreads / 16);
-    const long long first = (long long)blockIdx.x * (kFp8QuantThreads / 16) + threadIdx.x / 16;
-    for (long long b0 = first; b0 < blocks; b0 += halves * kFp8QuantUnroll) {
+    // half warp h has blocks h, h + halves, ... (rows after rows); the step as rows and blocks, so that only the first takes a division
+    const long long halves = (long long)gridDim.x * (kFp8QuantThreads / 16), step_row = halves / KB;
+    const int step_kb = (int)(halves - step_row * KB);
+    long long b0 = (long long)blockIdx.x * (kFp8QuantThreads / 16) + threadIdx.x / 16, row = b0 / KB;
+    int kb = (int)(b0 - row * KB);
+    // (a warp's two half warps go on together: the maximum is found by the whole warp)
+    for (; b0 - (threadIdx.x >> 4 & 1) < blocks; b0 += halves * kFp8QuantUnroll) {
         uint4 v[kFp8QuantUnroll];
         size_t at[kFp8QuantUnroll];
         bool in[kFp8QuantUnroll];
 #pragma unroll
         for (int i = 0; i < kFp8QuantUnroll; ++i) {
-            const long long b = b0 + i * halves;
-            const long long row = b / KB;
-            const int k = (int)(b - row * KB) * kFp8Block + lane16 * 8;
-            in[i] = b < blocks && k < K;
+            const int k = kb * kFp8Block + lane16 * 8;
+            in[i] = b0 + i * halves < blocks && k < K;
             at[i] = ((size_t)row * K + k) / 8;
-            v[i] = in[i] ? x[at[i]] : make_uint4(0, 0, 0, 0);
+            v[i] = in[i] ? ldg_behind(x + at[i]) : make_uint4(0, 0, 0, 0);
+            row += step_row, kb += step_kb;
+            if (kb >= KB) kb -= KB, ++row;
         }
 #pragma unroll
         for (int i = 0; i < kFp8QuantUnroll; ++i) {
@@ -71,8 +111,9 @@ __global__ void __launch_bounds__(kFp8QuantThreads) fp8_quantize_kernel(const ui
 #pragma unroll
             for (int o = 8; o; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
             const float s = fp8_scale(top);
+            const Fp8Quotient by(s);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) f[j] = make_float2(__fdiv_rn(f[j].x, s), __fdiv_rn(f[j].y, s));
+            for (int j = 0; j < 4; ++j) f[j] = make_float2(by(f[j].x), by(f[j].y));
             if (in[i]) q[at[i]] = make_uint2(fp8_four(f[0].x, f[0].y, f[1].x, f[1].y), fp8_four(f[2].x, f[2].y, f[3].x, f[3].y));
             if (lane16 == 0 && b0 + i * halves < blocks) scales[b0 + i * halves] = s;
         }
@@ -109,9 +150,10 @@ __global__ void __launch_bounds__(256) fp8_transpose_kernel(const uint8_t *w, co
 // memory, one block of K each, so that a block is drained while the next is multiplied.  Token rows are the MMA's rows: a thread that
 // drains holds one token row, hence one scale per block of K and weight block.  A drain warp has 2 x 64 of the tile's columns; in the gated
 // kinds these are gate and up of the same 64 columns, so that the activation needs no exchange but the maximum over two warps.
-//   warp 0  TMA of this CTA's halves; both CTAs' copies complete on the leader's barrier
+//   warps 0, 3  TMA of this CTA's halves, weights and activations (a turn of such a loop takes its thread 210 clocks whatever the
+//           copy's size); both CTAs' copies complete on the leader's barrier
 //   warp 1  the MMAs (the leader's)
-//   warps 2, 3  products of scales, two blocks ahead: 128 rows x 2 weight blocks per block of K into a ring of four
+//   warp 2  products of scales, two blocks ahead: 128 rows x 2 weight blocks per block of K into a ring of four
 //   warps 4 to 11 drain.  The first four give registers to them: 128 sums and 32 columns on their way.
 constexpr int kFp8TileM = 256, kFp8TileN = 256, kFp8HalfM = 128, kFp8Stages = 4;
 constexpr int kFp8FirstDrain = 4, kFp8DrainWarps = 8, kFp8Threads = 32 * (kFp8FirstDrain + kFp8DrainWarps);
@@ -240,11 +282,11 @@ fp8_tiles_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap x_map, con
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kFp8Stages; ++s) {
-            mbar_init(bar_full + 8 * s, 1);
+            mbar_init(bar_full + 8 * s, 2);      // the leader's threads for weights and activations, each with both CTAs' bytes
             mbar_init(bar_empty + 8 * s, 1);
         }
         for (int s = 0; s < 2; ++s) {
-            mbar_init(bar_dfull + 8 * s, 3);      // the MMAs, two warps' scales
+            mbar_init(bar_dfull + 8 * s, 2);      // the MMAs, the scales
             mbar_init(bar_dempty + 8 * s, 1);
         }
         for (int s = 0; s < 2 * kFp8DrainWarps; ++s) mbar_init(bar_in + 8 * s, 1);
@@ -265,37 +307,33 @@ fp8_tiles_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap x_map, con
 
     if (warp < kFp8FirstDrain) {
       setmaxnreg_dec<kFp8FewRegs>();
-      if (warp == 0) {
-        // ------------------------------------------------------------------------------------------ TMA (one thread)
+      if (warp == 0 || warp == 3) {
+        // ------------------------------------------------------------------------------------------ TMA (a thread each)
+        // The other CTA's bytes may be counted before the leader expects them: the barrier's phase cannot end without the leader's
+        // arrivals.  Weights do not depend on earlier kernels: they are not waited for.
         if (elect_one()) {
-            tma_prefetch_descriptor(&x_map);
-            tma_prefetch_descriptor(&w_map);
-            const uint32_t full = map_to_cluster_rank(bar_full, 0);
-            auto issue_w = [&](int s, int tn, int kb) {
-                const int n0 = KIND == kFp8Plain ? tn * kFp8TileN + rank * kFp8Block : rank * F + tn * kFp8Block;
-                tma_load_2d_pair(ring + s * kFp8StageBytes + kFp8HalfBytes, &w_map, kb * kFp8Block, n0, full + 8 * s);
-            };
-            // weights do not depend on earlier kernels: the first ones are requested before these have ended (the bytes are counted
-            // before they are expected: the barrier's phase cannot end without the leader's arrival)
-            int tm, tn, early = 0;
-            fp8_tile(pair, a.tiles_m, a.tiles_n, tm, tn);
-            for (; early < kFp8Stages && early < KB; ++early) issue_w(early, tn, early);
-            pdl_wait();
-            int i = 0;      // blocks requested
+            const CUtensorMap *map = warp == 0 ? &w_map : &x_map;
+            tma_prefetch_descriptor(map);
+            const uint32_t full = map_to_cluster_rank(bar_full, 0), to = ring + (warp == 0 ? kFp8HalfBytes : 0);
+            if (warp == 3) pdl_wait();
+            int s = 0, done = 0;
+            uint32_t ph = 1;
             bool ok = true;
             for (int t = pair; t < tiles && ok; t += pairs) {
+                int tm, tn;
                 fp8_tile(t, a.tiles_m, a.tiles_n, tm, tn);
-                for (int kb = 0; kb < KB; ++kb, ++i) {
-                    const int s = i % kFp8Stages;
-                    if (i >= kFp8Stages && !(ok = mbar_wait(bar_empty + 8 * s, (uint32_t)(i / kFp8Stages - 1) & 1))) break;
-                    if (rank == 0) mbar_arrive_expect_tx(bar_full + 8 * s, 2 * kFp8StageBytes);
-                    if (i >= early) issue_w(s, tn, kb);
-                    tma_load_2d_pair(ring + s * kFp8StageBytes, &x_map, kb * kFp8Block, tm * kFp8TileM + rank * kFp8HalfM, full + 8 * s);
+                const int row = warp == 3 ? tm * kFp8TileM + rank * kFp8HalfM : KIND == kFp8Plain ? tn * kFp8TileN + rank * kFp8Block : rank * F + tn * kFp8Block;
+                for (int kb = 0; kb < KB; ++kb) {
+                    if (done >= kFp8Stages && !(ok = mbar_wait_once(bar_empty + 8 * s, ph))) break;
+                    if (rank == 0) mbar_arrive_expect_tx(bar_full + 8 * s, 2 * kFp8HalfBytes);
+                    tma_load_2d_pair(to + s * kFp8StageBytes, map, kb * kFp8Block, row, full + 8 * s);
+                    ++done;
+                    if (++s == kFp8Stages) s = 0, ph ^= 1;
                 }
             }
             // nothing may be on its way into either shared memory when the CTAs end
-            if (rank == 0)
-                for (int j = i < kFp8Stages ? 0 : i - kFp8Stages; j < i; ++j) mbar_wait(bar_full + 8 * (j % kFp8Stages), (uint32_t)(j / kFp8Stages) & 1);
+            if (rank == 0 && warp == 0)
+                for (int j = done < kFp8Stages ? 0 : done - kFp8Stages; j < done; ++j) mbar_wait(bar_full + 8 * (j % kFp8Stages), (uint32_t)(j / kFp8Stages) & 1);
         }
       } else if (warp == 1) {
         // ------------------------------------------------------------------------------------------ MMA (one thread of the leader)
@@ -322,22 +360,25 @@ fp8_tiles_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap x_map, con
         }
       } else {
         // ------------------------------------------------------------------------------------------ scales
-        // Lane l of the two warps' 64 has rows 2 l and 2 l + 1.  Block i's go into slot i % 4 once block i - 2 is complete: its MMA
-        // waited until block i - 4, which had the slot, was drained.  They count as an arrival for block i's accumulator.
+        // Lane l has rows 4 l .. 4 l + 3.  Block i's go into slot i % 4 once block i - 2 is complete: its MMA waited until block
+        // i - 4, which had the slot, was drained.  They count as an arrival for block i's accumulator.
         pdl_wait();
-        const int nb_last = fp8_blocks(a.N) - 1, l2 = 2 * (threadIdx.x - 64);
+        const int nb_last = fp8_blocks(a.N) - 1, l4 = 4 * lane;
         const bool by_four = (KB & 3) == 0;
         auto four = [&](const float *p, int kb) {
-            if (by_four) return __ldg(reinterpret_cast<const float4 *>(p + kb));
-            return make_float4(__ldg(p + kb), __ldg(p + min(kb + 1, KB - 1)), __ldg(p + min(kb + 2, KB - 1)), __ldg(p + min(kb + 3, KB - 1)));
+            if (by_four) {
+                const uint4 v = ldg_behind(p + kb);
+                return make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
+            }
+            return make_float4(ldgf_behind(p + kb), ldgf_behind(p + min(kb + 1, KB - 1)), ldgf_behind(p + min(kb + 2, KB - 1)), ldgf_behind(p + min(kb + 3, KB - 1)));
         };
-        float4 x[2], w[2];      // [row], [weight block]: four blocks of K
+        float4 x[4], w[2];      // [row], [weight block]: four blocks of K
         auto fetch = [&](int t, int kb) {
             int tm, tn;
             fp8_tile(t, a.tiles_m, a.tiles_n, tm, tn);
-            const int row = tm * kFp8TileM + rank * kFp8HalfM + l2;
+            const int row = tm * kFp8TileM + rank * kFp8HalfM + l4;
 #pragma unroll
-            for (int r = 0; r < 2; ++r) x[r] = four(a.x_scales + (size_t)min(row + r, a.M - 1) * KB, kb);
+            for (int r = 0; r < 4; ++r) x[r] = four(a.x_scales + (size_t)min(row + r, a.M - 1) * KB, kb);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
                 w[h] = four(a.w_scales + (size_t)(KIND == kFp8Plain ? min(2 * tn + h, nb_last) : h * (F / kFp8Block) + tn) * KB, kb);
@@ -347,13 +388,13 @@ fp8_tiles_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap x_map, con
         fetch(pair, 0);
         for (int t = pair; t < tiles && ok; t += pairs)
             for (int kb0 = 0; kb0 < KB && ok; kb0 += 4) {
-                float2 p[2][4];      // [weight block][block of K]: the lane's rows
+                float4 p[2][4];      // [weight block][block of K]: the lane's rows
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    p[h][0] = make_float2(x[0].x * w[h].x, x[1].x * w[h].x);
-                    p[h][1] = make_float2(x[0].y * w[h].y, x[1].y * w[h].y);
-                    p[h][2] = make_float2(x[0].z * w[h].z, x[1].z * w[h].z);
-                    p[h][3] = make_float2(x[0].w * w[h].w, x[1].w * w[h].w);
+                    p[h][0] = make_float4(x[0].x * w[h].x, x[1].x * w[h].x, x[2].x * w[h].x, x[3].x * w[h].x);
+                    p[h][1] = make_float4(x[0].y * w[h].y, x[1].y * w[h].y, x[2].y * w[h].y, x[3].y * w[h].y);
+                    p[h][2] = make_float4(x[0].z * w[h].z, x[1].z * w[h].z, x[2].z * w[h].z, x[3].z * w[h].z);
+                    p[h][3] = make_float4(x[0].w * w[h].w, x[1].w * w[h].w, x[2].w * w[h].w, x[3].w * w[h].w);
                 }
                 if (kb0 + 4 < KB) fetch(t, kb0 + 4);
                 else if (t + pairs < tiles) fetch(t + pairs, 0);
@@ -361,9 +402,10 @@ fp8_tiles_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap x_map, con
                 for (int j = 0; j < 4; ++j) {
                     if (kb0 + j >= KB || !ok) break;
                     if (i >= 2) ok = mbar_wait_warp(bar_dfull + 8 * (i & 1), (uint32_t)(i / 2 - 1) & 1);
-                    const uint32_t slot = scale_ring + (i & 3) * kFp8ScaleBytes + 4 * l2;
+                    const uint32_t slot = scale_ring + (i & 3) * kFp8ScaleBytes + 4 * l4;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) sts64(slot + h * kFp8HalfM * 4, __float_as_uint(p[h][j].x), __float_as_uint(p[h][j].y));
+                    for (int h = 0; h < 2; ++h)
+                        sts128(slot + h * kFp8HalfM * 4, make_uint4(__float_as_uint(p[h][j].x), __float_as_uint(p[h][j].y), __float_as_uint(p[h][j].z), __float_as_uint(p[h][j].w)));
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar_dfull + 8 * (i & 1));
                     ++i;
@@ -457,7 +499,7 @@ fp8_tiles_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap x_map, con
                                 f[j].x += e.x, f[j].y += e.y;
                             }
                         };
-                        if (a.bias != nullptr && col + 8 * c < a.N) add(__ldg(reinterpret_cast<const uint4 *>(a.bias + col + 8 * c)));      // (N % 8 == 0)
+                        if (a.bias != nullptr && col + 8 * c < a.N) add(ldg_behind(a.bias + col + 8 * c));      // (N % 8 == 0)
                         if (a.has_in) add(lds128(piece(h, c)));
                         sts128(piece(h, c), make_uint4(pack_out16<BF>(f[0]), pack_out16<BF>(f[1]), pack_out16<BF>(f[2]), pack_out16<BF>(f[3])));
                     }
@@ -510,6 +552,7 @@ fp8_tiles_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap x_map, con
 #pragma unroll
                     for (int o = 0; o < kOuts; ++o) {
                         const float s = fp8_scale(top[o]);
+                        const Fp8Quotient by(s);
                         if (cols == 0 && row < a.M && ok) a.out_scales[(size_t)row * kOuts * FB + o * FB + tn] = s;
                         // 64-byte rows, 64-byte swizzle
 #pragma unroll
@@ -518,7 +561,7 @@ fp8_tiles_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap x_map, con
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
                                 const float2 f0 = unpack2(acc[o][8 * c + 2 * j]), f1 = unpack2(acc[o][8 * c + 2 * j + 1]);
-                                w[j] = fp8_four(__fdiv_rn(f0.x, s), __fdiv_rn(f0.y, s), __fdiv_rn(f1.x, s), __fdiv_rn(f1.y, s));
+                                w[j] = fp8_four(by(f0.x), by(f0.y), by(f1.x), by(f1.y));
                             }
                             sts128(stage + o * kFp8OutBytes + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
                         }
