@@ -28,17 +28,19 @@ __device__ __forceinline__ float fp8_scale(uint32_t top)
 // 1 / s and q = v y, the remainder v - q s is exact and q + (v - q s) y rounds to the nearest quotient.  Small blocks are scaled first, so that the
 // remainder does not underflow.  (The operator's own division leaves its fast way for zeros: padding rows made a gated call of 1000 rows 26 us instead of 17.)
 struct Fp8Quotient {
-    float f, s, y;
+    float s, y;
+    bool small;
     __device__ __forceinline__ explicit Fp8Quotient(float scale)
     {
-        f = scale < 0x1p-60f ? 0x1p64f : 1.0f;
-        s = scale * f;
+        small = scale < 0x1p-60f;
+        s = small ? scale * 0x1p64f : scale;
         y = __frcp_rn(s);
     }
     __device__ __forceinline__ float operator()(float v) const
     {
-        const float a = v * f, q = a * y;
-        return fmaf(fmaf(-q, s, a), y, q);
+        if (small) v *= 0x1p64f;
+        const float q = v * y;
+        return fmaf(fmaf(-q, s, v), y, q);
     }
 };
 // two numbers to e4m3, nearest even; a in the low byte; NaN becomes NaN, what rounds beyond 448 becomes 448
@@ -70,53 +72,55 @@ __device__ __forceinline__ float ldgf_behind(const float *p)
     asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(p));
     return v;
 }
-// Half a warp per block of 128: 16 bytes of x and 8 of the result per lane.  kFp8QuantUnroll blocks per half warp are requested
-// together.
-constexpr int kFp8QuantThreads = 256, kFp8QuantUnroll = 4;
+// Eight lanes per block of 128: a lane has numbers 8 l .. 8 l + 7 and 64 + 8 l .., two loads of 16 bytes.  Bound by instruction issue and by
+// memory alike: with sixteen lanes per block, maxima of fp32 bits and the operator's own division 4096 x 11008 took 46 us, as it is 24.8 (floor 21);
+// more blocks of a group requested together made it slower (two 26.1, four 30.7; 300 x 4096 2.3, 3.4 and 4.6).
+constexpr int kFp8QuantThreads = 256, kFp8QuantLanes = 8, kFp8QuantCtasPerSm = 16;
 template <bool BF>
 __global__ void __launch_bounds__(kFp8QuantThreads) fp8_quantize_kernel(const uint4 *x, uint2 *q, float *scales, int K, int KB, long long blocks)
 {
     pdl_launch_dependents();
     pdl_wait();
-    const int lane16 = threadIdx.x & 15;
-    // half warp h has blocks h, h + halves, ... (rows after rows); the step as rows and blocks, so that only the first takes a division
-    const long long halves = (long long)gridDim.x * (kFp8QuantThreads / 16), step_row = halves / KB;
-    const int step_kb = (int)(halves - step_row * KB);
-    long long b0 = (long long)blockIdx.x * (kFp8QuantThreads / 16) + threadIdx.x / 16, row = b0 / KB;
-    int kb = (int)(b0 - row * KB);
-    // (a warp's two half warps go on together: the maximum is found by the whole warp)
-    for (; b0 - (threadIdx.x >> 4 & 1) < blocks; b0 += halves * kFp8QuantUnroll) {
-        uint4 v[kFp8QuantUnroll];
-        size_t at[kFp8QuantUnroll];
-        bool in[kFp8QuantUnroll];
+    constexpr int kPer = kFp8QuantThreads / kFp8QuantLanes, kInWarp = 32 / kFp8QuantLanes;
+    const int l = threadIdx.x % kFp8QuantLanes;
+    // group h of eight lanes has blocks h, h + groups, ... (row after row); the step as rows and blocks: only the first takes a division
+    const long long groups = (long long)gridDim.x * kPer, step_row = groups / KB;
+    const int step_kb = (int)(groups - step_row * KB);
+    long long b = (long long)blockIdx.x * kPer + threadIdx.x / kFp8QuantLanes, row = b / KB;
+    int kb = (int)(b - row * KB);
+    // (a warp's groups go on together: the maximum is found by the whole warp)
+    for (; b - threadIdx.x / kFp8QuantLanes % kInWarp < blocks; b += groups) {
+        const int k = kb * kFp8Block + l * 8;
+        const size_t at = ((size_t)row * K + k) / 8;
+        uint32_t w[8], top = 0;
+        bool in[2];
 #pragma unroll
-        for (int i = 0; i < kFp8QuantUnroll; ++i) {
-            const int k = kb * kFp8Block + lane16 * 8;
-            in[i] = b0 + i * halves < blocks && k < K;
-            at[i] = ((size_t)row * K + k) / 8;
-            v[i] = in[i] ? ldg_behind(x + at[i]) : make_uint4(0, 0, 0, 0);
-            row += step_row, kb += step_kb;
-            if (kb >= KB) kb -= KB, ++row;
+        for (int h = 0; h < 2; ++h) {
+            in[h] = b < blocks && k + 64 * h < K;
+            const uint4 v = in[h] ? ldg_behind(x + at + 8 * h) : make_uint4(0, 0, 0, 0);
+            w[4 * h] = v.x, w[4 * h + 1] = v.y, w[4 * h + 2] = v.z, w[4 * h + 3] = v.w;
         }
+        // 16-bit numbers without their signs are ordered as integers, NaN above all
 #pragma unroll
-        for (int i = 0; i < kFp8QuantUnroll; ++i) {
-            const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+        for (int j = 0; j < 8; ++j) top = __vmaxu2(top, w[j] & 0x7fff7fffu);
+#pragma unroll
+        for (int o = kFp8QuantLanes / 2; o; o >>= 1) top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const float2 tops = pair_to_float2<BF>(top);
+        const float s = fp8_scale(max(__float_as_uint(tops.x), __float_as_uint(tops.y)));
+        const Fp8Quotient by(s);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
             float2 f[4];
-            uint32_t top = 0;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                f[j] = pair_to_float2<BF>(w[j]);
-                top = max(top, max(abs_bits(f[j].x), abs_bits(f[j].y)));
+                f[j] = pair_to_float2<BF>(w[4 * h + j]);
+                f[j] = make_float2(by(f[j].x), by(f[j].y));
             }
-#pragma unroll
-            for (int o = 8; o; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-            const float s = fp8_scale(top);
-            const Fp8Quotient by(s);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) f[j] = make_float2(by(f[j].x), by(f[j].y));
-            if (in[i]) q[at[i]] = make_uint2(fp8_four(f[0].x, f[0].y, f[1].x, f[1].y), fp8_four(f[2].x, f[2].y, f[3].x, f[3].y));
-            if (lane16 == 0 && b0 + i * halves < blocks) scales[b0 + i * halves] = s;
+            if (in[h]) q[at + 8 * h] = make_uint2(fp8_four(f[0].x, f[0].y, f[1].x, f[1].y), fp8_four(f[2].x, f[2].y, f[3].x, f[3].y));
         }
+        if (l == 0 && b < blocks) scales[b] = s;
+        row += step_row, kb += step_kb;
+        if (kb >= KB) kb -= KB, ++row;
     }
 }
 
@@ -437,23 +441,27 @@ fp8_tiles_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap x_map, con
             const bool live = row0 < a.M;
             // first column of this warp's 64 of half h, in y or (gated kinds) among the F columns of the result
             auto out_col = [&](int h) { return KIND == kFp8Plain ? tn * kFp8TileN + h * 128 + cols : tn * kFp8Block + cols; };
-            if (live && elect_one()) {
-                tma_store_wait_read();      // the last tile's results have left the stages
-                if (KIND == kFp8Backward || (KIND == kFp8Plain && a.has_in))
+            // the input, requested some blocks into the tile: the last tile's results have left the stages by then
+            auto request = [&]() {
+                if (live && elect_one()) {
+                    tma_store_wait_read();
 #pragma unroll
                     for (int h = 0; h < (KIND == kFp8Plain ? 2 : 1); ++h)
                         if (KIND != kFp8Plain || out_col(h) < a.N) {
                             mbar_arrive_expect_tx(my_in + 8 * h, kFp8OutBytes);
                             tma_load_2d(stage + h * kFp8OutBytes, &in_map, out_col(h), row0, my_in + 8 * h);
                         }
-            }
-            __syncwarp();
+                }
+                __syncwarp();
+            };
+            const int request_at = KIND == kFp8Backward || (KIND == kFp8Plain && a.has_in) ? min(4, KB - 1) : -1;
             uint64_t acc[2][32];
 #pragma unroll
             for (int j = 0; j < 64; ++j) acc[j / 32][j % 32] = 0;
             for (int kb = 0; kb < KB; ++kb) {
                 const uint32_t from = lanes + 32 * at + cols;
-                if (ok) ok = mbar_wait_warp_inline(bar_dfull + at, parity);
+                if (kb == request_at) request();
+                if (!mbar_wait_warp_inline(bar_dfull + at, parity)) ok = false;
                 tc_fence_after_sync();
                 if (live) {
                     uint32_t v[2][16];
@@ -476,6 +484,10 @@ fp8_tiles_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap x_map, con
                 slot = (slot + kFp8ScaleBytes) & (kFp8ScaleSlots * kFp8ScaleBytes - 1);
             }
             if (!live) continue;
+            if (request_at < 0) {
+                if (elect_one()) tma_store_wait_read();
+                __syncwarp();
+            }
 
             // row `lane` of a stage, 16-byte piece c: 128-byte rows, 128-byte swizzle (the tensor maps')
             auto piece = [&](int h, int c) { return stage + h * kFp8OutBytes + lane * 128 + ((c ^ (lane & 7)) << 4); };
@@ -623,8 +635,9 @@ inline int launch_fp8_quantize(const void *x, void *q, float *scales, int M, int
 {
     int KB = fp8_blocks(K);
     long long blocks = (long long)M * KB;
-    const long long per_cta = kFp8QuantThreads / 16, want = (blocks + per_cta - 1) / per_cta;
-    const int grid = (int)(want < 8ll * sms ? want : 8ll * sms);
+    const long long per_cta = kFp8QuantThreads / kFp8QuantLanes, want = (blocks + per_cta - 1) / per_cta;
+    const long long most = (long long)kFp8QuantCtasPerSm * sms;
+    const int grid = (int)(want < most ? want : most);
     const uint4 *xp = (const uint4 *)x;
     uint2 *qp = (uint2 *)q;
     void *args[] = {&xp, &qp, &scales, &K, &KB, &blocks};
