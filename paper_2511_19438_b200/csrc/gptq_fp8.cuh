@@ -159,6 +159,10 @@ __global__ void __launch_bounds__(256) fp8_transpose_kernel(const uint8_t *w, co
 //   warp 1  the MMAs (the leader's)
 //   warp 2  products of scales, two blocks ahead: 128 rows x 2 weight blocks per block of K into a ring of four
 //   warps 4 to 11 drain.  The first four give registers to them: 128 sums and 32 columns on their way.
+// What bounds it, by stamps of %clock: two accumulators, so that two blocks of K take an MMA (512 clocks), a drain (720) and both ways between the
+// MMA thread and the drain warps of two SMs (800): 1000 clocks per block; and the power limit (1.5 to 1.7 GHz in that loop).  4096 x 4096 x 12288: 211 us,
+// 1.95 PFLOP/s.  Tried and slower: accumulators of half a tile, four of them (304 us: the MMAs read their rows twice, and the drain warps wait twice as
+// often), 16 drain warps (304: instruction issue), one CTA per tile of 128 x 256 (356; gated kinds the same), results sent during the next tile (255).
 constexpr int kFp8TileM = 256, kFp8TileN = 256, kFp8HalfM = 128, kFp8Stages = 4;
 constexpr int kFp8FirstDrain = 4, kFp8DrainWarps = 8, kFp8Threads = 32 * (kFp8FirstDrain + kFp8DrainWarps);
 constexpr int kFp8LaunchRegs = 168, kFp8FewRegs = 72, kFp8ManyRegs = 216;
@@ -177,7 +181,6 @@ struct Fp8Args {
     float *out_scales;                     // gated kinds: the result is e4m3 with these scales; nullptr: 16 bits
     int M, N, K, KB;                       // gated kinds: N = 2 F
     int tiles_m, tiles_n;
-    int has_in;                            // a residual, or the gradient of the result
 };
 
 __device__ __forceinline__ void umma_f8_ss_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
@@ -206,21 +209,22 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t sr
 __device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 __device__ __forceinline__ void tma_store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 // A converged warp's wait in few instructions and without a call: what is live in the drain warps fills the registers, and a call
-// would have it stored.
-__device__ __forceinline__ bool mbar_wait_warp_inline(uint32_t bar, uint32_t parity)
+// would have it stored.  `more`: false once a wait has given up; then one try, so that all of a launch's waits together stay short.
+__device__ __forceinline__ bool mbar_wait_warp_inline(uint32_t bar, uint32_t parity, bool more = true)
 {
     uint64_t start = 0;
     for (;;) {
         uint32_t done;
         asm volatile(
-            "{\n\t.reg .pred p, more;\n\t.reg .u32 n;\n\tmov.u32 n, 0;\n"
+            "{\n\t.reg .pred p, again;\n\t.reg .u32 n;\n\tmov.u32 n, %3;\n"
             "TRY:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t@p bra.uni END;\n\t"
-            "add.u32 n, n, 1;\n\tsetp.lt.u32 more, n, 4096;\n\t@more bra.uni TRY;\n"
+            "sub.u32 n, n, 1;\n\tsetp.ne.u32 again, n, 0;\n\t@again bra.uni TRY;\n"
             "END:\n\tselp.u32 %0, 1, 0, p;\n\t}"
             : "=r"(done)
-            : "r"(bar), "r"(parity)
+            : "r"(bar), "r"(parity), "r"(more ? 4096 : 1)
             : "memory");
         if (__any_sync(0xffffffffu, done)) return true;
+        if (!more) return false;
         const uint64_t now = global_timer_ns();
         if (start == 0) start = now;
         if (__any_sync(0xffffffffu, now - start > kWaitLimitNs)) break;
@@ -268,7 +272,8 @@ __device__ __forceinline__ void fp8_tile(int t, int tiles_m, int tiles_n, int &t
     tn = in / rows;
 }
 
-template <int KIND, bool BF, bool OUT8>
+// IN: plain products have a residual (gated: nothing, backward: the gradient of the result in its place)
+template <int KIND, bool BF, bool OUT8, bool IN>
 __global__ void __launch_bounds__(kFp8Threads, 1)
 fp8_tiles_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map,
                  const __grid_constant__ CUtensorMap in_map, const __grid_constant__ CUtensorMap out_map)
@@ -454,14 +459,14 @@ fp8_tiles_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap x_map, con
                 }
                 __syncwarp();
             };
-            const int request_at = KIND == kFp8Backward || (KIND == kFp8Plain && a.has_in) ? min(4, KB - 1) : -1;
+            const int request_at = IN ? min(4, KB - 1) : -1;
             uint64_t acc[2][32];
 #pragma unroll
             for (int j = 0; j < 64; ++j) acc[j / 32][j % 32] = 0;
             for (int kb = 0; kb < KB; ++kb) {
                 const uint32_t from = lanes + 32 * at + cols;
-                if (kb == request_at) request();
-                if (!mbar_wait_warp_inline(bar_dfull + at, parity)) ok = false;
+                if (IN && kb == request_at) request();
+                if (!mbar_wait_warp_inline(bar_dfull + at, parity, ok)) ok = false;
                 tc_fence_after_sync();
                 if (live) {
                     uint32_t v[2][16];
@@ -484,7 +489,7 @@ fp8_tiles_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap x_map, con
                 slot = (slot + kFp8ScaleBytes) & (kFp8ScaleSlots * kFp8ScaleBytes - 1);
             }
             if (!live) continue;
-            if (request_at < 0) {
+            if (!IN) {
                 if (elect_one()) tma_store_wait_read();
                 __syncwarp();
             }
@@ -496,8 +501,8 @@ fp8_tiles_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap x_map, con
                 for (int h = 0; h < 2; ++h) {
                     const int col = out_col(h);
                     if (col >= a.N) break;
-                    if (a.has_in && ok) ok = mbar_wait_warp_inline(my_in + 8 * h, (uint32_t)ins >> h & 1);
-                    if (a.has_in) ins ^= 1 << h;
+                    if (IN && ok) ok = mbar_wait_warp_inline(my_in + 8 * h, (uint32_t)ins >> h & 1);
+                    if (IN) ins ^= 1 << h;
 #pragma unroll
                     for (int c = 0; c < 8; ++c) {
                         float2 f[4];
@@ -512,7 +517,7 @@ fp8_tiles_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap x_map, con
                             }
                         };
                         if (a.bias != nullptr && col + 8 * c < a.N) add(ldg_behind(a.bias + col + 8 * c));      // (N % 8 == 0)
-                        if (a.has_in) add(lds128(piece(h, c)));
+                        if (IN) add(lds128(piece(h, c)));
                         sts128(piece(h, c), make_uint4(pack_out16<BF>(f[0]), pack_out16<BF>(f[1]), pack_out16<BF>(f[2]), pack_out16<BF>(f[3])));
                     }
                     fence_proxy_async();
@@ -664,12 +669,12 @@ struct Fp8Call {
     int M, N, K, bf16, sms;
 };
 
-template <int KIND, bool BF, bool OUT8>
+template <int KIND, bool BF, bool OUT8, bool IN = KIND == kFp8Backward>
 int launch_fp8_tiles(const Fp8Call &c, cudaStream_t s)
 {
     static int configured[64];
     static std::atomic<int> registers{0};
-    auto kernel = fp8_tiles_kernel<KIND, BF, OUT8>;
+    auto kernel = fp8_tiles_kernel<KIND, BF, OUT8, IN>;
     int st = ensure_dynamic_smem((const void *)kernel, configured, kFp8SmemBytes);
     if (st) return st;
     if (registers.load() == 0) {      // the warps that take registers would wait for ever for what the launch did not bring
@@ -685,7 +690,6 @@ int launch_fp8_tiles(const Fp8Call &c, cudaStream_t s)
     a.M = c.M, a.N = c.N, a.K = c.K, a.KB = fp8_blocks(c.K);
     a.tiles_m = (c.M - 1) / kFp8TileM + 1;
     a.tiles_n = KIND == kFp8Plain ? (c.N - 1) / kFp8TileN + 1 : F / kFp8Block;
-    a.has_in = c.in != nullptr;
     const long long tiles = (long long)a.tiles_m * a.tiles_n;
     if (tiles > 0x3fffffffll) return GPTQ_ERR_UNSUPPORTED;
     CUtensorMap xm, wm, im, om;
@@ -712,8 +716,8 @@ inline int launch_fp8(const Fp8Call &c, cudaStream_t s)
 {
     const bool out8 = c.out_scales != nullptr;
     switch (c.kind * 4 + (out8 ? 2 : 0) + (c.bf16 ? 1 : 0)) {
-    case 0: return launch_fp8_tiles<kFp8Plain, false, false>(c, s);
-    case 1: return launch_fp8_tiles<kFp8Plain, true, false>(c, s);
+    case 0: return c.in ? launch_fp8_tiles<kFp8Plain, false, false, true>(c, s) : launch_fp8_tiles<kFp8Plain, false, false>(c, s);
+    case 1: return c.in ? launch_fp8_tiles<kFp8Plain, true, false, true>(c, s) : launch_fp8_tiles<kFp8Plain, true, false>(c, s);
     case 4: return launch_fp8_tiles<kFp8Gated, false, false>(c, s);
     case 5: return launch_fp8_tiles<kFp8Gated, true, false>(c, s);
     case 6: case 7: return launch_fp8_tiles<kFp8Gated, false, true>(c, s);      // (the type of the result is not the type of anything else)

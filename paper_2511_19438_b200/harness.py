@@ -353,10 +353,12 @@ def _format_of(dtype: torch.dtype) -> int:
     return B.GPTQ_FORMAT_BF16 if dtype == torch.bfloat16 else 0
 
 
-def _expect_rows(x: torch.Tensor, x_scales: torch.Tensor | None, dtype: torch.dtype, K: int) -> int:
+def _expect_rows(x: torch.Tensor, x_scales: torch.Tensor | None, dtype: torch.dtype, D: DeviceFp8Linear) -> int:
     M = x.shape[0]
-    _expect("x", x, dtype if x_scales is None else torch.float8_e4m3fn, (M, K))
-    _expect("x_scales", x_scales, torch.float32, (M, _blocks(K)))
+    if x.device != D.weight.device:
+        raise ValueError(f"x on {x.device}, the layer on {D.weight.device}")
+    _expect("x", x, dtype if x_scales is None else torch.float8_e4m3fn, (M, D.K))
+    _expect("x_scales", x_scales, torch.float32, (M, _blocks(D.K)))
     return M
 
 
@@ -380,7 +382,7 @@ def gemm_fp8(x: torch.Tensor, D: DeviceFp8Linear, bias: torch.Tensor | None = No
     ``dtype`` of the result."""
     dtype = x.dtype if x_scales is None else dtype or torch.float16
     fmt = _format_of(dtype)
-    M = _expect_rows(x, x_scales, dtype, D.K)
+    M = _expect_rows(x, x_scales, dtype, D)
     if y is None:
         y = torch.empty((M, D.N), dtype=dtype, device=x.device)
     _expect("bias", bias, dtype, (D.N,))
@@ -396,7 +398,7 @@ def gemm_fp8_silu_mul(x: torch.Tensor, D: DeviceFp8Linear, x_scales: torch.Tenso
     its scales."""
     dtype = x.dtype if x_scales is None else dtype or torch.float16
     fmt = _format_of(dtype)
-    M, F = _expect_rows(x, x_scales, dtype, D.K), D.N // 2
+    M, F = _expect_rows(x, x_scales, dtype, D), D.N // 2
     out, s = _rows_fp8(M, F, x.device) if quantized else (torch.empty((M, F), dtype=dtype, device=x.device), None)
     B.check(B.gptq_gemm_fp8_silu_mul(x, x_scales, D.weight, D.scales, out, s, M, F, D.K, fmt, stream), "gptq_gemm_fp8_silu_mul")
     return (out, s) if quantized else out
@@ -406,7 +408,7 @@ def gemm_fp8_silu_mul_backward(x: torch.Tensor, D: DeviceFp8Linear, d_out: torch
                                quantized: bool = True, stream=None):
     """The gradients [M, N] of gate's and up's columns through gptq_gemm_fp8_silu_mul_backward: e4m3 and scales, or 16-bit."""
     fmt = _format_of(d_out.dtype)
-    M, F = _expect_rows(x, x_scales, d_out.dtype, D.K), D.N // 2
+    M, F = _expect_rows(x, x_scales, d_out.dtype, D), D.N // 2
     _expect("d_out", d_out, d_out.dtype, (M, F))
     out, s = _rows_fp8(M, D.N, x.device) if quantized else (torch.empty((M, D.N), dtype=d_out.dtype, device=x.device), None)
     B.check(B.gptq_gemm_fp8_silu_mul_backward(x, x_scales, D.weight, D.scales, d_out, out, s, M, F, D.K, fmt, stream),
