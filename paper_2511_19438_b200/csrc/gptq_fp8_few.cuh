@@ -424,16 +424,16 @@ inline Fp8FewPlan plan_fp8_few(int kind, int M, int N, int K, int sms)
 }
 
 // Up to a tile of token rows the layer is read once here and the pairs of gptq_fp8.cuh would leave most SMs idle: always this kernel.
-// Beyond, the shorter of what both take (ns, fitted to calls of 128 to 1000 rows of K = 512 to 11008; us, this kernel / pairs: 256 rows 4096 x 4096
-// 11.8 / 21.9, 512 rows 17.3 / 22.1, 768 rows 33.9 / 22.9; 256 rows 4096 x 12288 34.1 / 23.4, 384 rows 35.8 / 41.5; gated, 256 rows 4096 x 2048
-// 14.6 / 24.0, 4096 x 11008 72 / 46.7).
+// Beyond, the shorter of what both take: ns, fitted to calls of 128 to 1000 rows of K = 512 to 11008 (us, this kernel / pairs, whose wave of tiles takes the
+// same however few there are: 4096 x 4096 256 rows 11.8 / 20.3, 512 rows 17.3 / 20.3, 768 rows 33.9 / 20.3; 4096 x 12288 384 rows 35.8 to 37.8 / 36.9; gated 4096 x 2048
+// 512 rows 22.3 / 24.2, 4096 x 11008 128 rows 47.3 / 42.8).
 inline bool fp8_few_is_shorter(int kind, int M, int N, int K, int sms, const Fp8FewPlan &p)
 {
     if (M <= few_most_rows(kind)) return true;
     const long long tiles = ((long long)(M - 1) / kFp8TileM + 1) * ((N - 1) / kFp8TileN + 1), pairs = sms / 2;
     const long long waves = (tiles + pairs - 1) / pairs, KB = fp8_blocks(K);
     const bool plain = kind == kFp8Plain;
-    return p.waves * (4000 + (plain ? 410ll : 590ll) * p.blocks) < (plain ? 4500 : 6000) + waves * KB * (plain ? 545 : 620);
+    return p.waves * (4000 + (plain ? 410ll : 590ll) * p.blocks) < (plain ? 4500 : 6000) + waves * KB * (plain ? 495 : 575);
 }
 
 template <int KIND, bool BF, bool OUT8, int TT, bool XQ = false>
