@@ -209,21 +209,15 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t sr
 __device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 __device__ __forceinline__ void tma_store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 // A converged warp's wait in few instructions and without a call: what is live in the drain warps fills the registers, and a call
-// would have it stored.  `more`: false once a wait has given up; then one try, so that all of a launch's waits together stay short.
+// would have it stored.  A lane's try is its own, limited in time: the warp goes on once every lane has seen the phase end.
+// `more`: false once a wait has given up; then one try, so that all of a launch's waits together stay short.
 __device__ __forceinline__ bool mbar_wait_warp_inline(uint32_t bar, uint32_t parity, bool more = true)
 {
     uint64_t start = 0;
     for (;;) {
-        uint32_t done;
-        asm volatile(
-            "{\n\t.reg .pred p, again;\n\t.reg .u32 n;\n\tmov.u32 n, %3;\n"
-            "TRY:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t@p bra.uni END;\n\t"
-            "sub.u32 n, n, 1;\n\tsetp.ne.u32 again, n, 0;\n\t@again bra.uni TRY;\n"
-            "END:\n\tselp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(done)
-            : "r"(bar), "r"(parity), "r"(more ? 4096 : 1)
-            : "memory");
-        if (__any_sync(0xffffffffu, done)) return true;
+#pragma unroll 1
+        for (int n = more ? 4096 : 1; n; --n)
+            if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
         if (!more) return false;
         const uint64_t now = global_timer_ns();
         if (start == 0) start = now;
