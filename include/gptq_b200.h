@@ -507,7 +507,8 @@ typedef struct {
                          2 = tcgen05 kernel (gptq_gemm, M >= 17),
                          3 = stream-K mma.sync kernel (gptq_gemm_noalloc),
                          4 = streaming tcgen05 decode kernel (gptq_gemm, M <= 2, see gptq_plan_decode),
-                         5 = persistent tcgen05 kernel (gptq_gemm, M >= 17, see gptq_plan_prefill) */
+                         5 = persistent tcgen05 kernel (gptq_gemm, M >= 17, see gptq_plan_prefill),
+                         6 = e4m3 kernel with the weights on the MMA's rows, 7 = e4m3 kernel on CTA pairs (see gptq_plan_fp8) */
     int m_tile;       /* tokens per CTA tile */
     int m_chunks;     /* launches along M */
     int stages;       /* pipeline depth */
@@ -536,6 +537,10 @@ int gptq_plan_decode(int M, int N, int K, int group_size, int act_order, int sm_
 int gptq_plan_prefill(int M, int N, int K, int group_size, int act_order, int eight_bit, int sm_count, gptq_plan_t *out);
 /* The same for gptq_gemm_noalloc (stream-K kernel; workspace_bytes is its need of the built-in scratch). */
 int gptq_plan_noalloc(int M, int N, int K, int group_size, int act_order, int sm_count, gptq_plan_t *out);
+
+/* The same for gptq_gemm_fp8 (gated = 0) or, with N = 2 F, for gptq_gemm_fp8_silu_mul and its backward pass (gated != 0).  `cluster_size` = CTAs
+ * that share the K range of a tile (kernel 6) or a tile (kernel 7), `items` = (tile, block of K); `workspace_bytes` = the need of 16-bit x. */
+int gptq_plan_fp8(int M, int N, int K, int gated, int sm_count, gptq_plan_t *out);
 
 /* For tests only (not needed to use the library): the stream-K partition gptq_gemm_noalloc's kernel uses, from
  * the same arithmetic as the kernel.  CTA `cta` of `ctas` works

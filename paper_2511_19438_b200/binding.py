@@ -113,6 +113,7 @@ _SIGNATURES = {
     "gptq_plan": (_i, [_i, _i, _i, _i, _i, _i, ctypes.POINTER(gptq_plan_t)]),
     "gptq_plan_decode": (_i, [_i, _i, _i, _i, _i, _i, ctypes.POINTER(gptq_plan_t)]),
     "gptq_plan_prefill": (_i, [_i, _i, _i, _i, _i, _i, _i, ctypes.POINTER(gptq_plan_t)]),
+    "gptq_plan_fp8": (_i, [_i, _i, _i, _i, _i, ctypes.POINTER(gptq_plan_t)]),
     "gptq_plan_noalloc": (_i, [_i, _i, _i, _i, _i, _i, ctypes.POINTER(gptq_plan_t)]),
     "gptq_plan_cta_range": (_i, [_i, _i, _i, ctypes.POINTER(_i), ctypes.POINTER(_i)]),
     "gptq_plan_panel_owners": (_i, [_i, _i, _i, _i, ctypes.POINTER(_i), ctypes.POINTER(_i)]),
@@ -461,6 +462,13 @@ def gptq_plan_decode(M, N, K, group_size, act_order, sm_count):
 def gptq_plan_prefill(M, N, K, group_size, act_order, eight_bit, sm_count):
     plan = gptq_plan_t()
     st = _lib.gptq_plan_prefill(M, N, K, group_size, int(act_order), int(eight_bit), sm_count, ctypes.byref(plan))
+    return st, plan
+
+
+def gptq_plan_fp8(M, N, K, gated, sm_count):
+    """Returns (status, gptq_plan_t) of the e4m3 products; gated: N = 2 F.  Host-only."""
+    plan = gptq_plan_t()
+    st = _lib.gptq_plan_fp8(M, N, K, int(gated), sm_count, ctypes.byref(plan))
     return st, plan
 
 

@@ -1405,6 +1405,34 @@ int gptq_fp8_transpose(const void *weight, const float *weight_scales, void *wei
     return launch_fp8_transpose(weight, weight_scales, weight_out, scales_out, N, K, (cudaStream_t)stream);
 }
 
+int gptq_plan_fp8(int M, int N, int K, int gated, int sm_count, gptq_plan_t *out)
+{
+    if (!out) return GPTQ_ERR_NULL;
+    int st = check_fp8(M, N, K, 0);
+    if (st) return st;
+    if (sm_count < 1 || (gated && N % (2 * kFp8Block))) return GPTQ_ERR_SHAPE;
+    const int kind = gated ? kFp8Gated : kFp8Plain;
+    const Fp8FewPlan p = plan_fp8_few(kind, M, N, K, sm_count);
+    const bool few = fp8_few_is_shorter(kind, M, N, K, sm_count, p);
+    const int rows = few_instance(p.tok);
+    out->kernel = few ? 6 : 7;
+    out->m_tile = few ? p.tok : kFp8TileM;
+    out->m_chunks = 1;
+    out->stages = few ? few_stages(kind, rows) : kFp8Stages;
+    const long long tiles = few ? (long long)p.tiles_m * p.tiles_n : fp8_tiles(kind, M, N);
+    const long long ctas = few ? tiles << p.log_S : 2 * (tiles < sm_count / 2 ? tiles : sm_count / 2), items = tiles * fp8_blocks(K);
+    out->ctas = (int)(ctas < 0x7fffffff ? ctas : 0x7fffffff);
+    out->items = (int)(items < 0x7fffffff ? items : 0x7fffffff);
+    out->split_panels = few && p.log_S ? p.tiles_n : 0;
+    out->smem_bytes = few ? few_smem(kind, rows) : kFp8SmemBytes;
+    out->workspace_bytes = fp8_workspace_need(M, K);
+    out->cluster_size = few ? 1 << p.log_S : 2;
+    out->tail_ctas = 0;
+    out->tail_cluster_size = 1;
+    set_kernel_name(out, few ? "fp8_few_kernel<%d,%d>" : "fp8_tiles_kernel<%d>", kind, rows);
+    return GPTQ_OK;
+}
+
 size_t gptq_fp8_workspace_bytes(int M, int K)
 {
     if (check_fp8(M, 8, K, 0) != GPTQ_OK) return 0;

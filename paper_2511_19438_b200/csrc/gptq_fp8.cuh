@@ -663,6 +663,11 @@ struct Fp8Call {
     int M, N, K, bf16, sms;
 };
 
+inline long long fp8_tiles(int kind, int M, int N)
+{
+    return ((long long)(M - 1) / kFp8TileM + 1) * (kind == kFp8Plain ? (N - 1) / kFp8TileN + 1 : N / 2 / kFp8Block);
+}
+
 template <int KIND, bool BF, bool OUT8, bool IN = KIND == kFp8Backward>
 int launch_fp8_tiles(const Fp8Call &c, cudaStream_t s)
 {
@@ -684,7 +689,7 @@ int launch_fp8_tiles(const Fp8Call &c, cudaStream_t s)
     a.M = c.M, a.N = c.N, a.K = c.K, a.KB = fp8_blocks(c.K);
     a.tiles_m = (c.M - 1) / kFp8TileM + 1;
     a.tiles_n = KIND == kFp8Plain ? (c.N - 1) / kFp8TileN + 1 : F / kFp8Block;
-    const long long tiles = (long long)a.tiles_m * a.tiles_n;
+    const long long tiles = fp8_tiles(KIND, c.M, c.N);
     if (tiles > 0x3fffffffll) return GPTQ_ERR_UNSUPPORTED;
     CUtensorMap xm, wm, im, om;
     const auto u8 = CU_TENSOR_MAP_DATA_TYPE_UINT8;

@@ -401,6 +401,9 @@ fp8_few_kernel(const Fp8FewArgs a, const __grid_constant__ CUtensorMap x_map, co
     }
 }
 
+// the instance that takes tiles of `tok` token rows
+__host__ __device__ constexpr int few_instance(int tok) { return tok <= 16 ? 16 : tok <= 32 ? 32 : tok <= 64 ? 64 : 128; }
+
 struct Fp8FewPlan {
     int tok, tiles_m, tiles_n, log_S;
     int waves, blocks;      // of CTAs; blocks of K of each CTA, at most
@@ -412,8 +415,7 @@ inline Fp8FewPlan plan_fp8_few(int kind, int M, int N, int K, int sms)
     p.tiles_m = (M - 1) / few_most_rows(kind) + 1;
     p.tok = (((M - 1) / p.tiles_m + 1) + 15) / 16 * 16;
     p.tiles_n = kind == kFp8Plain ? (N - 1) / 128 + 1 : N / 256;
-    const int TT = p.tok <= 16 ? 16 : p.tok <= 32 ? 32 : p.tok <= 64 ? 64 : 128;
-    const long long room = (long long)sms * few_per_sm(kind, TT), tiles = (long long)p.tiles_m * p.tiles_n;
+    const long long room = (long long)sms * few_per_sm(kind, few_instance(p.tok)), tiles = (long long)p.tiles_m * p.tiles_n;
     const int KB = fp8_blocks(K);
     while (2 << p.log_S <= kFp8FewMaxSplit && KB >= 4 << p.log_S &&
            (tiles * (2 << p.log_S) <= sms || (tiles * (2 << p.log_S) <= room && KB >= 16 << p.log_S)))
@@ -429,9 +431,8 @@ inline Fp8FewPlan plan_fp8_few(int kind, int M, int N, int K, int sms)
 // 512 rows 22.3 / 24.2, 4096 x 11008 128 rows 47.3 / 42.8).
 inline bool fp8_few_is_shorter(int kind, int M, int N, int K, int sms, const Fp8FewPlan &p)
 {
-    if (M <= few_most_rows(kind)) return true;
-    const long long tiles = ((long long)(M - 1) / kFp8TileM + 1) * ((N - 1) / kFp8TileN + 1), pairs = sms / 2;
-    const long long waves = (tiles + pairs - 1) / pairs, KB = fp8_blocks(K);
+    if (M <= few_most_rows(kind) || sms < 2) return true;
+    const long long pairs = sms / 2, waves = (fp8_tiles(kind, M, N) + pairs - 1) / pairs, KB = fp8_blocks(K);
     const bool plain = kind == kFp8Plain;
     return p.waves * (4000 + (plain ? 410ll : 590ll) * p.blocks) < (plain ? 4500 : 6000) + waves * KB * (plain ? 495 : 575);
 }

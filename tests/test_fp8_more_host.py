@@ -4,6 +4,9 @@ import re
 
 from paper_2511_19438_b200 import build as libbuild
 
+libbuild.build()
+from paper_2511_19438_b200 import binding as B  # noqa: E402
+
 
 def test_no_uniform_branch_on_a_lane_s_own_try():
     """mbarrier.try_wait answers each lane for itself: a branch that promises one answer for the warp (bra.uni) may not hang on it."""
@@ -11,3 +14,30 @@ def test_no_uniform_branch_on_a_lane_s_own_try():
         with open(os.path.join(libbuild.CSRC, f)) as h:
             for asm in re.findall(r"asm\s+volatile\s*\((.*?)\);", h.read(), re.S):
                 assert not ("try_wait" in asm and "bra.uni" in asm), f
+
+
+# ------------------------------------------------------------------------------------------------ which kernel takes a call
+PAIRS = [(1300, 4360, 656, 0), (1290, 3848, 1024, 0), (1100, 4104, 1040, 0), (4096, 12288, 4096, 0), (1300, 2 * 2048, 656, 1), (2100, 2 * 1408, 1040, 1),
+         (1300, 2 * 2048, 1024, 1), (65, 2 * 11008, 4096, 1)]
+FEW = [(1, 8, 16, 0), (128, 4096, 4096, 0), (300, 1000, 2064, 0), (512, 4096, 4096, 0), (1, 2 * 128, 16, 1), (64, 2 * 11008, 4096, 1), (512, 2 * 2048, 4096, 1)]
+
+
+def test_plan_says_which_kernel():
+    for shapes, kernel in ((FEW, 6), (PAIRS, 7)):
+        for M, N, K, gated in shapes:
+            st, p = B.gptq_plan_fp8(M, N, K, gated, 148)
+            assert st == B.GPTQ_OK and p.kernel == kernel, (M, N, K, gated, p.kernel)
+            assert 1 <= p.ctas and p.ctas % p.cluster_size == 0 and p.smem_bytes <= 227 * 1024
+            assert p.workspace_bytes == B.gptq_fp8_workspace_bytes(M, K)
+            tiles = -(-M // p.m_tile) * -(-N // (256 if gated or kernel == 7 else 128))
+            assert p.items == tiles * -(-K // 128)
+            assert p.ctas == tiles * p.cluster_size if kernel == 6 else p.ctas == min(148, 2 * tiles)
+
+
+def test_plan_refusals():
+    assert B._lib.gptq_plan_fp8(4, 256, 256, 0, 148, None) == B.GPTQ_ERR_NULL
+    for bad in ((0, 256, 256, 0, 148), (4, 4, 256, 0, 148), (4, 256, 24, 0, 148), (4, 256, 256, 0, 0), (4, 264, 256, 1, 148), (4, 128, 256, 1, 148)):
+        assert B.gptq_plan_fp8(*bad)[0] == B.GPTQ_ERR_SHAPE, bad
+    for M, N, K, gated in FEW + PAIRS:      # any number of SMs, one too
+        for sms in (1, 2, 3, 20, 1000):
+            assert B.gptq_plan_fp8(M, N, K, gated, sms)[0] == B.GPTQ_OK
