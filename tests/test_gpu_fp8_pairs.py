@@ -1,4 +1,4 @@
-"""GPU tests of the e4m3 products on CTA pairs (the kernel of long prompts).
+"""GPU tests of the e4m3 products on CTA pairs (the kernel of long prompts), and of what the fused epilogues round to.
 
 The sizes are ones that the rule gives to that kernel on 148 SMs; each test asks gptq_plan_fp8, so that a new rule cannot take them away
 unnoticed.  Plain implementations in 64 bits and the tolerances are those of test_gpu_fp8.
@@ -48,6 +48,21 @@ def test_gemm_bias_residual(ws, M, N, K, dtype):  # noqa: F811
             assert torch.equal(inplace, y)
 
 
+def check_nearest(q, s, want, e, least=0.7):
+    """The e4m3 results are the nearest numbers to result / scale, wherever an error of e and one rounding of the quotient cannot decide."""
+    per = s.double().repeat_interleave(128, 1)
+
+    def e4m3(v):
+        return (v / per).clamp(-448.0, 448.0).float().to(torch.float8_e4m3fn).double()
+
+    slack = e + 2 * F32 * want.abs()
+    low, high = e4m3(want - slack), e4m3(want + slack)
+    sure = low == high
+    assert torch.equal(q.double()[sure], low[sure])
+    assert sure.double().mean() >= least, sure.double().mean().item()
+    assert ((low <= q.double()) & (q.double() <= high)).all()
+
+
 GATED = [(1300, 4096, 16), (1300, 2048, 128), (1300, 2304, 528), (1300, 2048, 656), (2100, 1408, 1040), (1300, 2048, 1024), (65, 11008, 4096)]
 
 
@@ -65,6 +80,7 @@ def test_gated_and_backward(ws, M, F, K, dtype):  # noqa: F811
     assert torch.equal(H.gemm_fp8_silu_mul(q, D, x_scales=s, dtype=dtype), h)
     h8, hs = H.gemm_fp8_silu_mul(x, D, quantized=True)
     check_8(h8, hs, want.h, want.eh)
+    check_nearest(h8, hs, want.h, want.eh)
     dgu = H.gemm_fp8_silu_mul_backward(x, D, d, quantized=False)
     check_16(dgu[:, :F], want.dg, want.edg)
     check_16(dgu[:, F:], want.du, want.edu)
@@ -72,6 +88,20 @@ def test_gated_and_backward(ws, M, F, K, dtype):  # noqa: F811
     for part, cols, w, e in (("gate", slice(0, F), want.dg, want.edg), ("up", slice(F, 2 * F), want.du, want.edu)):
         sc = ds[:, cols.start // 128:cols.stop // 128]
         check_8(d8[:, cols], sc, w, e)
+        check_nearest(d8[:, cols], sc, w, e)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("M,F,K", T.GATED)
+def test_few_rows_round_to_the_nearest(ws, M, F, K, dtype):  # noqa: F811
+    x, D = rows(M, K, dtype), layer(2 * F, K, "gated")
+    d = (0.01 * normal(gen("d", M, F), M, F)).to(dtype)
+    H.ensure_for_fp8(ws, M, K)
+    want = Block(spread(*quantize(x)), D, d)
+    check_nearest(*H.gemm_fp8_silu_mul(x, D, quantized=True), want.h, want.eh)
+    d8, ds = H.gemm_fp8_silu_mul_backward(x, D, d)
+    check_nearest(d8[:, :F], ds[:, :F // 128], want.dg, want.edg)
+    check_nearest(d8[:, F:], ds[:, F // 128:], want.du, want.edu)
 
 
 def test_results_behind_the_last_row_stay(ws):  # noqa: F811
