@@ -475,13 +475,18 @@ int gptq_gemm_host_batch_w8(const gptq_host_problem_t *problems, int count, void
 
 /* Synchronises `stream` and returns GPTQ_ERR_LAYOUT if a kernel since the last check met a layer whose tiling does
  * not fit the call (see GPTQ_FORMAT_GATE_UP), GPTQ_ERR_TIMEOUT if a kernel's bounded wait gave up (the flag is
- * cleared either way), GPTQ_ERR_CUDA on a runtime error, else OK. */
+ * cleared either way), GPTQ_ERR_CUDA on a runtime error, else OK.  After GPTQ_ERR_TIMEOUT results of that kernel are missing; the e4m3 products
+ * (gptq_gemm_fp8 and those after it) leave such elements of the result as they were, the others' may be wrong. */
 int gptq_check_status(void *stream);
 
 /* Self-test of that mechanism (no counterpart in the paper): launches one thread that waits, the way the matmul
  * kernels wait, on a barrier nothing will ever complete, gives up after limit_us microseconds (1 .. 1e6) and
  * returns normally; the next gptq_check_status then reports GPTQ_ERR_TIMEOUT.  Nothing faults or hangs. */
 int gptq_selftest_wait_timeout(unsigned int limit_us, void *stream);
+
+/* The same for CTAs that finish each other's sums (the e4m3 products of few rows): a cluster of `ctas` (1, 2, 4 or 8), of which CTA `who` (-1: none) waits
+ * for what nothing brings.  stored[i], device memory, is set to 1 by CTA i unless a wait of any of them gave up. */
+int gptq_selftest_give_up(int ctas, int who, unsigned int limit_us, int *stored, void *stream);
 
 /* ---- launch timeline (no counterpart in the paper: a tracing aid) ------------------------ */
 

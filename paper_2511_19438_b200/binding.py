@@ -108,6 +108,7 @@ _SIGNATURES = {
     "gptq_gemm_host_batch_w8": (_i, [ctypes.POINTER(gptq_host_problem_t), _i, _vp, ctypes.POINTER(_i)]),
     "gptq_check_status": (_i, [_vp]),
     "gptq_selftest_wait_timeout": (_i, [ctypes.c_uint, _vp]),
+    "gptq_selftest_give_up": (_i, [_i, _i, ctypes.c_uint, _vp, _vp]),
     "gptq_trace_reset": (_i, [_vp]),
     "gptq_trace_read": (_i, [_vp, _i, _vp]),
     "gptq_plan": (_i, [_i, _i, _i, _i, _i, _i, ctypes.POINTER(gptq_plan_t)]),
@@ -428,6 +429,10 @@ def gptq_check_status(stream=None) -> int:
 
 def gptq_selftest_wait_timeout(limit_us, stream=None) -> int:
     return _lib.gptq_selftest_wait_timeout(int(limit_us), _stream(stream))
+
+
+def gptq_selftest_give_up(ctas, who, limit_us, stored, stream=None) -> int:
+    return _lib.gptq_selftest_give_up(ctas, who, int(limit_us), _ptr(stored), _stream(stream))
 
 
 def gptq_trace_reset(stream=None) -> int:

@@ -1381,7 +1381,46 @@ static int fp8_dispatch(Fp8Call c, int format, void *stream)
     return launch_fp8_any(c, s);
 }
 
+// Self-test: the exchange of fp8_few_kernel without its products.  CTA `who` waits for what nothing brings.
+__global__ void give_up_selftest_kernel(int S, int who, unsigned long long limit_ns, int *stored)
+{
+    __shared__ __align__(8) unsigned long long bar;
+    __shared__ uint32_t told;
+    const uint32_t b = smem_u32(&bar), flag = smem_u32(&told);
+    if (threadIdx.x == 0) {
+        mbar_init(b, 1);
+        asm volatile("st.shared.u32 [%0], %1;" ::"r"(flag), "r"(0u) : "memory");
+        fence_barrier_init();
+    }
+    __syncthreads();
+    if (threadIdx.x == 32 && (int)blockIdx.x == who && !mbar_wait_limited(b, 0, limit_ns)) asm volatile("st.shared.u32 [%0], %1;" ::"r"(flag), "r"(1u) : "memory");
+    cluster_arrive_release();
+    cluster_wait_acquire();
+    if (S > 1 && threadIdx.x == 0 && lds32(flag) != 0) few_tell_cluster(flag, S);
+    cluster_arrive_release();
+    cluster_wait_acquire();
+    if (lds32(flag) != 0) return;
+    if (threadIdx.x == 0) stored[blockIdx.x] = 1;
+}
+
 extern "C" {
+
+int gptq_selftest_give_up(int ctas, int who, unsigned int limit_us, int *stored, void *stream)
+{
+    if (ctas < 1 || ctas > 8 || (ctas & (ctas - 1)) || who >= ctas || limit_us < 1 || limit_us > 1000000) return GPTQ_ERR_SHAPE;
+    if (!stored) return GPTQ_ERR_NULL;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = (unsigned)ctas;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3(64);
+    cfg.stream = (cudaStream_t)stream;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return record_cuda_error(cudaLaunchKernelEx(&cfg, give_up_selftest_kernel, ctas, who, (unsigned long long)limit_us * 1000ull, stored));
+}
 
 int gptq_fp8_quantize(const void *x, void *x_fp8, float *x_scales, int M, int K, int format, void *stream)
 {

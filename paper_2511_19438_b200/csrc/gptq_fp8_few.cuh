@@ -73,6 +73,13 @@ __device__ __forceinline__ void fma2_of(uint64_t &acc, uint32_t lo, uint32_t hi,
                  : "+l"(acc) : "r"(lo), "r"(hi), "r"(s_lo), "r"(s_hi));
 }
 
+// Between the two barriers of a cluster's exchange, one thread of a CTA whose wait gave up: then no CTA of the cluster stores a row, since each
+// adds parts of all of them.
+__device__ __forceinline__ void few_tell_cluster(uint32_t flag, int S)
+{
+    for (int p = 0; p < S; ++p) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_to_cluster_rank(flag, p)), "r"(1u) : "memory");
+}
+
 // XQ: x is 16-bit.  Two warps make e4m3 of the rows, a block of K each in turn, write them where TMA would have put them (128-byte rows, 128-byte
 // swizzle) and their scales where the scale warp would have; every CTA does so for its part of K.
 template <int KIND, bool BF, bool OUT8, int TT, bool XQ>
@@ -135,8 +142,6 @@ fp8_few_kernel(const Fp8FewArgs a, const __grid_constant__ CUtensorMap x_map, co
                     done = i + 1;
                     if (++s == NS) s = 0, ph ^= 1;
                 }
-                // nothing may be on its way into the ring when the sums' parts are put there, or when the CTA ends
-                for (int j = done < NS ? 0 : done - NS; j < done; ++j) mbar_wait(bar_full + 8 * (j % NS), (uint32_t)(j / NS) & 1);
             } else {
                 tma_prefetch_descriptor(&x_map);
                 pdl_wait();
@@ -146,9 +151,12 @@ fp8_few_kernel(const Fp8FewArgs a, const __grid_constant__ CUtensorMap x_map, co
                     if (i >= NS && !mbar_wait_once(bar_empty + 8 * s, ph)) break;
                     mbar_arrive_expect_tx(bar_full + 8 * s, x_bytes);
                     tma_load_2d(ring + s * kStage + kW, &x_map, k, m0, bar_full + 8 * s);
+                    done = i + 1;
                     if (++s == NS) s = 0, ph ^= 1;
                 }
             }
+            // nothing of this thread's may be on its way into the ring when the sums' parts are put there, or when the CTA ends
+            for (int j = done < NS ? 0 : done - NS; j < done; ++j) mbar_wait(bar_full + 8 * (j % NS), (uint32_t)(j / NS) & 1);
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------------------------------------ MMA (one thread)
@@ -312,6 +320,7 @@ fp8_few_kernel(const Fp8FewArgs a, const __grid_constant__ CUtensorMap x_map, co
     } else {
         __syncthreads();
     }
+    if (S > 1 && threadIdx.x == 0 && lds32(flag) != 0) few_tell_cluster(flag, S);
     const int mine = TT >> log_S;      // rows per sender (of which those below `rows` are sent)
     if (warp >= kFp8FewFirstDrain) {
 #pragma unroll

@@ -41,3 +41,9 @@ def test_plan_refusals():
     for M, N, K, gated in FEW + PAIRS:      # any number of SMs, one too
         for sms in (1, 2, 3, 20, 1000):
             assert B.gptq_plan_fp8(M, N, K, gated, sms)[0] == B.GPTQ_OK
+
+
+def test_selftest_refusals():
+    for bad in ((0, 0, 200), (3, 0, 200), (16, 0, 200), (4, 4, 200), (4, 0, 0), (4, 0, 1000001)):
+        assert B.gptq_selftest_give_up(*bad, 4096, stream=0) == B.GPTQ_ERR_SHAPE, bad
+    assert B.gptq_selftest_give_up(4, 0, 200, None, stream=0) == B.GPTQ_ERR_NULL
