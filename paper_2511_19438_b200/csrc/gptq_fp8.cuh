@@ -210,15 +210,13 @@ __device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.b
 __device__ __forceinline__ void tma_store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 // A converged warp's wait in few instructions and without a call: what is live in the drain warps fills the registers, and a call
 // would have it stored.  A lane's try is its own, limited in time: the warp goes on once every lane has seen the phase end.
-// `more`: false once a wait has given up; then one try, so that all of a launch's waits together stay short.
-__device__ __forceinline__ bool mbar_wait_warp_inline(uint32_t bar, uint32_t parity, bool more = true)
+__device__ __forceinline__ bool mbar_wait_warp_inline(uint32_t bar, uint32_t parity)
 {
     uint64_t start = 0;
     for (;;) {
 #pragma unroll 1
-        for (int n = more ? 4096 : 1; n; --n)
+        for (int n = 0; n < 4096; ++n)
             if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-        if (!more) return false;
         const uint64_t now = global_timer_ns();
         if (start == 0) start = now;
         if (__any_sync(0xffffffffu, now - start > kWaitLimitNs)) break;
@@ -335,7 +333,7 @@ fp8_tiles_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap x_map, con
                 }
             }
             // nothing may be on its way into either shared memory when the CTAs end
-            if (rank == 0 && warp == 0)
+            if (rank == 0)
                 for (int j = done < kFp8Stages ? 0 : done - kFp8Stages; j < done; ++j) mbar_wait(bar_full + 8 * (j % kFp8Stages), (uint32_t)(j / kFp8Stages) & 1);
         }
       } else if (warp == 1) {
@@ -432,7 +430,10 @@ fp8_tiles_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap x_map, con
         };
         uint32_t at = 0, parity = 0, slot = 0;      // of this block of K: its barriers' offset (0 or 8), their parity, its scales
         int ins = 0;
-        bool ok = true;      // false once a wait has given up: from then on nothing is waited for or stored, but every barrier met
+        // false once a wait has given up: from then on this warp waits for nothing, hands no accumulator back and stores nothing, but meets every barrier of
+        // the CTA.  The MMAs end with the accumulators that it has not drained, so that the pair's other warps give up too instead of draining what
+        // is not whole.
+        bool ok = true;
         for (int t = pair; t < tiles; t += pairs) {
             int tm, tn;
             fp8_tile(t, a.tiles_m, a.tiles_n, tm, tn);
@@ -457,10 +458,17 @@ fp8_tiles_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap x_map, con
             uint64_t acc[2][32];
 #pragma unroll
             for (int j = 0; j < 64; ++j) acc[j / 32][j % 32] = 0;
-            for (int kb = 0; kb < KB; ++kb) {
+            for (int kb = ok ? 0 : KB; kb < KB; ++kb) {
                 const uint32_t from = lanes + 32 * at + cols;
                 if (IN && kb == request_at) request();
-                if (!mbar_wait_warp_inline(bar_dfull + at, parity, ok)) ok = false;
+                if (!mbar_wait_warp_inline(bar_dfull + at, parity)) {
+                    ok = false;
+                    if (IN && live && kb >= request_at)      // no copy into the stages may be on its way when the CTA ends
+#pragma unroll 1
+                        for (int h = 0; h < (KIND == kFp8Plain ? 2 : 1); ++h)
+                            if (KIND != kFp8Plain || out_col(h) < a.N) mbar_wait_warp_inline(my_in + 8 * h, (uint32_t)ins >> h & 1);
+                    break;
+                }
                 tc_fence_after_sync();
                 if (live) {
                     uint32_t v[2][16];
@@ -553,11 +561,13 @@ fp8_tiles_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap x_map, con
                 constexpr int kOuts = KIND == kFp8Backward ? 2 : 1;
                 __syncwarp();      // every lane has read its input: the stages are free
                 if constexpr (OUT8) {
-                    // the two warps that hold a row's 128 columns exchange their maxima (in their stages)
+                    // the two warps that hold a row's 128 columns exchange their maxima (in their stages), and whether they are whole
+                    if (!ok) top[0] = ~0u;
                     asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(stage + 8 * lane), "r"(top[0]), "r"(top[1]) : "memory");
                     named_bar_sync(1 + q, 64);
                     const uint2 other = lds64(out_stage + ((warp - kFp8FirstDrain) ^ 4) * 2 * kFp8OutBytes + 8 * lane);
                     named_bar_sync(1 + q, 64);
+                    ok = __all_sync(0xffffffffu, ok && (int)other.x >= 0);      // (a vote: what hangs on ok stays the warp's; without it 2 to 5 % slower)
                     top[0] = max(top[0], other.x), top[1] = max(top[1], other.y);
                     const int FB = F / kFp8Block;
 #pragma unroll
