@@ -402,7 +402,7 @@ fp8_tiles_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap x_map, con
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     if (kb0 + j >= KB || !ok) break;
-                    if (i >= 2) ok = mbar_wait_warp(bar_dfull + 8 * (i & 1), (uint32_t)(i / 2 - 1) & 1);
+                    if (i >= 2 && !(ok = mbar_wait_warp(bar_dfull + 8 * (i & 1), (uint32_t)(i / 2 - 1) & 1))) break;      // (the slot may still be read)
                     const uint32_t slot = scale_ring + (i & 3) * kFp8ScaleBytes + 4 * l4;
 #pragma unroll
                     for (int h = 0; h < 2; ++h)

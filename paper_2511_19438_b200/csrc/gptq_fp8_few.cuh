@@ -218,6 +218,7 @@ fp8_few_kernel(const Fp8FewArgs a, const __grid_constant__ CUtensorMap x_map, co
             // the stage is free, and the scales' slot (as below)
             if (i >= NS) ok = mbar_wait_warp(bar_empty + 8 * s, ph);
             if (ok && i >= NB) ok = mbar_wait_warp(bar_dfull + 8 * (i & (NB - 1)), (uint32_t)(i / NB - 1) & 1);
+            if (!ok) break;      // (stage and slot may still be read)
             const uint32_t to = ring + s * kStage + kW + (lane & 3) * 4, slot = scale_ring + (i & (2 * NB - 1)) * kScale;
 #pragma unroll
             for (int m = 0; m < kFp8FewInline; ++m) {
@@ -259,7 +260,7 @@ fp8_few_kernel(const Fp8FewArgs a, const __grid_constant__ CUtensorMap x_map, co
             for (int j = 0; j < 2; ++j) {
                 const int i = i0 + j;
                 if (i >= nkb || !ok) break;
-                if (i >= NB) ok = mbar_wait_warp(bar_dfull + 8 * (i & (NB - 1)), (uint32_t)(i / NB - 1) & 1);
+                if (i >= NB && !(ok = mbar_wait_warp(bar_dfull + 8 * (i & (NB - 1)), (uint32_t)(i / NB - 1) & 1))) break;      // (the slot may still be read)
                 const uint32_t slot = scale_ring + (i & (2 * NB - 1)) * kScale;
 #pragma unroll
                 for (int g = 0; g < G; ++g)
