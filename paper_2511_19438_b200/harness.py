@@ -6,6 +6,7 @@ call into libgptq_b200.so through ``binding``.
 """
 from __future__ import annotations
 
+import contextlib
 from dataclasses import dataclass
 
 import numpy as np
@@ -416,12 +417,22 @@ def gemm_fp8_silu_mul_backward(x: torch.Tensor, D: DeviceFp8Linear, d_out: torch
     return (out, s) if quantized else out
 
 
+def _memory_of(stream, device):
+    """What is allocated inside and freed before the call returns is used again on ``stream`` only, behind the kernels that read it."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(B._stream(stream), device=device))
+
+
 def mlp_fp8(x: torch.Tensor, gate_up: DeviceFp8Linear, down: DeviceFp8Linear, residual: torch.Tensor | None = None,
             y: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """A gated feed-forward block, y = down(silu(gate) * up) + residual, the activation in 8 bits between the layers
     (workspace: ensure_for_fp8 of x)."""
-    h, s = gemm_fp8_silu_mul(x, gate_up, quantized=True, stream=stream)
-    return gemm_fp8(h, down, residual=residual, y=y, x_scales=s, dtype=x.dtype, stream=stream)
+    if y is None:
+        y = torch.empty((x.shape[0], down.N), dtype=x.dtype, device=x.device)
+    with _memory_of(stream, x.device):
+        h, s = gemm_fp8_silu_mul(x, gate_up, quantized=True, stream=stream)
+        return gemm_fp8(h, down, residual=residual, y=y, x_scales=s, dtype=x.dtype, stream=stream)
 
 
 def mlp_fp8_backward(x: torch.Tensor, gate_up: DeviceFp8Linear, down: DeviceFp8Linear, d_y: torch.Tensor, stream=None) -> torch.Tensor:
@@ -429,6 +440,8 @@ def mlp_fp8_backward(x: torch.Tensor, gate_up: DeviceFp8Linear, down: DeviceFp8L
     and of x)."""
     if gate_up.transposed is None or down.transposed is None:
         raise ValueError("gate_up and down are needed the other way round too: fp8_linear(..., transpose=True)")
-    d_h = gemm_fp8(d_y, down.transposed, stream=stream)
-    d_gate_up, s = gemm_fp8_silu_mul_backward(x, gate_up, d_h, stream=stream)
-    return gemm_fp8(d_gate_up, gate_up.transposed, x_scales=s, dtype=x.dtype, stream=stream)
+    dx = torch.empty((x.shape[0], gate_up.K), dtype=x.dtype, device=x.device)
+    with _memory_of(stream, x.device):
+        d_h = gemm_fp8(d_y, down.transposed, stream=stream)
+        d_gate_up, s = gemm_fp8_silu_mul_backward(x, gate_up, d_h, stream=stream)
+        return gemm_fp8(d_gate_up, gate_up.transposed, y=dx, x_scales=s, dtype=x.dtype, stream=stream)

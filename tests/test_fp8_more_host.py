@@ -2,10 +2,14 @@
 import os
 import re
 
+import pytest
+import torch
+
 from paper_2511_19438_b200 import build as libbuild
 
 libbuild.build()
 from paper_2511_19438_b200 import binding as B  # noqa: E402
+from paper_2511_19438_b200 import harness as H  # noqa: E402
 
 
 def test_no_uniform_branch_on_a_lane_s_own_try():
@@ -47,3 +51,66 @@ def test_selftest_refusals():
     for bad in ((0, 0, 200), (3, 0, 200), (16, 0, 200), (4, 4, 200), (4, 0, 0), (4, 0, 1000001)):
         assert B.gptq_selftest_give_up(*bad, 4096, stream=0) == B.GPTQ_ERR_SHAPE, bad
     assert B.gptq_selftest_give_up(4, 0, 200, None, stream=0) == B.GPTQ_ERR_NULL
+
+
+# ------------------------------------------------------------------------------------------------ the harness, on stand-ins for the GPU's calls
+@pytest.fixture
+def calls(monkeypatch):
+    """The library's calls and torch's streams replaced by a list of what happened."""
+    log, inside = [], []
+
+    class Stream:
+        cuda_stream = 77
+
+        def __init__(self, *a, **kw):
+            pass
+
+        def synchronize(self):
+            log.append("synchronize")
+
+    class Under:
+        def __init__(self, stream):
+            pass
+
+        def __enter__(self):
+            inside.append(1)
+
+        def __exit__(self, *a):
+            inside.pop()
+
+    empty = torch.empty
+
+    def record_empty(*a, **kw):
+        t = empty(*a, **kw)
+        log.append(("empty", t.data_ptr(), bool(inside)))
+        return t
+
+    for name in ("gptq_fp8_quantize", "gptq_fp8_transpose", "gptq_gemm_fp8", "gptq_gemm_fp8_silu_mul", "gptq_gemm_fp8_silu_mul_backward"):
+        monkeypatch.setattr(B, name, lambda *a, name=name: log.append(name) or B.GPTQ_OK)
+    monkeypatch.setattr(torch, "empty", record_empty)
+    monkeypatch.setattr(torch.cuda, "Stream", Stream)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", Stream)
+    monkeypatch.setattr(torch.cuda, "stream", Under)
+    monkeypatch.setattr(torch.cuda, "current_stream", Stream)
+    monkeypatch.setattr(H, "_expect_here", lambda *a: None, raising=False)
+    return log
+
+
+def layer(N, K):
+    return H.DeviceFp8Linear(K, N, torch.zeros((N, K), dtype=torch.uint8).view(torch.float8_e4m3fn), torch.ones((-(-N // 128), -(-K // 128))))
+
+
+@pytest.mark.parametrize("stream", ["object", 77, None])
+def test_what_the_block_allocates_for_itself_belongs_to_its_stream(calls, stream):
+    """Memory that the caller never sees is freed when the call returns: on another stream than its own it could be given away while it is read."""
+    given = torch.cuda.Stream() if stream == "object" else stream
+    gate_up, down = layer(512, 256), layer(256, 256)
+    gate_up.transposed, down.transposed = layer(256, 512), layer(256, 256)
+    x = torch.zeros((4, 256), dtype=torch.float16)
+    for run, own in ((lambda: H.mlp_fp8(x, gate_up, down, stream=given), 2), (lambda: H.mlp_fp8_backward(x, gate_up, down, x, stream=given), 3)):
+        calls.clear()
+        out = run()
+        made = [c for c in calls if c[0] == "empty"]
+        assert len(made) == own + 1
+        for _, address, under in made:
+            assert under == (given is not None and address != out.data_ptr())

@@ -2,12 +2,16 @@
 import pytest
 import torch
 
+from . import test_gpu_fp8 as T
+from .test_gpu_fp8 import layer, quantize, rows, spread, weights, ws  # noqa: F401
+
 pytestmark = pytest.mark.gpu
 
 if torch.cuda.is_available():
     from paper_2511_19438_b200 import build as libbuild
     libbuild.build()
     from paper_2511_19438_b200 import binding as B
+    from paper_2511_19438_b200 import harness as H
 
 
 @pytest.mark.parametrize("ctas", [1, 2, 4, 8])
@@ -20,3 +24,26 @@ def test_a_wait_that_gave_up_keeps_the_whole_cluster_from_storing(ctas):
         assert B.gptq_check_status() == (B.GPTQ_OK if who < 0 else B.GPTQ_ERR_TIMEOUT)
         assert (stored == (1 if who < 0 else 0)).all()
     assert B.gptq_check_status() == B.GPTQ_OK
+
+
+@pytest.mark.parametrize("handle", [False, True])
+def test_the_block_on_a_stream_that_is_not_the_current_one(ws, handle):  # noqa: F811
+    """What it allocates for itself stays its own until its kernels have read it, whatever the current stream allocates behind the call."""
+    M, K, F = 64, 1024, 2048
+    gate_up, down = layer(2 * F, K, "up", transpose=True), layer(K, F, "down", transpose=True)
+    x, d_y = rows(M, K, torch.bfloat16, "stream"), rows(M, K, torch.bfloat16, "stream-d")
+    H.ensure_for_fp8(ws, M, K)
+    want = T.step(x, d_y, gate_up, down)
+    side = torch.cuda.Stream()
+    given = side.cuda_stream if handle else side
+    for _ in range(3):
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)      # the block's kernels start some ms behind what follows on the current stream
+        y = H.mlp_fp8(x, gate_up, down, residual=x, stream=given)
+        dx = H.mlp_fp8_backward(x, gate_up, down, d_y, stream=given)
+        taken = [torch.full(shape, 0x7f, dtype=torch.uint8, device="cuda") for shape in ((M, F), (M, F // 32), (M, 2 * F), (M, 2 * F // 32), (M, 2 * K))
+                 for _ in range(3)]
+        torch.cuda.synchronize()
+        assert torch.equal(y, want[0]) and torch.equal(dx, want[1])
+        del taken
