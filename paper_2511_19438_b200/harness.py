@@ -339,6 +339,7 @@ def fp8_linear(weight: torch.Tensor, scales: torch.Tensor, transpose: bool = Fal
         T = DeviceFp8Linear(N, K, torch.empty((K, N), dtype=weight.dtype, device=weight.device),
                             torch.empty((_blocks(K), _blocks(N)), dtype=scales.dtype, device=scales.device))
         B.check(B.gptq_fp8_transpose(weight, scales, T.weight, T.scales, N, K), "gptq_fp8_transpose")
+        torch.cuda.current_stream().synchronize()      # products on any stream, which do not wait for weights, may follow
         D.transposed = T
     return D
 

@@ -114,3 +114,12 @@ def test_what_the_block_allocates_for_itself_belongs_to_its_stream(calls, stream
         assert len(made) == own + 1
         for _, address, under in made:
             assert under == (given is not None and address != out.data_ptr())
+
+
+def test_a_layer_is_laid_out_when_it_is_returned(calls):
+    """Products read weights before earlier kernels have ended, and may run on any stream."""
+    D = layer(256, 128)
+    H.fp8_linear(D.weight, D.scales)
+    assert calls == []
+    H.fp8_linear(D.weight, D.scales, transpose=True)
+    assert [c for c in calls if c[0] != "empty"] == ["gptq_fp8_transpose", "synchronize"]

@@ -47,3 +47,19 @@ def test_the_block_on_a_stream_that_is_not_the_current_one(ws, handle):  # noqa:
         torch.cuda.synchronize()
         assert torch.equal(y, want[0]) and torch.equal(dx, want[1])
         del taken
+
+
+def test_a_new_layer_on_another_stream(ws):  # noqa: F811
+    """The transposed layer is whole when fp8_linear returns, even if its stream was busy."""
+    M, N, K = 16, 4096, 2048
+    D = layer(N, K, "late")
+    d = rows(M, N, torch.bfloat16, "late")
+    q, s = quantize(d)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(20_000_000)
+    L = H.fp8_linear(D.weight, D.scales, transpose=True)
+    dx = H.gemm_fp8(q, L.transposed, x_scales=s, dtype=torch.bfloat16, stream=side)
+    torch.cuda.synchronize()
+    T.check_gemm(dx, spread(q, s), L.transposed)
+    assert torch.equal(weights(L.transposed), weights(D).t())
