@@ -329,11 +329,24 @@ def _blocks(n: int) -> int:
     return -(-n // 128)
 
 
+def _here() -> torch.device:
+    return torch.device("cuda", torch.cuda.current_device())
+
+
+def _expect_here(*tensors: torch.Tensor | None) -> None:
+    """The kernels run on the current device, with the addresses that they are given."""
+    here = _here()
+    for t in tensors:
+        if t is not None and t.device != here:
+            raise ValueError(f"a tensor on {t.device}, the current device is {here}")
+
+
 def fp8_linear(weight: torch.Tensor, scales: torch.Tensor, transpose: bool = False) -> DeviceFp8Linear:
     """A layer whose tensors are on the GPU; ``transpose``: laid out the other way round too (gptq_fp8_transpose)."""
     N, K = weight.shape
     _expect("weight", weight, torch.float8_e4m3fn, (N, K))
     _expect("scales", scales, torch.float32, (_blocks(N), _blocks(K)))
+    _expect_here(weight, scales)
     D = DeviceFp8Linear(K, N, weight, scales)
     if transpose:
         T = DeviceFp8Linear(N, K, torch.empty((K, N), dtype=weight.dtype, device=weight.device),
@@ -357,10 +370,9 @@ def _format_of(dtype: torch.dtype) -> int:
 
 def _expect_rows(x: torch.Tensor, x_scales: torch.Tensor | None, dtype: torch.dtype, D: DeviceFp8Linear) -> int:
     M = x.shape[0]
-    if x.device != D.weight.device:
-        raise ValueError(f"x on {x.device}, the layer on {D.weight.device}")
     _expect("x", x, dtype if x_scales is None else torch.float8_e4m3fn, (M, D.K))
     _expect("x_scales", x_scales, torch.float32, (M, _blocks(D.K)))
+    _expect_here(x, x_scales, D.weight, D.scales)
     return M
 
 
@@ -372,6 +384,7 @@ def fp8_quantize(x: torch.Tensor, stream=None) -> tuple[torch.Tensor, torch.Tens
     """(e4m3 [M, K], fp32 scales [M, ceil(K / 128)]) of 16-bit rows through gptq_fp8_quantize."""
     M, K = x.shape
     _expect("x", x, x.dtype, (M, K))
+    _expect_here(x)
     q, s = _rows_fp8(M, K, x.device)
     B.check(B.gptq_fp8_quantize(x, q, s, M, K, _format_of(x.dtype), stream), "gptq_fp8_quantize")
     return q, s
@@ -390,6 +403,7 @@ def gemm_fp8(x: torch.Tensor, D: DeviceFp8Linear, bias: torch.Tensor | None = No
     _expect("bias", bias, dtype, (D.N,))
     _expect("residual", residual, dtype, (M, D.N))
     _expect("y", y, dtype, (M, D.N))
+    _expect_here(bias, residual, y)
     B.check(B.gptq_gemm_fp8(x, x_scales, D.weight, D.scales, bias, residual, y, M, D.N, D.K, fmt, stream), "gptq_gemm_fp8")
     return y
 
@@ -412,6 +426,7 @@ def gemm_fp8_silu_mul_backward(x: torch.Tensor, D: DeviceFp8Linear, d_out: torch
     fmt = _format_of(d_out.dtype)
     M, F = _expect_rows(x, x_scales, d_out.dtype, D), D.N // 2
     _expect("d_out", d_out, d_out.dtype, (M, F))
+    _expect_here(d_out)
     out, s = _rows_fp8(M, D.N, x.device) if quantized else (torch.empty((M, D.N), dtype=d_out.dtype, device=x.device), None)
     B.check(B.gptq_gemm_fp8_silu_mul_backward(x, x_scales, D.weight, D.scales, d_out, out, s, M, F, D.K, fmt, stream),
             "gptq_gemm_fp8_silu_mul_backward")

@@ -123,3 +123,28 @@ def test_a_layer_is_laid_out_when_it_is_returned(calls):
     assert calls == []
     H.fp8_linear(D.weight, D.scales, transpose=True)
     assert [c for c in calls if c[0] != "empty"] == ["gptq_fp8_transpose", "synchronize"]
+
+
+def test_tensors_elsewhere_are_refused(monkeypatch):
+    """Any one of them on another device than the current one: the kernel would be given an address of that device."""
+    for name in ("gptq_fp8_quantize", "gptq_fp8_transpose", "gptq_gemm_fp8", "gptq_gemm_fp8_silu_mul", "gptq_gemm_fp8_silu_mul_backward"):
+        monkeypatch.setattr(B, name, lambda *a: B.GPTQ_OK)
+    monkeypatch.setattr(B, "_stream", lambda s: 0)
+    monkeypatch.setattr(H, "_here", lambda: torch.device("cpu"))      # as if the CPU were the current device
+    D, x = layer(256, 256), torch.zeros((4, 256), dtype=torch.float16)
+    x8, s = x.to(torch.float8_e4m3fn), torch.ones((4, 2))
+    runs = {
+        "linear": (lambda weight, scales: H.fp8_linear(weight, scales), dict(weight=D.weight, scales=D.scales)),
+        "quantize": (lambda x: H.fp8_quantize(x), dict(x=x)),
+        "gemm": (lambda x, xs, w, ws, b, r, y: H.gemm_fp8(x, H.DeviceFp8Linear(256, 256, w, ws), b, r, y, x_scales=xs),
+                 dict(x=x8, xs=s, w=D.weight, ws=D.scales, b=x[0].clone(), r=x, y=x.clone())),
+        "gated": (lambda x, xs, w, ws: H.gemm_fp8_silu_mul(x, H.DeviceFp8Linear(256, 256, w, ws), x_scales=xs),
+                  dict(x=x8, xs=s, w=D.weight, ws=D.scales)),
+        "backward": (lambda x, xs, w, ws, d: H.gemm_fp8_silu_mul_backward(x, H.DeviceFp8Linear(256, 256, w, ws), d, x_scales=xs),
+                     dict(x=x8, xs=s, w=D.weight, ws=D.scales, d=x[:, :128].contiguous())),
+    }
+    for name, (run, tensors) in runs.items():
+        run(**tensors)
+        for t in tensors:
+            with pytest.raises(ValueError, match="meta"):
+                run(**{**tensors, t: tensors[t].to("meta")})
