@@ -376,6 +376,12 @@ def _expect_rows(x: torch.Tensor, x_scales: torch.Tensor | None, dtype: torch.dt
     return M
 
 
+def _gated_columns(D: DeviceFp8Linear) -> int:
+    if D.N % 256:
+        raise ValueError(f"gate's rows, then as many of up's, a multiple of 128 each, expected, got {D.N} rows")
+    return D.N // 2
+
+
 def _rows_fp8(M: int, N: int, device) -> tuple[torch.Tensor, torch.Tensor]:
     return (torch.empty((M, N), dtype=torch.float8_e4m3fn, device=device), torch.empty((M, _blocks(N)), dtype=torch.float32, device=device))
 
@@ -414,7 +420,7 @@ def gemm_fp8_silu_mul(x: torch.Tensor, D: DeviceFp8Linear, x_scales: torch.Tenso
     its scales."""
     dtype = x.dtype if x_scales is None else dtype or torch.float16
     fmt = _format_of(dtype)
-    M, F = _expect_rows(x, x_scales, dtype, D), D.N // 2
+    M, F = _expect_rows(x, x_scales, dtype, D), _gated_columns(D)
     out, s = _rows_fp8(M, F, x.device) if quantized else (torch.empty((M, F), dtype=dtype, device=x.device), None)
     B.check(B.gptq_gemm_fp8_silu_mul(x, x_scales, D.weight, D.scales, out, s, M, F, D.K, fmt, stream), "gptq_gemm_fp8_silu_mul")
     return (out, s) if quantized else out
@@ -424,7 +430,7 @@ def gemm_fp8_silu_mul_backward(x: torch.Tensor, D: DeviceFp8Linear, d_out: torch
                                quantized: bool = True, stream=None):
     """The gradients [M, N] of gate's and up's columns through gptq_gemm_fp8_silu_mul_backward: e4m3 and scales, or 16-bit."""
     fmt = _format_of(d_out.dtype)
-    M, F = _expect_rows(x, x_scales, d_out.dtype, D), D.N // 2
+    M, F = _expect_rows(x, x_scales, d_out.dtype, D), _gated_columns(D)
     _expect("d_out", d_out, d_out.dtype, (M, F))
     _expect_here(d_out)
     out, s = _rows_fp8(M, D.N, x.device) if quantized else (torch.empty((M, D.N), dtype=d_out.dtype, device=x.device), None)

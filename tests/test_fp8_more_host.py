@@ -148,3 +148,15 @@ def test_tensors_elsewhere_are_refused(monkeypatch):
         for t in tensors:
             with pytest.raises(ValueError, match="meta"):
                 run(**{**tensors, t: tensors[t].to("meta")})
+
+
+def test_a_gated_layer_has_as_many_rows_of_up_as_of_gate(calls):
+    """An odd row at the end would have been left out without a word."""
+    x, d = torch.zeros((4, 256), dtype=torch.float16), torch.zeros((4, 128), dtype=torch.float16)
+    for N in (257, 264, 128, 384):
+        with pytest.raises(ValueError, match="rows"):
+            H.gemm_fp8_silu_mul(x, layer(N, 256))
+        with pytest.raises(ValueError, match="rows"):
+            H.gemm_fp8_silu_mul_backward(x, layer(N, 256), torch.zeros((4, N // 2), dtype=torch.float16))
+    H.gemm_fp8_silu_mul(x, layer(256, 256))
+    H.gemm_fp8_silu_mul_backward(x, layer(256, 256), d)
