@@ -360,6 +360,7 @@ int gptq_gemm_lora_bf16(const void *x, const void *qweight, const void *qzeros, 
  * [ceil(N / 128), ceil(K / 128)], w[n, k] = weight[n, k] * weight_scales[n / 128, k / 128].  Rows of activations or gradients: e4m3
  * [M, K] and x_scales fp32 [M, ceil(K / 128)].  e4m3: 1 sign, 4 exponent (bias 7), 3 fraction bits, largest number 448, no infinities.
  * `format`: 0 (16-bit inputs and results are fp16) or GPTQ_FORMAT_BF16 (bfloat16); anything else: GPTQ_ERR_LAYOUT.
+ * No result may lie over an input or another result, not in part either (GPTQ_ERR_LAYOUT); a residual may be the result itself.
  * K is a multiple of 16, N of 8 (GPTQ_ERR_SHAPE); a last block may have fewer than 128.  Pointers, NULL or not, are 16-byte aligned.
  * Stream semantics as for gptq_gemm: launches overlap the end of earlier kernels on the stream, and weights (not their scales, nor anything
  * else) are read before these have ended, which matters only if the kernel in front writes weights and lets later kernels start early. */
@@ -376,7 +377,7 @@ int gptq_fp8_transpose(const void *weight, const float *weight_scales, void *wei
  * NULL: x is 16-bit [M, K] and becomes e4m3 as by gptq_fp8_quantize, in the registered workspace: gptq_fp8_workspace_bytes(M, K)
  * (GPTQ_ERR_WORKSPACE without it), under the rules of gptq_set_workspace.  Sums over a block of 128 in the tensor core's fp32, times the two
  * scales (their product in fp32: below 2^-126 it counts as zero), over blocks, bias and residual in fp32, one rounding of y.  The order of the sums is fixed.
- * y must not be x (GPTQ_ERR_LAYOUT).  The gradient of x is the same call with the gradient of y in the place of x and the layer of
+ * The gradient of x is the same call with the gradient of y in the place of x and the layer of
  * gptq_fp8_transpose (rounding to e4m3 counts as the identity). */
 size_t gptq_fp8_workspace_bytes(int M, int K);
 int gptq_gemm_fp8(const void *x, const float *x_scales, const void *weight, const float *weight_scales, const void *bias,
@@ -393,7 +394,7 @@ int gptq_gemm_fp8_silu_mul(const void *x, const float *x_scales, const void *wei
  *     d_gate = d_out * up * p * (1 + gate * (1 - p)),  d_up = d_out * gate * p,  p = 1 / (1 + exp(-gate))
  * with gate and up formed again from x and weight.  d_gate_up [M, 2 F] = gate's columns, then up's: e4m3 with d_gate_up_scales [M, 2 F / 128],
  * or (NULL) 16-bit.  The gradient of x is gptq_gemm_fp8(d_gate_up, d_gate_up_scales, the layer of gptq_fp8_transpose, ..., M, K, 2 F).
- * d_gate_up must not be x or d_out.  Otherwise as gptq_gemm_fp8_silu_mul. */
+ * Otherwise as gptq_gemm_fp8_silu_mul. */
 int gptq_gemm_fp8_silu_mul_backward(const void *x, const float *x_scales, const void *weight, const float *weight_scales, const void *d_out,
                                     void *d_gate_up, float *d_gate_up_scales, int M, int F, int K, int format, void *stream);
 

@@ -1353,6 +1353,30 @@ static int check_fp8(int M, int N, int K, int format)
     return GPTQ_OK;
 }
 
+struct Extent {
+    const void *at;      // nullptr: nothing
+    size_t bytes;
+};
+static bool overlap(const Extent &a, const Extent &b)
+{
+    const uintptr_t p = (uintptr_t)a.at, q = (uintptr_t)b.at;
+    return p && q && p < q + b.bytes && q < p + a.bytes;
+}
+
+// Results over inputs: while some CTAs write theirs, others still read.  (The residual in place: each element is read where it is written.)
+static bool fp8_overlaps(const Fp8Call &c)
+{
+    const size_t M = c.M, N = c.N, K = c.K, KB = fp8_blocks(c.K), in_columns = c.kind == kFp8Plain ? N : N / 2, columns = c.kind == kFp8Gated ? N / 2 : N;
+    const bool in_place = c.kind == kFp8Plain && c.in == c.out;
+    const Extent out[] = {{c.out, M * columns * (c.out_scales ? 1 : 2)}, {c.out_scales, M * (columns / kFp8Block) * 4}};
+    const Extent in[] = {{c.x, M * K * (c.x_scales ? 1 : 2)}, {c.x_scales, M * KB * 4}, {c.w, N * K}, {c.w_scales, fp8_blocks(c.N) * KB * 4},
+                         {c.bias, N * 2},  {in_place ? nullptr : c.in, M * in_columns * 2}};
+    for (const Extent &o : out)
+        for (const Extent &i : in)
+            if (overlap(o, i)) return true;
+    return overlap(out[0], out[1]);
+}
+
 static int fp8_dispatch(Fp8Call c, int format, void *stream)
 {
     int st = check_fp8(c.M, c.N, c.K, format);
@@ -1362,7 +1386,7 @@ static int fp8_dispatch(Fp8Call c, int format, void *stream)
     const void *ptrs[] = {c.x, c.x_scales, c.w, c.w_scales, c.bias, c.in, c.out, c.out_scales};
     for (const void *p : ptrs)
         if (!aligned16(p)) return GPTQ_ERR_ALIGN;
-    if (c.out == c.x || (c.kind == kFp8Backward && c.out == c.in)) return GPTQ_ERR_LAYOUT;      // rows of them are read while others of the result are written
+    if (fp8_overlaps(c)) return GPTQ_ERR_LAYOUT;
     int dev;
     st = current_device_sms(&dev, &c.sms);
     if (st) return st;
@@ -1428,7 +1452,8 @@ int gptq_fp8_quantize(const void *x, void *x_fp8, float *x_scales, int M, int K,
     if (st) return st;
     if (!x || !x_fp8 || !x_scales) return GPTQ_ERR_NULL;
     if (!aligned16(x) || !aligned16(x_fp8) || !aligned16(x_scales)) return GPTQ_ERR_ALIGN;
-    if (x == x_fp8) return GPTQ_ERR_LAYOUT;
+    const Extent in{x, (size_t)M * K * 2}, q{x_fp8, (size_t)M * K}, s{x_scales, (size_t)M * fp8_blocks(K) * 4};
+    if (overlap(in, q) || overlap(in, s) || overlap(q, s)) return GPTQ_ERR_LAYOUT;
     int dev, sms;
     st = current_device_sms(&dev, &sms);
     if (st) return st;
@@ -1440,7 +1465,11 @@ int gptq_fp8_transpose(const void *weight, const float *weight_scales, void *wei
     if (N < 16 || K < 16 || N % 16 || K % 16) return GPTQ_ERR_SHAPE;
     if (!weight || !weight_scales || !weight_out || !scales_out) return GPTQ_ERR_NULL;
     if (!aligned16(weight) || !aligned16(weight_scales) || !aligned16(weight_out) || !aligned16(scales_out)) return GPTQ_ERR_ALIGN;
-    if (weight == weight_out || weight_scales == scales_out) return GPTQ_ERR_LAYOUT;
+    const size_t nk = (size_t)N * K, blocks = (size_t)fp8_blocks(N) * fp8_blocks(K) * 4;
+    const Extent all[] = {{weight, nk}, {weight_scales, blocks}, {weight_out, nk}, {scales_out, blocks}};
+    for (int o = 2; o < 4; ++o)
+        for (int i = 0; i < o; ++i)
+            if (overlap(all[o], all[i])) return GPTQ_ERR_LAYOUT;
     return launch_fp8_transpose(weight, weight_scales, weight_out, scales_out, N, K, (cudaStream_t)stream);
 }
 

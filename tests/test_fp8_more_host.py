@@ -160,3 +160,37 @@ def test_a_gated_layer_has_as_many_rows_of_up_as_of_gate(calls):
             H.gemm_fp8_silu_mul_backward(x, layer(N, 256), torch.zeros((4, N // 2), dtype=torch.float16))
     H.gemm_fp8_silu_mul(x, layer(256, 256))
     H.gemm_fp8_silu_mul_backward(x, layer(256, 256), d)
+
+
+# ------------------------------------------------------------------------------------------------ results over inputs
+A, GAP = 1 << 20, 1 << 20      # addresses that are never followed
+M, N, K = 8, 512, 256
+
+
+def overlapping(fn, sizes, results, allowed, numbers):
+    """Each result laid over the first, the last and all bytes of each other argument: refused, unless `allowed`; then beside it: not refused
+    for that."""
+    at = {n: A + GAP * i for i, n in enumerate(sizes)}
+    for r in results:
+        for n in sizes:
+            if n == r or sizes[n] == 0 or sizes[r] == 0:
+                continue
+            first, last = at[n] - (sizes[r] - 1) // 16 * 16, at[n] + (sizes[n] - 1) // 16 * 16
+            for place in {first, last, at[n]}:
+                if (r, n) in allowed and place == at[n]:
+                    continue
+                assert fn(*[None if sizes[k] == 0 else place if k == r else v for k, v in at.items()], *numbers, stream=0) == B.GPTQ_ERR_LAYOUT, (r, n)
+
+
+def test_refused_overlaps():
+    q = {"x": M * K * 2, "q": M * K, "s": M * 2 * 4}
+    overlapping(B.gptq_fp8_quantize, q, ("q", "s"), (), (M, K, 0))
+    overlapping(B.gptq_fp8_transpose, {"w": N * K, "s": 4 * 2 * 4, "wo": N * K, "so": 4 * 2 * 4}, ("wo", "so"), (), (N, K))
+    for x8 in (False, True):
+        x = {"x": M * K * (1 if x8 else 2), "xs": M * 2 * 4 if x8 else 0, "w": N * K, "ws": 4 * 2 * 4}
+        overlapping(B.gptq_gemm_fp8, {**x, "bias": 2 * N, "residual": 2 * M * N, "y": 2 * M * N}, ("y",), (("y", "residual"),), (M, N, K, 0))
+        for out8 in (False, True):
+            def outs(columns):
+                return {"out": M * columns * (1 if out8 else 2), "outs": M * (columns // 128) * 4 if out8 else 0}
+            overlapping(B.gptq_gemm_fp8_silu_mul, {**x, **outs(N // 2)}, ("out", "outs"), (), (M, N // 2, K, 0))
+            overlapping(B.gptq_gemm_fp8_silu_mul_backward, {**x, "d": M * N // 2 * 2, **outs(N)}, ("out", "outs"), (), (M, N // 2, K, 0))

@@ -63,3 +63,24 @@ def test_a_new_layer_on_another_stream(ws):  # noqa: F811
     torch.cuda.synchronize()
     T.check_gemm(dx, spread(q, s), L.transposed)
     assert torch.equal(weights(L.transposed), weights(D).t())
+
+
+@pytest.mark.parametrize("M", [3, 40, 1300])
+def test_arguments_side_by_side(ws, M):  # noqa: F811
+    """Inputs and results without a gap between them are not refused, and none is written over."""
+    F, K, dtype = 2048, 512, torch.float16
+    D, x, d = layer(2 * F, K, "beside"), rows(M, K, dtype, "beside"), rows(M, F, dtype, "beside-d")
+    q, s = quantize(x)
+    want = H.gemm_fp8_silu_mul_backward(q, D, d, x_scales=s)
+    parts = [(M * K, q), (M * 2 * F, None), (4 * M * (K // 128), s), (4 * M * (2 * F // 128), None), (2 * M * F, d)]
+    assert all(n % 16 == 0 for n, _ in parts)
+    one = torch.full((sum(n for n, _ in parts),), 0x55, dtype=torch.uint8, device="cuda")
+    views = one.split([n for n, _ in parts])
+    for v, (_, t) in zip(views, parts):
+        if t is not None:
+            v.copy_(t.reshape(-1).view(torch.uint8))
+    qv, out, sv, outs, dv = views
+    B.check(B.gptq_gemm_fp8_silu_mul_backward(qv, sv, D.weight, D.scales, dv, out, outs, M, F, K, 0), "backward")
+    assert torch.equal(out, want[0].reshape(-1).view(torch.uint8)) and torch.equal(outs, want[1].reshape(-1).view(torch.uint8))
+    for v, (_, t) in zip(views, parts):
+        assert t is None or torch.equal(v, t.reshape(-1).view(torch.uint8))
