@@ -13,7 +13,7 @@ namespace gptq {
 
 constexpr int kFp8Block = 128;                        // columns (and weight rows) per scale
 constexpr float kFp8Max = 448.0f, kFp8ScaleMin = 1.17549435e-38f;      // largest e4m3 number; 2^-126
-__host__ __device__ inline int fp8_blocks(int n) { return (n + kFp8Block - 1) / kFp8Block; }
+__host__ __device__ inline int fp8_blocks(int n) { return (n - 1) / kFp8Block + 1; }      // (n up to 2^31 - 1)
 
 // ---- rows of numbers to e4m3 -------------------------------------------------------------------------------------------
 // s = max(max|v| / 448, 2^-126), q = e4m3(v / s): both divisions to the nearest, since with 16-bit v the quotient lies exactly in the
@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(kFp8QuantThreads) fp8_quantize_kernel(const ui
 __global__ void __launch_bounds__(256) fp8_transpose_kernel(const uint8_t *w, const float *scales, uint8_t *w_out, float *scales_out, int N, int K)
 {
     __shared__ uint8_t tile[64][68];
-    const int tiles_k = (K + 63) / 64;
+    const int tiles_k = (K - 1) / 64 + 1;
     const int n0 = (int)(blockIdx.x / tiles_k) * 64, k0 = (int)(blockIdx.x % tiles_k) * 64;
     const int r = threadIdx.x / 4, c = threadIdx.x % 4 * 16;
     if (n0 + r < N && k0 + c < K) {
@@ -655,7 +655,7 @@ inline int launch_fp8_quantize(const void *x, void *q, float *scales, int M, int
 
 inline int launch_fp8_transpose(const void *w, const float *scales, void *w_out, float *scales_out, int N, int K, cudaStream_t s)
 {
-    const long long tiles = (long long)((N + 63) / 64) * ((K + 63) / 64);
+    const long long tiles = (long long)((N - 1) / 64 + 1) * ((K - 1) / 64 + 1);
     if (tiles > 0x7fffffffll) return GPTQ_ERR_UNSUPPORTED;
     fp8_transpose_kernel<<<(unsigned)tiles, 256, 0, s>>>((const uint8_t *)w, scales, (uint8_t *)w_out, scales_out, N, K);
     return record_cuda_error(cudaGetLastError());

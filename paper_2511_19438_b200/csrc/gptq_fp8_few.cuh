@@ -133,12 +133,12 @@ fp8_few_kernel(const Fp8FewArgs a, const __grid_constant__ CUtensorMap x_map, co
             uint32_t ph = 1;
             if (warp == 0) {
                 tma_prefetch_descriptor(&w_map);
-                int k = kb0 * kFp8Block;
+                uint32_t k = (uint32_t)kb0 * kFp8Block;      // (the last step may leave an int)
                 for (int i = 0; i < nkb; ++i, k += kFp8Block) {
                     if (i >= NS && !mbar_wait_once(bar_empty + 8 * s, ph)) break;
                     mbar_arrive_expect_tx(bar_full + 8 * s, kW);
 #pragma unroll
-                    for (int g = 0; g < G; ++g) tma_load_2d(ring + s * kStage + g * 128 * kFp8Block, &w_map, k, g * F + tn * 128, bar_full + 8 * s);
+                    for (int g = 0; g < G; ++g) tma_load_2d(ring + s * kStage + g * 128 * kFp8Block, &w_map, (int)k, g * F + tn * 128, bar_full + 8 * s);
                     done = i + 1;
                     if (++s == NS) s = 0, ph ^= 1;
                 }
@@ -146,11 +146,11 @@ fp8_few_kernel(const Fp8FewArgs a, const __grid_constant__ CUtensorMap x_map, co
                 tma_prefetch_descriptor(&x_map);
                 pdl_wait();
                 const uint32_t x_bytes = (uint32_t)a.tok * kFp8Block;
-                int k = kb0 * kFp8Block;
+                uint32_t k = (uint32_t)kb0 * kFp8Block;
                 for (int i = 0; i < nkb; ++i, k += kFp8Block) {
                     if (i >= NS && !mbar_wait_once(bar_empty + 8 * s, ph)) break;
                     mbar_arrive_expect_tx(bar_full + 8 * s, x_bytes);
-                    tma_load_2d(ring + s * kStage + kW, &x_map, k, m0, bar_full + 8 * s);
+                    tma_load_2d(ring + s * kStage + kW, &x_map, (int)k, m0, bar_full + 8 * s);
                     done = i + 1;
                     if (++s == NS) s = 0, ph ^= 1;
                 }
@@ -190,10 +190,10 @@ fp8_few_kernel(const Fp8FewArgs a, const __grid_constant__ CUtensorMap x_map, co
         uint2 next[kFp8FewInline];      // four numbers of each row
         float w_next[G];
         auto fetch = [&](int i) {
-            const int k = (kb0 + i) * kFp8Block + 4 * lane;
+            const uint32_t k = (uint32_t)(kb0 + i) * kFp8Block + 4 * lane;
 #pragma unroll
             for (int m = 0; m < kFp8FewInline; ++m)
-                next[m] = i < nkb && m < a.M && k < a.K ? ldg64_behind(a.x16 + ((size_t)m * a.K + k) * 2) : make_uint2(0, 0);
+                next[m] = i < nkb && m < a.M && k < (uint32_t)a.K ? ldg64_behind(a.x16 + ((size_t)m * a.K + k) * 2) : make_uint2(0, 0);
 #pragma unroll
             for (int g = 0; g < G; ++g) w_next[g] = i < nkb ? ldgf_behind(ws[g] + i) : 0.0f;
         };

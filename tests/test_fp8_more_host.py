@@ -194,3 +194,13 @@ def test_refused_overlaps():
                 return {"out": M * columns * (1 if out8 else 2), "outs": M * (columns // 128) * 4 if out8 else 0}
             overlapping(B.gptq_gemm_fp8_silu_mul, {**x, **outs(N // 2)}, ("out", "outs"), (), (M, N // 2, K, 0))
             overlapping(B.gptq_gemm_fp8_silu_mul_backward, {**x, "d": M * N // 2 * 2, **outs(N)}, ("out", "outs"), (), (M, N // 2, K, 0))
+
+
+def test_the_longest_rows():
+    """K up to the last multiple of 16 below 2^31."""
+    K = (1 << 31) - 16
+    assert B.gptq_fp8_workspace_bytes(1, K) == (1 << 31) + 4 * (1 << 24)      # (e4m3 rows end on 256 bytes)
+    assert B.gptq_fp8_workspace_bytes(3, K - 128) == 3 * (K - 128) + (-3 * (K - 128) % 256) + 3 * 4 * ((1 << 24) - 1)
+    for shape in ((1, 8, K), (1, (1 << 31) - 8, 16), (1300, (1 << 31) - 8, 16)):
+        st, p = B.gptq_plan_fp8(*shape, 0, 148)
+        assert st == B.GPTQ_OK and p.items >= 1 << 23 and p.ctas >= 1

@@ -84,3 +84,19 @@ def test_arguments_side_by_side(ws, M):  # noqa: F811
     assert torch.equal(out, want[0].reshape(-1).view(torch.uint8)) and torch.equal(outs, want[1].reshape(-1).view(torch.uint8))
     for v, (_, t) in zip(views, parts):
         assert t is None or torch.equal(v, t.reshape(-1).view(torch.uint8))
+
+
+def test_the_longest_row():
+    """One row of the last multiple of 16 below 2^31."""
+    K = (1 << 31) - 16
+    if torch.cuda.mem_get_info()[0] < 16 << 30:
+        pytest.skip("needs 16 GB")
+    x = torch.zeros((1, K), dtype=torch.float16, device="cuda")
+    head, tail = rows(1, 4096, torch.float16, "head"), rows(1, 4080, torch.float16, "tail")
+    x[:, :4096], x[:, -4080:] = head, tail
+    q, s = H.fp8_quantize(x)
+    assert s.shape == (1, 1 << 24)
+    for got, scales, part in ((q[:, :4096], s[:, :32], head), (q[:, -4080:], s[:, -32:], tail)):
+        want = quantize(part)
+        assert torch.equal(scales, want[1]) and torch.equal(got.contiguous().view(torch.uint8), want[0].view(torch.uint8))
+    assert (s[:, 32:-32] == 2.0 ** -126).all()
