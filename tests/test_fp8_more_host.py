@@ -1,7 +1,10 @@
 """Layers in 8-bit floating point, what needs no GPU: waits, refusals, the harness's streams and devices, sizes, the quotient."""
+import ctypes
+import ctypes.util
 import os
 import re
 
+import numpy as np
 import pytest
 import torch
 
@@ -204,3 +207,36 @@ def test_the_longest_rows():
     for shape in ((1, 8, K), (1, (1 << 31) - 8, 16), (1300, (1 << 31) - 8, 16)):
         st, p = B.gptq_plan_fp8(*shape, 0, 148)
         assert st == B.GPTQ_OK and p.items >= 1 << 23 and p.ctas >= 1
+
+
+# ------------------------------------------------------------------------------------------------ the quotient of the e4m3 results
+def test_the_quotient_decides_as_the_nearest_number_does():
+    """q + (v - q s) y, q = v y, y = 1 / s rounded, is within 2^-46 of v / s before its last rounding: the e4m3 number can differ from that of the
+    correctly rounded quotient only where v / s is that near b, the middle of two fp32 numbers of which one is a middle t of e4m3 numbers (five bits).  With
+    s = S 2^a and v = V 2^c (24 bits each) and b = B 2^e, B = 2^20 T +- 1, that is |V 2^j - S B| <= 8, j = 24 or 25: every such pair."""
+    fmaf = ctypes.CDLL(ctypes.util.find_library("m")).fmaf
+    fmaf.restype, fmaf.argtypes = ctypes.c_float, [ctypes.c_float] * 3
+    f = np.float32
+    pairs, got, want = 0, [], []
+    for T in range(16, 33):
+        for sign in (1, -1):
+            B_ = (T << 20) + sign
+            if not 1 << 24 < B_ < 1 << 25:
+                continue
+            for n in range(-9, 10):
+                for S in ((k << 20) - sign * n for k in range(8, 17)):
+                    for j in (24, 25):
+                        V, rest = divmod(S * B_ + n, 1 << j)
+                        if rest or not (1 << 23 <= S < 1 << 24 and 1 << 23 <= V < 1 << 24):
+                            continue
+                        pairs += 1
+                        s = np.ldexp(f(S), -23)
+                        for e in range(-20, 9):      # from beside zero to beyond the largest number
+                            v = np.ldexp(f(V), e - 23)
+                            y = f(1) / s
+                            q = v * y
+                            got.append(fmaf(fmaf(-q, s, v), y, q))
+                            want.append(v / s)
+    assert pairs == 205
+    got, want = (torch.tensor(np.array(a, dtype=f)).clamp(max=448.0).to(torch.float8_e4m3fn).view(torch.uint8) for a in (got, want))
+    assert torch.equal(got, want)
