@@ -385,8 +385,8 @@ int gptq_gemm_fp8(const void *x, const float *x_scales, const void *weight, cons
 
 /* The first half of a gated feed-forward block: out[M, F] = silu(x Wg^T) * (x Wu^T), weight [2 F, K] = gate rows, then up rows; F is a multiple of
  * 128.  out_scales != NULL: out is e4m3 [M, F] with out_scales [M, F / 128], formed from the fp32 result as by gptq_fp8_quantize: what
- * gptq_gemm_fp8 takes for the down projection.  NULL: out is 16-bit.  Otherwise as gptq_gemm_fp8; the exponential is the fast one (2^-20 of the
- * result for gates above -10). */
+ * gptq_gemm_fp8 takes for the down projection.  NULL: out is 16-bit.  Otherwise as gptq_gemm_fp8; the exponential is the fast one: beside the
+ * errors of gate and up the fp32 result is off by (6 + 1.5 |gate|) 2^-23 of itself at most, and the logistic function counts as zero below 2^-126. */
 int gptq_gemm_fp8_silu_mul(const void *x, const float *x_scales, const void *weight, const float *weight_scales, void *out,
                            float *out_scales, int M, int F, int K, int format, void *stream);
 

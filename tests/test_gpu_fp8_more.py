@@ -100,3 +100,30 @@ def test_the_longest_row():
         want = quantize(part)
         assert torch.equal(scales, want[1]) and torch.equal(got.contiguous().view(torch.uint8), want[0].view(torch.uint8))
     assert (s[:, 32:-32] == 2.0 ** -126).all()
+
+
+@pytest.mark.parametrize("M", [1, 20, 300])
+def test_the_error_of_the_logistic_function(M):
+    """Gates of any fp32 value and up = 1, formed without an error: weights of one at the first column, a block's gate is its scale.  All of a
+    block's results are alike, so that its scale times 448 shows the fp32 result (one rounding): off by (6 + 1.5 |gate|) 2^-23 of itself at most.
+    Gradients of d = 1: d_up as the result, d_gate = p (1 + gate (1 - p)) by each term's share and 1 - p by 2^-23."""
+    n, K, F32 = 1024, 16, 2.0 ** -23
+    F = 128 * n
+    gates = 160 * torch.rand(n, generator=T.gen("gates"), device="cuda") - 80
+    gates[:64] = torch.linspace(-20, 20, 64, device="cuda")
+    w = torch.zeros((2 * F, K), device="cuda")
+    w[:, 0] = 1
+    D = H.fp8_linear(w.to(torch.float8_e4m3fn), torch.cat([gates, torch.ones_like(gates)])[:, None].contiguous())
+    x = torch.zeros((M, K), device="cuda")
+    x[:, 0] = 1
+    x, s = x.to(torch.float8_e4m3fn), torch.ones((M, 1), device="cuda")
+    g = gates.double()
+    p = 1 / (1 + torch.exp(-g))
+    rel = (6 + 1.5 * g.abs()) * F32
+    _, hs = H.gemm_fp8_silu_mul(x, D, x_scales=s, quantized=True)
+    assert ((448 * hs.double() - (g * p).abs()).abs() <= (rel + F32) * (g * p).abs()).all()
+    _, ds = H.gemm_fp8_silu_mul_backward(x, D, torch.ones((M, F), dtype=torch.float16, device="cuda"), x_scales=s)
+    slope = p * (1 + g * (1 - p))
+    e = rel * (p + (g * p * (1 - p)).abs()) + F32 * p * (1 + g.abs())
+    assert ((448 * ds[:, :n].double() - slope.abs()).abs() <= e + F32 * slope.abs()).all()
+    assert ((448 * ds[:, n:].double() - (g * p).abs()).abs() <= (rel + F32) * (g * p).abs()).all()
