@@ -39,7 +39,13 @@ __host__ __device__ constexpr int few_stages(int kind, int TT)
     const int n = room / few_stage_bytes(kind, TT);
     return n < 8 ? n : 8;
 }
-__host__ __device__ constexpr int few_smem(int kind, int TT) { return 2048 + few_stages(kind, TT) * few_stage_bytes(kind, TT) + few_scale_bytes(kind, TT); }
+// With 113 KB two CTAs fill an SM's 228 KB (1 KB goes with each), and neither fits beside one of the kernels that take all 512 columns of tensor memory
+// (116736 bytes and more).  Such a pair on one SM, of two streams' clusters, each with its columns on one SM and waiting for them on another, would never end.
+__host__ __device__ constexpr int few_smem(int kind, int TT)
+{
+    const int need = 2048 + few_stages(kind, TT) * few_stage_bytes(kind, TT) + few_scale_bytes(kind, TT);
+    return need < 113 * 1024 ? 113 * 1024 : need;
+}
 // the parts of the sums that land in the idle ring: of each of S CTAs, of every S-th token row (S divides TT)
 __host__ __device__ constexpr int few_parts_bytes(int kind, int TT) { return TT * few_parts(kind) * 512; }
 
@@ -91,6 +97,7 @@ fp8_few_kernel(const Fp8FewArgs a, const __grid_constant__ CUtensorMap x_map, co
     constexpr int NS = few_stages(KIND, TT), kStage = few_stage_bytes(KIND, TT), kW = G * 128 * kFp8Block, kScale = G * TT * 4;
     constexpr uint32_t kCols = few_columns(KIND, TT);
     static_assert(NS >= 2 && COLS % 16 == 0, "");
+    static_assert(kCols <= 512 / few_per_sm(KIND, TT) && few_per_sm(KIND, TT) * (few_smem(KIND, TT) + 1024) <= 228 * 1024, "tensor memory and shared memory of an SM");
     static_assert(few_parts_bytes(KIND, TT) <= NS * kStage, "the parts would run over the scales");
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t bar_full = base, bar_empty = base + 64, bar_dfull = base + 128, bar_dempty = base + 160, tmem_slot = base + 192, flag = base + 196;

@@ -1,6 +1,7 @@
 """Layers in 8-bit floating point, what needs no GPU: waits, refusals, the harness's streams and devices, sizes, the quotient."""
 import ctypes
 import ctypes.util
+import itertools
 import os
 import re
 
@@ -240,3 +241,39 @@ def test_the_quotient_decides_as_the_nearest_number_does():
     assert pairs == 205
     got, want = (torch.tensor(np.array(a, dtype=f)).clamp(max=448.0).to(torch.float8_e4m3fn).view(torch.uint8) for a in (got, want))
     assert torch.equal(got, want)
+
+
+# ------------------------------------------------------------------------------------------------ tensor memory of an SM
+SM_BYTES, CTA_BYTES = 228 * 1024, 1024      # shared memory of an SM, and what each CTA takes of it beside its own
+
+
+def fp8_residents():
+    """(bytes, columns) of each instance of the e4m3 kernels."""
+    out = set()
+    for gated in (0, 1):
+        for M in (1, 16, 20, 32, 40, 64, 100, 128, 3000):
+            st, p = B.gptq_plan_fp8(M, 22016, 4096, gated, 148)
+            assert st == B.GPTQ_OK
+            name = p.kernel_name.decode()
+            if p.kernel == 6:
+                kind, rows = (int(v) for v in re.findall(r"\d+", name.split("<")[1]))
+                columns = (1 + kind) * rows * (4 if (1 + kind) * rows <= 128 else 2)      # accumulators of a block of K each
+                out.add((name, p.smem_bytes, max(32, columns)))
+            else:
+                out.add((name, p.smem_bytes, 512))
+    assert len(out) >= 8
+    return out
+
+
+def test_e4m3_kernels_never_wait_for_tensor_memory_beside_another_kernel():
+    """A CTA that waits for columns holds its cluster up, whose other CTAs may hold columns that the first one's neighbour's cluster waits for: kernels on one
+    SM together must fit into its 512 columns.  The 4-bit kernels take at least these bytes: for all columns more than half of an SM's, for 256 more than a
+    third, for 128 more than a quarter."""
+    others = [("all columns", 227 * 1024 // 2 + 512, 512), ("two per SM", 227 * 1024 // 3 + 512, 256), ("three per SM", 227 * 1024 // 4 + 512, 128)]
+    mine = sorted(fp8_residents())
+    for first in mine:
+        for n in range(1, 4):
+            for rest in itertools.combinations_with_replacement(mine + others, n):
+                together = (first, *rest)
+                if sum(b + CTA_BYTES for _, b, _ in together) <= SM_BYTES:
+                    assert sum(c for _, _, c in together) <= 512, together
