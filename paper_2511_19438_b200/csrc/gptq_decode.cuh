@@ -799,7 +799,7 @@ inline DecodePlan plan_decode(int M, int N, int K, int group_size, int fuse, int
     }
     pl.use = best >= 0 && fixed_time + per_item * items < other;
     pl.ctas = pl.clusters * pl.S;
-    const int floor_two_per_sm = (227 * 1024) / 3 + 512;                 // no third CTA: tensor memory holds two
+    const int floor_two_per_sm = tmem_smem_floor(kDecodeCols);           // no third CTA: tensor memory holds two
     if (pl.smem_bytes < floor_two_per_sm) pl.smem_bytes = floor_two_per_sm;
     return pl;
 }

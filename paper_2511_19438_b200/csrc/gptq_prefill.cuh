@@ -757,7 +757,7 @@ inline PrefillPlan plan_prefill(int M, int N, int K, int group_size, int sm_coun
     pl.ctas = pl.S > 1 ? pl.tiles * pl.S : pl.tiles < sm_count ? pl.tiles : sm_count;
     pl.x_slots = prefill_x_slots(pl.tok, w8);
     pl.smem_bytes = 2048 + prefill_ring_bytes(pl.tok, w8) + pl.x_slots * pl.tok * 256;
-    const int floor_one_per_sm = (227 * 1024) / 2 + 512;                 // the CTA owns all tensor memory
+    const int floor_one_per_sm = tmem_smem_floor(512);                   // the CTA owns all tensor memory
     if (pl.smem_bytes < floor_one_per_sm) pl.smem_bytes = floor_one_per_sm;
     return pl;
 }

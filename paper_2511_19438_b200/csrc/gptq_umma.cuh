@@ -48,6 +48,10 @@ constexpr int kUmmaWBlockBytes = 4096;   // packed weights of one K64 block of a
 constexpr int kUmmaDoneRing = 16;        // "block multiplied" barriers, indexed by block number mod 16
 
 // ---- tcgen05 wrappers ------------------------------------------------------------------------
+// Least shared memory of a CTA that takes `cols` columns of tensor memory: CTAs that are on an SM together, of whatever kernels, must fit into its 512 columns.
+// One that has to wait for columns holds its cluster up; if the cluster of the CTA that has them waits, on another SM, for columns of the first one,
+// neither ends.  The smallest CTAs have 57.25 KB and 128 columns: none goes beside 175 KB (all columns) and none beside two of 84 KB (256 columns each).
+__host__ __device__ constexpr int tmem_smem_floor(int cols) { return cols > 256 ? 175 * 1024 : cols > 128 ? 84 * 1024 : (227 * 1024) / 4 + 512; }
 __device__ __forceinline__ void tmem_alloc(uint32_t smem_slot, uint32_t cols)
 {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_slot), "r"(cols)
@@ -941,6 +945,8 @@ inline UmmaPlan plan_umma(int M, int N, int K, int sm_count, bool w8 = false)
         }
     }
     pl.ctas = (tiles - pl.tail_tiles) * S;
+    const int tmem_floor = tmem_smem_floor(umma_tmem_cols(tok, umma_a_stages(tok, np), np, umma_issuers(tok, sets)));
+    if (pl.smem_bytes < tmem_floor) pl.smem_bytes = tmem_floor;
     return pl;
 }
 

@@ -327,7 +327,7 @@ inline Umma2Plan plan_umma2(int M, int N, int K)
     pl.stages = stages;
     pl.ctas = (N / kPanel) * ((M + kUmma2Tok - 1) / kUmma2Tok);
     pl.smem_bytes = 2048 + stages * stage;
-    const int floor_one_per_sm = (227 * 1024) / 2 + 512;     // one CTA per SM: the pair owns all tensor memory
+    const int floor_one_per_sm = tmem_smem_floor(kUmma2Cols);     // one CTA per SM: the pair owns all tensor memory
     if (pl.smem_bytes < floor_one_per_sm) pl.smem_bytes = floor_one_per_sm;
     return pl;
 }
