@@ -163,8 +163,8 @@ __global__ void __launch_bounds__(256) fp8_transpose_kernel(const uint8_t *w, co
 //   warp 2  products of scales, two blocks ahead: 128 rows x 2 weight blocks per block of K into a ring of four
 //   warps 4 to 11 drain.  The first four give registers to them: 128 sums and 32 columns on their way.
 // What bounds it, by stamps of %clock: two accumulators, so that two blocks of K take an MMA (512 clocks), a drain (720) and both ways between the
-// MMA thread and the drain warps of two SMs (800): 1000 clocks per block; and the power limit (1.5 to 1.7 GHz in that loop).  4096 x 4096 x 12288: 211 us,
-// 1.95 PFLOP/s.  Tried and slower: accumulators of half a tile, four of them (304 us: the MMAs read their rows twice, and the drain warps wait twice as
+// MMA thread and the drain warps of two SMs (800): 1000 clocks per block; and the power limit (1.5 to 1.7 GHz in that loop).  4096 x 4096 x 12288: 199 us (2.07
+// PFLOP/s) on a cool card to 230 at the power limit.  Tried and slower: accumulators of half a tile, four of them (304 us: the MMAs read their rows twice, and the drain warps wait twice as
 // often), 16 drain warps (304: instruction issue), one CTA per tile of 128 x 256 (356; gated kinds the same), results sent during the next tile (255).
 constexpr int kFp8TileM = 256, kFp8TileN = 256, kFp8HalfM = 128, kFp8Stages = 4;
 constexpr int kFp8FirstDrain = 4, kFp8DrainWarps = 8, kFp8Threads = 32 * (kFp8FirstDrain + kFp8DrainWarps);

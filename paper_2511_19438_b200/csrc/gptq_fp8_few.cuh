@@ -6,8 +6,8 @@
 // column's scale comes from shared memory, where a warp of its own puts the products of both scales ahead of time.
 // At the end the CTAs of a cluster hand each other the sums of the token rows that each finishes (rank r: r, r + S, ...); a warp
 // finishes a whole row of 128 columns: it adds the parts in a fixed order, and has the maximum that e4m3 results need at hand.
-// Measured (device, weights from memory): 1 row 4096 x 4096 6.1 us, 16 rows 4096 x 12288 12.0 (4.2 TB/s), 48 rows 14.1, 128 rows 17.8; gated 4096 x 11008 1 row 18.2
-// (4.9 TB/s).  What bounds it: launch, first loads and the exchange (4 us), above 16 rows the drain warps (100 clocks per block of K and 190 per 16 columns).
+// Measured (device, weights from memory): 1 row 4096 x 4096 6.2 us, 16 rows 4096 x 12288 12.0 (4.2 TB/s), 48 rows 13.9, 128 rows 17.0; gated 4096 x 11008 1 row 18.4
+// (4.9 TB/s), 64 rows 23.6.  What bounds it: launch, first loads and the exchange (4 us), above 16 rows the drain warps (100 clocks per block of K and 190 per 16 columns).
 // Nothing per weight passes through an execution unit: mma.sync has no e4m3 here (it is converted to fp16 first, 283 instructions per 2 KB of weights
 // and warp; 1 row 4096 x 4096 7.4 us, gated 4096 x 11008 26).
 #pragma once
