@@ -368,6 +368,12 @@ def _format_of(dtype: torch.dtype) -> int:
     return B.GPTQ_FORMAT_BF16 if dtype == torch.bfloat16 else 0
 
 
+def _result_dtype(x: torch.Tensor, x_scales: torch.Tensor | None, dtype: torch.dtype | None) -> torch.dtype:
+    if x_scales is None and dtype not in (None, x.dtype):
+        raise ValueError(f"the result of {x.dtype} rows is {x.dtype}, not {dtype}")
+    return x.dtype if x_scales is None else dtype or torch.float16
+
+
 def _expect_rows(x: torch.Tensor, x_scales: torch.Tensor | None, dtype: torch.dtype, D: DeviceFp8Linear) -> int:
     M = x.shape[0]
     _expect("x", x, dtype if x_scales is None else torch.float8_e4m3fn, (M, D.K))
@@ -401,7 +407,7 @@ def gemm_fp8(x: torch.Tensor, D: DeviceFp8Linear, bias: torch.Tensor | None = No
              stream=None) -> torch.Tensor:
     """y = x w^T + bias + residual through gptq_gemm_fp8: x 16-bit (workspace: ensure_for_fp8), or e4m3 with ``x_scales`` and the
     ``dtype`` of the result."""
-    dtype = x.dtype if x_scales is None else dtype or torch.float16
+    dtype = _result_dtype(x, x_scales, dtype)
     fmt = _format_of(dtype)
     M = _expect_rows(x, x_scales, dtype, D)
     if y is None:
@@ -418,7 +424,7 @@ def gemm_fp8_silu_mul(x: torch.Tensor, D: DeviceFp8Linear, x_scales: torch.Tenso
                       dtype: torch.dtype | None = None, stream=None):
     """silu(gate) * up [M, N / 2] through gptq_gemm_fp8_silu_mul, D's rows = gate's, then up's: 16-bit, or (``quantized``) e4m3 and
     its scales."""
-    dtype = x.dtype if x_scales is None else dtype or torch.float16
+    dtype = _result_dtype(x, x_scales, dtype)
     fmt = _format_of(dtype)
     M, F = _expect_rows(x, x_scales, dtype, D), _gated_columns(D)
     out, s = _rows_fp8(M, F, x.device) if quantized else (torch.empty((M, F), dtype=dtype, device=x.device), None)

@@ -277,3 +277,14 @@ def test_e4m3_kernels_never_wait_for_tensor_memory_beside_another_kernel():
                 together = (first, *rest)
                 if sum(b + CTA_BYTES for _, b, _ in together) <= SM_BYTES:
                     assert sum(c for _, _, c in together) <= 512, together
+
+
+def test_rows_of_16_bits_give_results_of_their_own_type(calls):
+    """Another type that was asked for was passed over without a word."""
+    x, D = torch.zeros((4, 256), dtype=torch.float16), layer(256, 256)
+    for fn in (H.gemm_fp8, H.gemm_fp8_silu_mul):
+        with pytest.raises(ValueError, match="bfloat16"):
+            fn(x, D, dtype=torch.bfloat16)
+        assert fn(x, D, dtype=torch.float16).dtype == fn(x, D).dtype == torch.float16
+        x8, s = x.to(torch.float8_e4m3fn), torch.ones((4, 2))
+        assert fn(x8, D, x_scales=s).dtype == torch.float16 and fn(x8, D, x_scales=s, dtype=torch.bfloat16).dtype == torch.bfloat16
